@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libscheinfer.so (see include/scheinfer.h for the contract).
+"""Thin ctypes binding of libscheinfer.so (see include/scheinfer*.h for the contract).
 
 Argument marshalling only: every step of the layer runs in the library's HIP kernels / host
 workers.  PyTorch appears only as the owner of device memory and streams in the callers.
@@ -24,8 +24,13 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_layer_create_q4", "si_repack_chunks_q4", "si_cc_compute_q4", "si_layer_create_placed", "si_place_experts", "si_layer_resplit",
            # scheinfer_solver.h
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
-           "si_assign_gpu_memory", "si_profile", "si_measure_peaks"]
+           "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
+           # scheinfer_attention.h
+           "si_norm"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
+SI_F32, SI_BF16 = 0, 1
+SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
+SI_NORM_MAX_D = 32768
 
 
 class si_layer_desc_t(ctypes.Structure):
@@ -95,6 +100,16 @@ class si_profile_result_t(ctypes.Structure):
     _fields_ = [("model", si_perf_model_t), ("r2_g", ctypes.c_double), ("r2_c", ctypes.c_double),
                 ("r2_c2g", ctypes.c_double), ("sigma_launch", ctypes.c_double), ("n_points", ctypes.c_int32)] + \
                [(n, ctypes.c_double * SI_PROFILE_MAX_SIZES) for n in ("n_gemm", "t_g", "t_c", "bytes", "t_c2g")]
+
+
+def _fields(pointers, int64s, int32s, floats=""):
+    return ([(n, ctypes.c_void_p) for n in pointers.split()] + [(n, ctypes.c_int64) for n in int64s.split()] +
+            [(n, ctypes.c_int32) for n in int32s.split()] + [(n, ctypes.c_float) for n in floats.split()])
+
+
+class si_norm_t(ctypes.Structure):
+    _fields_ = _fields("r y gate w_post b_post w_pre b_pre r_out out", "r_stride y_stride gate_stride r_out_stride out_stride",
+                       "rows d r_type y_type gate_type w_type r_out_type out_type post pre", "eps res_scale y_scale")
 
 
 SI_K_NAMES = ["route", "decode_gateup", "decode_down", "decode_combine", "prefill_gateup", "prefill_down",
@@ -181,6 +196,8 @@ def lib():
         L.si_measure_peaks.argtypes = [i32, ctypes.POINTER(si_peaks_t)]
         L.si_profile.restype = ctypes.c_int
         L.si_profile.argtypes = [ctypes.POINTER(si_profile_desc_t), ctypes.POINTER(si_profile_result_t)]
+        L.si_norm.restype = ctypes.c_int
+        L.si_norm.argtypes = [ctypes.POINTER(si_norm_t), vp]
         _lib = L
     return _lib
 
@@ -476,3 +493,10 @@ def si_measure_peaks(device=0) -> dict:
     out = si_peaks_t()
     _check(lib().si_measure_peaks(device, ctypes.byref(out)))
     return {n: getattr(out, n) for n, _ in si_peaks_t._fields_}
+
+
+# ---------------------------------------------------------------- scheinfer_attention.h
+# Descriptors (si_norm_t, ...) are made once and passed to every call; their pointers are device addresses (tensor.data_ptr()).
+def si_norm(desc, stream=0):
+    """r_out = res_scale r + y_scale gate N1(y), out = N2 of it; desc: si_norm_t."""
+    _check(lib().si_norm(ctypes.byref(desc), stream))
