@@ -66,6 +66,80 @@ typedef struct {
 } si_norm_t;
 int si_norm(const si_norm_t* desc, void* stream);
 
+/* ------------------------------------------------------------------------------------------------ the cache
+ * Keys and values lie in pages of page_tokens tokens each; a page is one contiguous run over all layers, so that a page moves as one:
+ *   pages [n_pages][n_layers][2: K, V][n_kv_heads][page_tokens / B blocks]
+ * with E = 16 bytes / element size (8 bf16, 16 e4m3) and blocks of B = 4 E tokens, laid out as the matrix instructions take them:
+ *   K block [head_dim / E][B slots][E]: elements E c .. E c + E - 1 of the token in a slot; token t of the block is in slot
+ *                                       (t % E / 4) * 16 + 4 * (t / E) + t % 4
+ *   V block [4][head_dim][E]:           tokens E g .. E g + E - 1 of an element
+ * si_kv_offsets gives the place of one element.  A stored e4m3 code (OCP, 448 the largest) stands for code * scale of its head.
+ *
+ * table [n_seqs][max_pages]: page of each page_tokens tokens of a sequence, -1 where it has none; lens [n_seqs]; refs [n_pages]: how many
+ * places of the table name the page, 0: it is free.  The page calls keep the three consistent; a program that starts with an empty
+ * cache fills table with -1 and the others with 0.
+ */
+#define SI_KV_BF16 0
+#define SI_KV_E4M3 1
+
+/* bits of *status */
+#define SI_CACHE_BAD_SEQ 1   /* a sequence number outside the table, or one that a call may not name (twice) */
+#define SI_CACHE_BAD_LEN 2   /* a length or position that is negative, beyond the table, or more than there is */
+#define SI_CACHE_BAD_PAGE 4  /* a page number outside the pool (or -1) where a page has to be, or a reference count of a page that does not fit */
+#define SI_CACHE_NO_PAGES 8  /* more pages needed than are free */
+#define SI_CACHE_NO_ROOM 16  /* more tokens than the output arrays hold */
+
+typedef struct {
+  void* pages;            /* the pool, 16-byte aligned */
+  const float* scale_k;   /* [n_kv_heads], e4m3 only; NULL: 1 */
+  const float* scale_v;
+  int32_t* table;         /* [n_seqs][max_pages] */
+  int32_t* lens;          /* [n_seqs] */
+  int32_t* refs;          /* [n_pages]; may be NULL for si_cache_append and si_attend */
+  int32_t* status;        /* [1] */
+  void* scratch;          /* si_cache_scratch_bytes bytes, 16-byte aligned, zero before the first call that uses it and left so by every
+                             call: the page calls only */
+  int32_t n_pages;        /* >= 1 */
+  int32_t page_tokens;    /* a multiple of B: 32 (bf16) or 64 (e4m3) */
+  int32_t n_layers;
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* bf16: 64, 96, 128, 192 or 256; e4m3: 64, 128, 192 or 256 */
+  int32_t type;           /* SI_KV_* */
+  int32_t n_seqs, max_pages;
+} si_cache_t;
+
+/* Element offsets inside a page, from its first: K and V of element `dim` of the token at position t_in_page (host, no GPU needed).
+ * Errors: SI_EINVAL (bad descriptor, an index outside it). */
+int si_kv_offsets(const si_cache_t* cache, int32_t layer, int32_t kv_head, int32_t t_in_page, int32_t dim, int64_t* k_offset, int64_t* v_offset);
+
+/*
+ * New tokens into the cache: for token i, with s = seq[i] and p = pos[i],
+ *   q_out[i] = R(p) q[i],   K of (s, p) = R(p) k[i],   V of (s, p) = v[i]
+ * R(p) turns the first rot_dim elements of every head by the angles p * inv_freq[j], j < rot_dim / 2, formed in 64 bits: elements j and
+ * j + rot_dim / 2, or with rot_pairs elements 2 j and 2 j + 1, become (a cos - b sin, b cos + a sin).  The rest stays as it is.  Everything in
+ * fp32, rounded once; e4m3: x / scale of the head, cut to +-448, rounded to nearest even (NaN stays NaN).
+ * Nothing else of the cache changes: si_cache_extend has given the tokens their pages and counted them.
+ * A token with seq -1 is left out (q_out is 0), so that a recorded graph may have more tokens than a step needs.  So is, with
+ * a bit in *status, one whose sequence, position or page is not there.  A place that two tokens of a call name gets one of them.
+ * Strides are in elements between tokens, at least the row they stride (or 0 where there is one token); q, k and v may be slices of one
+ * projection.  q == NULL: keys and values only.
+ * Errors: SI_EINVAL (NULL or misaligned pointer: 2 bytes for rows, 4 for the others; rot_dim odd, negative or beyond head_dim; rot_dim without
+ * inv_freq; n_heads not a multiple of n_kv_heads or above 4096; layer outside the cache; bad cache descriptor; more than 2^22 tokens, or more
+ * than 2^33 elements of k, in one call), SI_EHIP.  n_tokens == 0 is a no-op.
+ */
+typedef struct {
+  const void* q;         /* bf16 [n_tokens][n_heads][head_dim], or NULL */
+  const void* k;         /* bf16 [n_tokens][n_kv_heads][head_dim] */
+  const void* v;
+  void* q_out;           /* bf16 [n_tokens][n_heads][head_dim]; may be q */
+  const int32_t* seq;    /* [n_tokens] */
+  const int32_t* pos;
+  const float* inv_freq; /* [rot_dim / 2], NULL where rot_dim == 0 */
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  int32_t n_tokens, n_heads, rot_dim, rot_pairs;
+} si_append_t;
+int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* desc, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

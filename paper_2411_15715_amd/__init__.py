@@ -26,11 +26,13 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
-           "si_norm"]
+           "si_norm", "si_kv_offsets", "si_cache_append"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
 SI_F32, SI_BF16 = 0, 1
 SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
 SI_NORM_MAX_D = 32768
+SI_KV_BF16, SI_KV_E4M3 = 0, 1
+SI_CACHE_BAD_SEQ, SI_CACHE_BAD_LEN, SI_CACHE_BAD_PAGE, SI_CACHE_NO_PAGES, SI_CACHE_NO_ROOM = 1, 2, 4, 8, 16
 
 
 class si_layer_desc_t(ctypes.Structure):
@@ -110,6 +112,15 @@ def _fields(pointers, int64s, int32s, floats=""):
 class si_norm_t(ctypes.Structure):
     _fields_ = _fields("r y gate w_post b_post w_pre b_pre r_out out", "r_stride y_stride gate_stride r_out_stride out_stride",
                        "rows d r_type y_type gate_type w_type r_out_type out_type post pre", "eps res_scale y_scale")
+
+
+class si_cache_t(ctypes.Structure):
+    _fields_ = _fields("pages scale_k scale_v table lens refs status scratch", "",
+                       "n_pages page_tokens n_layers n_kv_heads head_dim type n_seqs max_pages")
+
+
+class si_append_t(ctypes.Structure):
+    _fields_ = _fields("q k v q_out seq pos inv_freq", "q_stride k_stride v_stride q_out_stride", "n_tokens n_heads rot_dim rot_pairs")
 
 
 SI_K_NAMES = ["route", "decode_gateup", "decode_down", "decode_combine", "prefill_gateup", "prefill_down",
@@ -198,6 +209,11 @@ def lib():
         L.si_profile.argtypes = [ctypes.POINTER(si_profile_desc_t), ctypes.POINTER(si_profile_result_t)]
         L.si_norm.restype = ctypes.c_int
         L.si_norm.argtypes = [ctypes.POINTER(si_norm_t), vp]
+        pc, i64 = ctypes.POINTER(si_cache_t), ctypes.c_int64
+        L.si_kv_offsets.restype = ctypes.c_int
+        L.si_kv_offsets.argtypes = [pc, i32, i32, i32, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+        L.si_cache_append.restype = ctypes.c_int
+        L.si_cache_append.argtypes = [pc, i32, ctypes.POINTER(si_append_t), vp]
         _lib = L
     return _lib
 
@@ -500,3 +516,15 @@ def si_measure_peaks(device=0) -> dict:
 def si_norm(desc, stream=0):
     """r_out = res_scale r + y_scale gate N1(y), out = N2 of it; desc: si_norm_t."""
     _check(lib().si_norm(ctypes.byref(desc), stream))
+
+
+def si_kv_offsets(cache, layer, kv_head, t_in_page, dim):
+    """(k, v): element offsets inside a page; no GPU needed."""
+    k, v = ctypes.c_int64(), ctypes.c_int64()
+    _check(lib().si_kv_offsets(ctypes.byref(cache), layer, kv_head, t_in_page, dim, ctypes.byref(k), ctypes.byref(v)))
+    return k.value, v.value
+
+
+def si_cache_append(cache, layer, desc, stream=0):
+    """Rotates q and k of new tokens and writes k and v into their pages; cache: si_cache_t, desc: si_append_t."""
+    _check(lib().si_cache_append(ctypes.byref(cache), layer, ctypes.byref(desc), stream))

@@ -36,3 +36,93 @@ def test_norm_refuses(kw):
 def test_norm_refuses_no_descriptor_and_takes_no_rows():
     assert si.lib().si_norm(None, None) == si.SI_EINVAL
     si.si_norm(norm(rows=0))
+
+
+def cache(**kw):
+    d = dict(pages=BASE, table=BASE, lens=BASE, refs=BASE, status=BASE, scratch=BASE, n_pages=4, page_tokens=64, n_layers=2, n_kv_heads=2, head_dim=64, type=si.SI_KV_BF16,
+             n_seqs=2, max_pages=2)
+    d.update(kw)
+    return si.si_cache_t(**d)
+
+
+BAD_CACHES = [dict(type=2), dict(type=-1), dict(head_dim=80), dict(head_dim=0), dict(head_dim=320), dict(head_dim=96, type=si.SI_KV_E4M3), dict(page_tokens=48),
+              dict(page_tokens=32, type=si.SI_KV_E4M3), dict(page_tokens=0), dict(page_tokens=-64), dict(page_tokens=1 << 17), dict(n_pages=0), dict(n_layers=0), dict(n_kv_heads=0),
+              dict(n_seqs=0), dict(max_pages=0), dict(max_pages=1 << 26), dict(pages=None), dict(table=None), dict(lens=None), dict(status=None), dict(pages=BASE + 8),
+              dict(table=BASE + 2), dict(lens=BASE + 1), dict(refs=BASE + 2), dict(status=BASE + 3), dict(scale_k=BASE + 2)]
+
+
+@pytest.mark.parametrize("kw", BAD_CACHES)
+def test_bad_caches_are_refused(kw):
+    refused(si.si_kv_offsets, cache(**kw), 0, 0, 0, 0)
+    refused(si.si_cache_append, cache(**kw), 0, append())
+
+
+def append(**kw):
+    d = dict(q=BASE, k=BASE, v=BASE, q_out=BASE, seq=BASE, pos=BASE, inv_freq=BASE, q_stride=256, k_stride=128, v_stride=128, q_out_stride=256, n_tokens=3,
+             n_heads=4, rot_dim=64)
+    d.update(kw)
+    return si.si_append_t(**d)
+
+
+@pytest.mark.parametrize("kw", [dict(k=None), dict(v=None), dict(seq=None), dict(pos=None), dict(q_out=None), dict(n_heads=3), dict(n_heads=0), dict(n_heads=8192, q_stride=1 << 20, q_out_stride=1 << 20),
+                                dict(rot_dim=63), dict(rot_dim=-2), dict(rot_dim=66), dict(inv_freq=None), dict(q_stride=255), dict(k_stride=127), dict(v_stride=0),
+                                dict(q_out_stride=-256), dict(k=BASE + 1), dict(seq=BASE + 2), dict(pos=BASE + 1), dict(n_tokens=-1), dict(n_tokens=1 << 23)])
+def test_append_refuses(kw):
+    assert "si_cache_append" in refused(si.si_cache_append, cache(), 0, append(**kw))
+
+
+def test_append_refuses_layers_outside_the_cache():
+    for layer in (-1, 2):
+        refused(si.si_cache_append, cache(), layer, append())
+        refused(si.si_kv_offsets, cache(), layer, 0, 0, 0)
+    assert si.lib().si_cache_append(None, 0, None, None) == si.SI_EINVAL
+    assert si.lib().si_cache_append(ctypes.byref(cache()), 0, None, None) == si.SI_EINVAL
+    si.si_cache_append(cache(), 0, append(n_tokens=0))
+
+
+@pytest.mark.parametrize("kind,E", [(si.SI_KV_BF16, 8), (si.SI_KV_E4M3, 16)])
+def test_layout_of_a_page(kind, E):
+    """Every element of a page has one place of its own, where the description says."""
+    page, K, L, d = 128, 2, 2, 64
+    c = cache(type=kind, page_tokens=page, n_kv_heads=K, n_layers=L, head_dim=d)
+    seen = set()
+    for layer in range(L):
+        for h in range(K):
+            for t in range(page):
+                for dim in range(0, d, 7):
+                    k, v = si.si_kv_offsets(c, layer, h, t, dim)
+                    block, u = t // (4 * E), t % (4 * E)
+                    slot = u % E // 4 * 16 + 4 * (u // E) + u % 4
+                    head = lambda which: ((layer * 2 + which) * K + h) * page * d  # noqa: E731
+                    assert k == head(0) + block * 4 * E * d + (dim // E * 4 * E + slot) * E + dim % E
+                    assert v == head(1) + block * 4 * E * d + (u // E * d + dim) * E + u % E
+                    seen |= {k, v}
+    assert len(seen) == 2 * L * K * page * len(range(0, d, 7)) and max(seen) < 2 * L * K * page * d
+    for bad in ((0, -1, 0, 0), (0, K, 0, 0), (0, 0, page, 0), (0, 0, -1, 0), (0, 0, 0, d), (0, 0, 0, -1)):
+        refused(si.si_kv_offsets, c, *bad)
+
+
+def test_places_of_positions_stay_inside_the_table(tmp_path):
+    """The lookup that the kernels use, built for the host: bad sequences, positions and page numbers give -1 and a reason, and no access
+    outside the table (which ends at a guard value that would be taken for a page)."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "lookup.cpp"
+    src.write_text('#include "kv_layout.h"\nextern "C" int lookup(const si_cache_t* c, int seq, int pos, int* why) { return si::kv_page_of(*c, seq, pos, *why); }\n')
+    so = str(tmp_path / "lookup.so")
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2411_15715_amd", "csrc"), "-o", so, str(src)], check=True)
+    f = ctypes.CDLL(so).lookup
+    table = np.array([3, 3] + [0, 3, -1] + [1, 4, 2] + [3, 3], np.int32)  # guard, two rows of three, guard
+    c = cache(table=table.ctypes.data + 8, n_pages=4, n_seqs=2, max_pages=3, page_tokens=32)
+
+    def at(seq, pos):
+        why = ctypes.c_int(0)
+        return f(ctypes.byref(c), seq, pos, ctypes.byref(why)), why.value
+
+    assert at(0, 0) == (0, 0) and at(0, 31) == (0, 0) and at(0, 32) == (3, 0) and at(1, 0) == (1, 0) and at(1, 95) == (2, 0)
+    assert at(0, 64) == (-1, si.SI_CACHE_BAD_PAGE) and at(1, 32) == (-1, si.SI_CACHE_BAD_PAGE)
+    for seq in (-1, 2, 1 << 30, -(1 << 31)):
+        assert at(seq, 0) == (-1, si.SI_CACHE_BAD_SEQ)
+    for pos in (-1, 96, 0x7fffffff, -(1 << 31)):
+        assert at(0, pos) == (-1, si.SI_CACHE_BAD_LEN)
