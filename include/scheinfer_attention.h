@@ -140,6 +140,43 @@ typedef struct {
 } si_append_t;
 int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* desc, void* stream);
 
+/*
+ * Attention of the last n_new tokens of n sequences over the cache (they are in it: si_cache_append came before).  Row i * n_new + j of q
+ * and out is token j of sequence seqs[i], at position lens - n_new + j; it sees the positions p with
+ *   p <= lens - n_new + j,  and with window > 0 also  p > lens - n_new + j - window,
+ * and for every head h, with kv head h / (n_heads / n_kv_heads):
+ *   out = softmax over them of (scale q . K) applied to V,   lse = ln sum exp(scale q . K)
+ * A token that sees nothing (its position is negative: lens < n_new) gets out 0 and lse -infinity.  What a token does not see has no part in
+ * its output, whatever the pages hold there, NaN and infinities included.  Products are of bf16 operands (e4m3 codes widen to bf16
+ * exactly), sums, maxima and weights fp32.
+ * max_len sizes the launch: an upper bound of lens (a sequence beyond it is still computed, by fewer blocks than it deserves).
+ * scratch: si_attend_scratch_bytes of these descriptors or more, 16-byte aligned, zero before its first use; every call leaves it fit for
+ * any other call.  Two calls that may run at once need one each.  Results do not depend on the order in which blocks run.
+ * Left out with a bit in *status: a sequence outside the table (as if its length were 0), a length that is negative or
+ * beyond the table (cut to it), a page outside the pool (its tokens are not seen).
+ * Errors: SI_EINVAL (NULL or misaligned pointer: 2 bytes for q and out, 4 for lse and seqs; n_heads not a multiple of n_kv_heads or above 4096;
+ * a stride smaller than its row; n_new < 1 or above 65536; window or max_len negative; scale not finite; scratch_bytes too small; layer outside the
+ * cache; bad cache descriptor), SI_EHIP.  n == 0 is a no-op.
+ */
+typedef struct {
+  const void* q;        /* bf16 [n * n_new][n_heads][head_dim] */
+  void* out;            /* bf16, the same shape */
+  float* lse;           /* [n * n_new][n_heads], or NULL */
+  const int32_t* seqs;  /* [n], or NULL: sequences 0 .. n - 1 */
+  void* scratch;
+  int64_t scratch_bytes;
+  int64_t q_stride, out_stride; /* elements between rows */
+  int32_t n, n_new, n_heads;
+  int32_t window;       /* 0: all */
+  int32_t max_len;
+  float scale;          /* 0: 1 / sqrt(head_dim) */
+} si_attend_t;
+int si_attend(const si_cache_t* cache, int32_t layer, const si_attend_t* desc, void* stream);
+
+/* Bytes of scratch that si_attend needs for these descriptors, or a negative SI_E* code (host only, no GPU needed; q, out, lse, scratch and
+ * scratch_bytes are not looked at). */
+int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc);
+
 #ifdef __cplusplus
 }
 #endif

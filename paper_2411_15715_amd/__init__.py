@@ -26,7 +26,7 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
-           "si_norm", "si_kv_offsets", "si_cache_append"]
+           "si_norm", "si_kv_offsets", "si_cache_append", "si_attend", "si_attend_scratch_bytes"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
 SI_F32, SI_BF16 = 0, 1
 SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
@@ -123,6 +123,10 @@ class si_append_t(ctypes.Structure):
     _fields_ = _fields("q k v q_out seq pos inv_freq", "q_stride k_stride v_stride q_out_stride", "n_tokens n_heads rot_dim rot_pairs")
 
 
+class si_attend_t(ctypes.Structure):
+    _fields_ = _fields("q out lse seqs scratch", "scratch_bytes q_stride out_stride", "n n_new n_heads window max_len", "scale")
+
+
 SI_K_NAMES = ["route", "decode_gateup", "decode_down", "decode_combine", "prefill_gateup", "prefill_down",
               "prefill_combine", "fill"]
 
@@ -214,6 +218,10 @@ def lib():
         L.si_kv_offsets.argtypes = [pc, i32, i32, i32, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]
         L.si_cache_append.restype = ctypes.c_int
         L.si_cache_append.argtypes = [pc, i32, ctypes.POINTER(si_append_t), vp]
+        L.si_attend.restype = ctypes.c_int
+        L.si_attend.argtypes = [pc, i32, ctypes.POINTER(si_attend_t), vp]
+        L.si_attend_scratch_bytes.restype = i64
+        L.si_attend_scratch_bytes.argtypes = [pc, ctypes.POINTER(si_attend_t)]
         _lib = L
     return _lib
 
@@ -528,3 +536,14 @@ def si_kv_offsets(cache, layer, kv_head, t_in_page, dim):
 def si_cache_append(cache, layer, desc, stream=0):
     """Rotates q and k of new tokens and writes k and v into their pages; cache: si_cache_t, desc: si_append_t."""
     _check(lib().si_cache_append(ctypes.byref(cache), layer, ctypes.byref(desc), stream))
+
+
+def si_attend_scratch_bytes(cache, desc) -> int:
+    n = lib().si_attend_scratch_bytes(ctypes.byref(cache), ctypes.byref(desc))
+    _check(min(n, SI_OK))
+    return n
+
+
+def si_attend(cache, layer, desc, stream=0):
+    """Attention of the last n_new tokens of each sequence over the cache; desc: si_attend_t."""
+    _check(lib().si_attend(ctypes.byref(cache), layer, ctypes.byref(desc), stream))

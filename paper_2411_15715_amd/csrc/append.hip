@@ -280,7 +280,7 @@ int check_cache(const si_cache_t* c, const char* who) {
   if (c->n_pages < 1 || c->n_layers < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_layers > (1 << 16) || c->n_seqs < 1 || c->max_pages < 1)
     return set_error(SI_EINVAL, "%s: bad n_pages=%d n_layers=%d n_kv_heads=%d n_seqs=%d max_pages=%d", who, c->n_pages, c->n_layers, c->n_kv_heads, c->n_seqs,
                      c->max_pages);
-  if ((int64_t)c->max_pages * c->page_tokens > 0x7fffffff) return set_error(SI_EINVAL, "%s: max_pages * page_tokens does not fit 31 bits", who);
+  if ((int64_t)c->max_pages * c->page_tokens > 0x7fff0000) return set_error(SI_EINVAL, "%s: max_pages * page_tokens exceeds 0x7fff0000", who);
   if (!c->pages || !c->table || !c->lens || !c->status) return set_error(SI_EINVAL, "%s: pages, table, lens or status is NULL", who);
   if (misaligned(c->pages, 16)) return set_error(SI_EINVAL, "%s: pages are not aligned to 16 bytes", who);
   if (misaligned(c->table, 4) || misaligned(c->lens, 4) || misaligned(c->refs, 4) || misaligned(c->status, 4) || misaligned(c->scale_k, 4) || misaligned(c->scale_v, 4))

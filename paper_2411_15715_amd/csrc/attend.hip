@@ -1,0 +1,88 @@
+// Attention over the paged cache: arguments, and how a call is cut into blocks.
+#include "si_internal.h"
+#include "si_error.h"
+#include "attend_device.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace si {
+namespace {
+
+struct Cut {
+  int nt, groups, splits, chunk;
+  int64_t scratch;
+};
+
+// Row tiles of a block, row groups, and the parts that a sequence of max_len is cut into.
+Cut cut(const si_cache_t& c, const si_attend_t& a) {
+  Cut k{};
+  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, most = c.head_dim <= 128 ? 4 : 2, B = kv_block(c.type);
+  k.groups = (tiles + most - 1) / most;
+  k.nt = (tiles + k.groups - 1) / k.groups;
+  int64_t seen = a.max_len;
+  if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
+  const int64_t blocks = (seen + B - 1) / B, units = (int64_t)a.n * c.n_kv_heads * k.groups;
+  k.splits = 1;
+  k.chunk = (int)std::max<int64_t>(1, blocks);
+  // about 1024 blocks in all, none with fewer than 2 cache blocks a wave
+  if (units <= ATTEND_COUNTERS && blocks > 2 * ATTEND_WAVES) {
+    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, units));
+    k.chunk = (int)std::max<int64_t>((blocks + want - 1) / want, 2 * ATTEND_WAVES);
+    k.splits = (int)((blocks + k.chunk - 1) / k.chunk);
+  }
+  if (k.splits > 1) k.scratch = (int64_t)ATTEND_COUNTERS * 4 + units * k.splits * (16 * k.nt) * (c.head_dim + 2) * 4;
+  return k;
+}
+
+bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+int check_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
+  if (int rc = check_cache(c, who)) return rc;
+  if (!a) return set_error(SI_EINVAL, "%s: descriptor is NULL", who);
+  if (a->n < 0 || a->n > 65535) return set_error(SI_EINVAL, "%s: n %d outside 0 .. 65535", who, a->n);
+  if (a->n_new < 1 || a->n_new > 65536) return set_error(SI_EINVAL, "%s: n_new %d outside 1 .. 65536", who, a->n_new);
+  if (a->n_heads < 1 || a->n_heads > 4096 || a->n_heads % c->n_kv_heads != 0)
+    return set_error(SI_EINVAL, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, a->n_heads, c->n_kv_heads);
+  if (a->window < 0 || a->max_len < 0) return set_error(SI_EINVAL, "%s: window %d or max_len %d is negative", who, a->window, a->max_len);
+  if (!std::isfinite(a->scale)) return set_error(SI_EINVAL, "%s: scale is not finite", who);
+  const Cut k = cut(*c, *a);
+  // (a launch has fewer than 2^32 threads and fewer than 2^16 blocks along its second index)
+  if ((int64_t)c->n_kv_heads * k.groups > 65535 || (int64_t)c->n_kv_heads * k.groups * a->n * k.splits >= ((int64_t)1 << 24))
+    return set_error(SI_EINVAL, "%s: n * n_new * n_heads is too large for one call (%d, %d, %d)", who, a->n, a->n_new, a->n_heads);
+  return SI_OK;
+}
+
+}  // namespace
+}  // namespace si
+
+extern "C" int64_t si_attend_scratch_bytes(const si_cache_t* c, const si_attend_t* a) {
+  using namespace si;
+  if (int rc = check_shape(c, a, "si_attend_scratch_bytes")) return rc;
+  return cut(*c, *a).scratch;
+}
+
+extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* a, void* stream) {
+  using namespace si;
+  const char* who = "si_attend";
+  if (int rc = check_shape(c, a, who)) return rc;
+  if (int rc = check_layer(c, layer, who)) return rc;
+  if (!a->q || !a->out) return set_error(SI_EINVAL, "%s: q or out is NULL", who);
+  if (misaligned(a->q, 2) || misaligned(a->out, 2) || misaligned(a->lse, 4) || misaligned(a->seqs, 4)) return set_error(SI_EINVAL, "%s: a pointer is not aligned to its element", who);
+  if (!a->seqs && a->n > c->n_seqs) return set_error(SI_EINVAL, "%s: n %d of %d sequences", who, a->n, c->n_seqs);
+  const int64_t row = (int64_t)a->n_heads * c->head_dim;
+  if (a->q_stride < row || a->out_stride < row) return set_error(SI_EINVAL, "%s: a stride is smaller than its row", who);
+  const Cut k = cut(*c, *a);
+  if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
+    return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
+  if (a->n == 0) return SI_OK;
+  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.splits, k.chunk, 0.f, nullptr, nullptr};
+  g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
+  if (k.scratch > 0) {
+    g.count = static_cast<uint32_t*>(a->scratch);
+    g.part = reinterpret_cast<float*>(g.count + ATTEND_COUNTERS);
+  }
+  const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, k.nt, (hipStream_t)stream);
+  if (e != hipSuccess) return set_error(SI_EHIP, "attention launch failed: %s", hipGetErrorString(e));
+  return SI_OK;
+}

@@ -1,0 +1,16 @@
+// Attention over a bf16 cache: the kernels' instances (a file for each type, so that they are compiled side by side).
+#include "attend_device.h"
+
+namespace si {
+
+hipError_t launch_attend_bf16(const AttendArgs& g, int nt, hipStream_t stream) {
+  switch (g.c.head_dim) {
+    case 64: return launch_rows<SI_KV_BF16, 64, 4>(g, nt, stream);
+    case 96: return launch_rows<SI_KV_BF16, 96, 4>(g, nt, stream);
+    case 128: return launch_rows<SI_KV_BF16, 128, 4>(g, nt, stream);
+    case 192: return launch_rows<SI_KV_BF16, 192, 2>(g, nt, stream);
+    default: return launch_rows<SI_KV_BF16, 256, 2>(g, nt, stream);
+  }
+}
+
+}  // namespace si

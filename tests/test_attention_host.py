@@ -126,3 +126,42 @@ def test_places_of_positions_stay_inside_the_table(tmp_path):
         assert at(seq, 0) == (-1, si.SI_CACHE_BAD_SEQ)
     for pos in (-1, 96, 0x7fffffff, -(1 << 31)):
         assert at(0, pos) == (-1, si.SI_CACHE_BAD_LEN)
+
+
+def attend(**kw):
+    d = dict(q=BASE, out=BASE, lse=BASE, q_stride=256, out_stride=256, n=2, n_new=1, n_heads=4, max_len=64)
+    d.update(kw)
+    return si.si_attend_t(**d)
+
+
+BAD_SHAPES = [dict(n=-1), dict(n=65536), dict(n_new=0), dict(n_new=65537), dict(n_heads=3), dict(n_heads=0), dict(n_heads=4098), dict(window=-1), dict(max_len=-1),
+              dict(scale=float("nan")), dict(scale=float("inf")), dict(n=65535, n_new=65536, n_heads=4096)]
+
+
+@pytest.mark.parametrize("kw", BAD_SHAPES + [dict(q=None), dict(out=None), dict(q=BASE + 1), dict(lse=BASE + 2), dict(seqs=BASE + 2), dict(q_stride=255), dict(out_stride=0), dict(n=3)])
+def test_attend_refuses(kw):
+    assert "si_attend" in refused(si.si_attend, cache(), 0, attend(**kw))
+    if kw in BAD_SHAPES:
+        refused(si.si_attend_scratch_bytes, cache(), attend(**kw))
+
+
+def test_attend_refuses_caches_layers_and_too_little_scratch():
+    for kw in BAD_CACHES:
+        refused(si.si_attend, cache(**kw), 0, attend())
+    for layer in (-1, 2):
+        refused(si.si_attend, cache(), layer, attend())
+    assert si.lib().si_attend(None, 0, None, None) == si.SI_EINVAL
+    assert si.lib().si_attend(ctypes.byref(cache()), 0, None, None) == si.SI_EINVAL
+    c, a = cache(max_pages=1000), attend(max_len=50000, scratch=BASE)
+    need = si.si_attend_scratch_bytes(c, a)
+    assert need > 0
+    for kw in (dict(scratch_bytes=need - 1), dict(scratch_bytes=need, scratch=None), dict(scratch_bytes=need, scratch=BASE + 8)):
+        assert str(need) in refused(si.si_attend, c, 0, attend(**{**dict(max_len=50000, scratch=BASE), **kw}))
+    si.si_attend(cache(), 0, attend(n=0))
+
+
+def test_scratch_grows_with_no_shape_that_needs_less():
+    """The counters' place does not depend on the call: any scratch that is large enough serves."""
+    c = cache(max_pages=4000, n_seqs=200)
+    sizes = [si.si_attend_scratch_bytes(c, attend(n=n, n_new=m, max_len=L)) for n in (1, 7, 128) for m in (1, 5, 40) for L in (0, 1, 64, 5000, 200000)]
+    assert all(s == 0 or s > 65536 for s in sizes) and max(sizes) < 1 << 30
