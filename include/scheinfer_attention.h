@@ -177,6 +177,49 @@ int si_attend(const si_cache_t* cache, int32_t layer, const si_attend_t* desc, v
  * scratch_bytes are not looked at). */
 int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc);
 
+/* ------------------------------------------------------------------------------------------------ moves of pages
+ * All act on every layer at once.  `seqs` and the like are DEVICE int32 [n], n <= SI_CACHE_MAX_LIST.  Pages are taken from the free ones (refs
+ * 0) in ascending order, in the order of the list and of the positions, so that results do not depend on scheduling.  The list of
+ * si_cache_trim is taken sequence by sequence; the other calls do all that they are asked or, with a bit in *status, nothing.
+ * cache->refs and cache->scratch are needed.
+ * Errors: SI_EINVAL (NULL or misaligned pointer, n negative or above SI_CACHE_MAX_LIST, bad cache descriptor), SI_EHIP.  n == 0 is a no-op.
+ */
+#define SI_CACHE_MAX_LIST 2048
+
+/* Bytes of cache->scratch, or a negative SI_E* code (host only; pages and tables may be NULL). */
+int64_t si_cache_scratch_bytes(const si_cache_t* cache);
+
+/*
+ * Cuts sequence seqs[i] to its first keep[i] tokens (keep NULL: to nothing, i.e. frees it): rejected drafts, ended sequences.  Pages
+ * that no other sequence shares become free.  A sequence number outside the table or a length above the present one is left out.
+ */
+int si_cache_trim(const si_cache_t* cache, const int32_t* seqs, int32_t n, const int32_t* keep, void* stream);
+
+/*
+ * Adds counts[i] tokens (counts NULL: n_new) to sequence seqs[i] and gives them pages.  A partly filled last page that other
+ * sequences share is replaced by a copy first (the last of its sharers keeps it).  The new tokens, in list order and ascending
+ * positions, are written to seq_out / pos_out, -1 from there to `capacity`: the arrays that si_cache_append takes (both NULL: not wanted).
+ * Nothing is done, seq_out is all -1, and *status has a bit, where a sequence is outside the table or named twice, a length is bad or grows
+ * beyond the table's row, more than `capacity` tokens are added, or pages run out (looked at in this order).
+ */
+int si_cache_extend(const si_cache_t* cache, const int32_t* seqs, int32_t n, const int32_t* counts, int32_t n_new, int32_t* seq_out, int32_t* pos_out,
+                    int32_t capacity, void* stream);
+
+/*
+ * Makes sequence children[i], which has to be empty, a copy of parents[i]: full pages are shared, a partly filled last one is copied (a parent's
+ * once read, however many children it has).  A sequence may be the parent of several, but not a parent and a child in one call.
+ */
+int si_cache_fork(const si_cache_t* cache, const int32_t* parents, const int32_t* children, int32_t n, void* stream);
+
+/*
+ * Packs the pool: of m pages in use, those with a number below m keep it, the others move, in ascending order, into the free places below m.
+ * `to` is a cache of the same shape but for n_pages (>= m), whose pages, table, lens and refs are written (its status and scratch are not used), or
+ * the same cache: then it is packed in place.  Anything between (some arrays shared, pools that overlap) is allowed for whole arrays
+ * only: each of to's four is either the cache's own or memory of its own.  n_used, DEVICE [1] or NULL, receives m.  Where m exceeds to's
+ * n_pages, nothing else is written.
+ */
+int si_cache_compact(const si_cache_t* cache, const si_cache_t* to, int32_t* n_used, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,12 +26,14 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
-           "si_norm", "si_kv_offsets", "si_cache_append", "si_attend", "si_attend_scratch_bytes"]
+           "si_norm", "si_kv_offsets", "si_cache_append", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
+           "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
 SI_F32, SI_BF16 = 0, 1
 SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
 SI_NORM_MAX_D = 32768
 SI_KV_BF16, SI_KV_E4M3 = 0, 1
+SI_CACHE_MAX_LIST = 2048
 SI_CACHE_BAD_SEQ, SI_CACHE_BAD_LEN, SI_CACHE_BAD_PAGE, SI_CACHE_NO_PAGES, SI_CACHE_NO_ROOM = 1, 2, 4, 8, 16
 
 
@@ -222,6 +224,16 @@ def lib():
         L.si_attend.argtypes = [pc, i32, ctypes.POINTER(si_attend_t), vp]
         L.si_attend_scratch_bytes.restype = i64
         L.si_attend_scratch_bytes.argtypes = [pc, ctypes.POINTER(si_attend_t)]
+        L.si_cache_scratch_bytes.restype = i64
+        L.si_cache_scratch_bytes.argtypes = [pc]
+        L.si_cache_trim.restype = ctypes.c_int
+        L.si_cache_trim.argtypes = [pc, vp, i32, vp, vp]
+        L.si_cache_extend.restype = ctypes.c_int
+        L.si_cache_extend.argtypes = [pc, vp, i32, vp, i32, vp, vp, i32, vp]
+        L.si_cache_fork.restype = ctypes.c_int
+        L.si_cache_fork.argtypes = [pc, vp, vp, i32, vp]
+        L.si_cache_compact.restype = ctypes.c_int
+        L.si_cache_compact.argtypes = [pc, pc, vp, vp]
         _lib = L
     return _lib
 
@@ -547,3 +559,30 @@ def si_attend_scratch_bytes(cache, desc) -> int:
 def si_attend(cache, layer, desc, stream=0):
     """Attention of the last n_new tokens of each sequence over the cache; desc: si_attend_t."""
     _check(lib().si_attend(ctypes.byref(cache), layer, ctypes.byref(desc), stream))
+
+
+def si_cache_scratch_bytes(cache) -> int:
+    n = lib().si_cache_scratch_bytes(ctypes.byref(cache))
+    _check(min(n, SI_OK))
+    return n
+
+
+# Lists are device addresses of int32 arrays of n entries.
+def si_cache_trim(cache, seqs, n, keep=None, stream=0):
+    """Cuts sequences to keep tokens (None: frees them)."""
+    _check(lib().si_cache_trim(ctypes.byref(cache), seqs, n, keep, stream))
+
+
+def si_cache_extend(cache, seqs, n, counts, n_new, seq_out, pos_out, capacity, stream=0):
+    """Adds counts (None: n_new each) tokens to sequences; writes the tokens' sequences and positions."""
+    _check(lib().si_cache_extend(ctypes.byref(cache), seqs, n, counts, n_new, seq_out, pos_out, capacity, stream))
+
+
+def si_cache_fork(cache, parents, children, n, stream=0):
+    """Makes empty sequences copies of others, full pages shared."""
+    _check(lib().si_cache_fork(ctypes.byref(cache), parents, children, n, stream))
+
+
+def si_cache_compact(cache, to, n_used=None, stream=0):
+    """Packs the pages in use into the pool of `to` (or in place, to = cache)."""
+    _check(lib().si_cache_compact(ctypes.byref(cache), ctypes.byref(to), n_used, stream))

@@ -109,3 +109,114 @@ def attend64(q, k, v, n_new, window, scale):
             out[j, h] = p @ vv
             mag_o[j, h] = p @ np.abs(vv)
     return out, lse, mag_s, mag_o
+
+
+class Books:
+    """The page calls on Python integers.  content[p]: which page's original content page p holds."""
+
+    def __init__(self, cache):
+        self.page = cache.page
+        self.table, self.lens, self.refs = (t.cpu().numpy().astype(np.int64) for t in (cache.table, cache.lens, cache.refs))
+        self.content = np.arange(len(self.refs))
+
+    def pages_of(self, length):
+        return -(-length // self.page)
+
+    def _try(self, f):
+        """all or nothing"""
+        keep = [a.copy() for a in (self.table, self.lens, self.refs, self.content)]
+        try:
+            return f(), 0
+        except _Refused as e:
+            self.table, self.lens, self.refs, self.content = keep
+            return None, e.bit
+
+    def _take(self):
+        free = np.flatnonzero(self.refs <= 0)
+        if len(free) == 0:
+            raise _Refused(si.SI_CACHE_NO_PAGES)
+        self.refs[free[0]] = 1
+        return int(free[0])
+
+    def trim(self, seqs, keep=None):
+        status = 0
+        for i, s in enumerate(seqs):
+            k = 0 if keep is None else keep[i]
+            if k < 0:
+                status |= si.SI_CACHE_BAD_LEN
+            elif not 0 <= s < len(self.lens):
+                status |= si.SI_CACHE_BAD_SEQ
+            elif k > self.lens[s]:
+                status |= si.SI_CACHE_BAD_LEN
+            else:
+                for j in range(self.pages_of(k), self.pages_of(self.lens[s])):
+                    self.refs[self.table[s, j]] -= 1
+                    self.table[s, j] = -1
+                self.lens[s] = k
+        return status
+
+    def extend(self, seqs, counts, capacity):
+        def f():
+            out, seen = [], set()
+            for s, m in zip(seqs, counts):
+                if not 0 <= s < len(self.lens) or s in seen:
+                    raise _Refused(si.SI_CACHE_BAD_SEQ)
+                seen.add(s)
+                if m < 0 or self.lens[s] + m > self.table.shape[1] * self.page:
+                    raise _Refused(si.SI_CACHE_BAD_LEN)
+            if sum(counts) > capacity:
+                raise _Refused(si.SI_CACHE_NO_ROOM)
+            for s, m in zip(seqs, counts):
+                for p in range(self.lens[s], self.lens[s] + m):
+                    j = p // self.page
+                    old = self.table[s, j]
+                    if p % self.page == 0:
+                        self.table[s, j] = self._take()
+                    elif self.refs[old] > 1:
+                        new = self._take()
+                        self.content[new] = self.content[old]
+                        self.refs[old] -= 1
+                        self.table[s, j] = new
+                    out.append((s, p))
+                self.lens[s] += m
+            return out
+        out, status = self._try(f)
+        out = out or []
+        return out + [(-1, -1)] * (capacity - len(out)), status
+
+    def fork(self, parents, children):
+        def f():
+            if len(set(children)) < len(children) or set(children) & set(parents):
+                raise _Refused(si.SI_CACHE_BAD_SEQ)
+            for a, b in zip(parents, children):
+                if not (0 <= a < len(self.lens) and 0 <= b < len(self.lens)):
+                    raise _Refused(si.SI_CACHE_BAD_SEQ)
+                if self.lens[b] != 0:
+                    raise _Refused(si.SI_CACHE_BAD_LEN)
+            for a, b in zip(parents, children):
+                for j in range(self.pages_of(self.lens[a])):
+                    p = self.table[a, j]
+                    if (j + 1) * self.page > self.lens[a]:
+                        new = self._take()
+                        self.content[new] = self.content[p]
+                        p = new
+                    else:
+                        self.refs[p] += 1
+                    self.table[b, j] = p
+                self.lens[b] = self.lens[a]
+        return self._try(f)[1]
+
+    def compact(self):
+        """(new number of each page or -1, number in use)"""
+        used = self.refs > 0
+        m = int(used.sum())
+        place = np.full(len(self.refs), -1)
+        holes = [p for p in range(m) if not used[p]]
+        for p in np.flatnonzero(used):
+            place[p] = p if p < m else holes.pop(0)
+        return place, m
+
+
+class _Refused(Exception):
+    def __init__(self, bit):
+        self.bit = bit

@@ -165,3 +165,47 @@ def test_scratch_grows_with_no_shape_that_needs_less():
     c = cache(max_pages=4000, n_seqs=200)
     sizes = [si.si_attend_scratch_bytes(c, attend(n=n, n_new=m, max_len=L)) for n in (1, 7, 128) for m in (1, 5, 40) for L in (0, 1, 64, 5000, 200000)]
     assert all(s == 0 or s > 65536 for s in sizes) and max(sizes) < 1 << 30
+
+
+def moves(c):
+    """every page call with these lists, on cache c"""
+    return {"si_cache_trim": lambda a=BASE, n=2, k=BASE: si.si_cache_trim(c, a, n, k),
+            "si_cache_extend": lambda a=BASE, n=2, k=BASE: si.si_cache_extend(c, a, n, k, 1, BASE, BASE, 8),
+            "si_cache_fork": lambda a=BASE, n=2, k=BASE: si.si_cache_fork(c, a, k, n),
+            "si_cache_compact": lambda a=BASE, n=2, k=BASE: si.si_cache_compact(c, c, BASE)}
+
+
+@pytest.mark.parametrize("kw", BAD_CACHES + [dict(refs=None), dict(scratch=None), dict(scratch=BASE + 8)])
+def test_moves_refuse_bad_caches(kw):
+    for name, f in moves(cache(**kw)).items():
+        assert name in refused(f)
+
+
+def test_moves_refuse_bad_lists():
+    for name, f in moves(cache()).items():
+        if name == "si_cache_compact":
+            continue
+        for kw in (dict(a=None), dict(a=BASE + 2), dict(k=BASE + 1), dict(n=-1), dict(n=si.SI_CACHE_MAX_LIST + 1)):
+            assert name in refused(lambda: f(**kw))
+    c = cache()
+    refused(si.si_cache_fork, c, BASE, None, 2)
+    refused(si.si_cache_extend, c, BASE, 2, None, -1, BASE, BASE, 8)
+    refused(si.si_cache_extend, c, BASE, 2, None, 1, BASE, None, 8)
+    refused(si.si_cache_extend, c, BASE, 2, None, 1, None, BASE, 8)
+    refused(si.si_cache_extend, c, BASE, 2, None, 1, BASE + 2, BASE, 8)
+    refused(si.si_cache_extend, c, BASE, 2, None, 1, BASE, BASE, -1)
+
+
+def test_compact_refuses_targets_of_another_shape():
+    c = cache()
+    for kw in (dict(page_tokens=32), dict(n_layers=1), dict(n_kv_heads=1), dict(head_dim=128), dict(type=si.SI_KV_E4M3), dict(n_seqs=3), dict(max_pages=3), dict(refs=None), dict(n_pages=0)):
+        refused(si.si_cache_compact, c, cache(**kw), None)
+    refused(si.si_cache_compact, c, c, BASE + 2)
+    assert si.lib().si_cache_compact(ctypes.byref(c), None, None, None) == si.SI_EINVAL
+
+
+def test_scratch_of_the_cache():
+    assert si.si_cache_scratch_bytes(cache(pages=None, table=None)) >= 4 * (2 + 2 * 4)
+    for kw in (dict(n_seqs=0), dict(n_pages=0)):
+        refused(si.si_cache_scratch_bytes, cache(**kw))
+    assert si.lib().si_cache_scratch_bytes(None) == si.SI_EINVAL
