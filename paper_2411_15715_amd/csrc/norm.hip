@@ -303,8 +303,10 @@ hipError_t launch_norm(const si_norm_t& a, hipStream_t stream) {
   if (slots <= 32) return launch<32, 1, 256>(a, {256, 8}, stream);
   if (slots <= 64) return launch<64, 1, 256>(a, {256, 4}, stream);
   auto shape = [&](int n) { return Shape{(slots + WAVE * n - 1) / (WAVE * n) * WAVE, 1}; };
-  // one slot a thread as long as a block has the threads: 4096 x 6144 52.8 us against 66.2 with two slots and 79.5 with four
-  if (slots <= 1024) return launch<0, 1, 1024>(a, shape(1), stream);
+  // One slot a thread: 4096 x 6144 in 45.1 us, with two 46.6 (more threads hold fewer registers each, and more rows are in flight).  Beyond 12
+  // waves a row's barriers leave too little beside it: 3000 x 8192 with N1 59.4 us with one slot, 45.1 with two (plain: 46.3, 45.5).
+  if (slots <= 768) return launch<0, 1, 768>(a, shape(1), stream);
+  if (slots <= 1024) return launch<0, 2, 512>(a, shape(2), stream);
   if (slots <= 2048) return launch<0, 4, 512>(a, shape(4), stream);
   return launch<0, 4, 1024>(a, shape(4), stream);
 }
