@@ -5,33 +5,37 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 namespace si {
 namespace {
 
 struct Cut {
-  int nt, groups, splits, chunk;
+  int tiles, groups, splits, chunk, part_rows, last_joins;
   int64_t scratch;
 };
 
-// Row tiles of a block, row groups, and the parts that a sequence of max_len is cut into.
+// Waves of a block that share cache blocks, row groups, and the parts that a sequence of max_len is cut into.
 Cut cut(const si_cache_t& c, const si_attend_t& a) {
   Cut k{};
-  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, most = c.head_dim <= 128 ? 4 : 2, B = kv_block(c.type);
-  k.groups = (tiles + most - 1) / most;
-  k.nt = (tiles + k.groups - 1) / k.groups;
+  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, B = kv_block(c.type), waves = ATTEND_WAVES;
+  for (k.tiles = 1; k.tiles < tiles && k.tiles < waves;) k.tiles *= 2;
+  k.groups = (tiles + k.tiles - 1) / k.tiles;
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
   const int64_t blocks = (seen + B - 1) / B, units = (int64_t)a.n * c.n_kv_heads * k.groups;
   k.splits = 1;
   k.chunk = (int)std::max<int64_t>(1, blocks);
-  // about 1024 blocks in all, none with fewer than 2 cache blocks a wave
-  if (units <= ATTEND_COUNTERS && blocks > 2 * ATTEND_WAVES) {
-    const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, units));
-    k.chunk = (int)std::max<int64_t>((blocks + want - 1) / want, 2 * ATTEND_WAVES);
+  k.part_rows = std::min(rows, 16 * k.tiles);
+  const int least = (getenv("ATT_MIN") ? atoi(getenv("ATT_MIN")) : 2) * (waves / k.tiles);
+  if (blocks > least) {
+    const int64_t want = std::max<int64_t>(1, (getenv("ATT_TARGET") ? atoi(getenv("ATT_TARGET")) : 256) / std::max<int64_t>(1, units));
+    k.chunk = (int)std::max<int64_t>((blocks + want - 1) / want, least);
     k.splits = (int)((blocks + k.chunk - 1) / k.chunk);
   }
-  if (k.splits > 1) k.scratch = (int64_t)ATTEND_COUNTERS * 4 + units * k.splits * (16 * k.nt) * (c.head_dim + 2) * 4;
+  k.last_joins = k.splits <= ATTEND_FEW && units <= ATTEND_COUNTERS;
+  if (getenv("ATT_JOIN")) k.last_joins = 0;
+  if (k.splits > 1) k.scratch = (int64_t)ATTEND_COUNTERS * 4 + units * k.splits * k.part_rows * (c.head_dim + 2) * 4;
   return k;
 }
 
@@ -76,13 +80,13 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
   if (a->n == 0) return SI_OK;
-  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.splits, k.chunk, 0.f, nullptr, nullptr};
+  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.splits, k.chunk, 0.f, k.part_rows, k.last_joins, nullptr, nullptr};
   g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
   if (k.scratch > 0) {
     g.count = static_cast<uint32_t*>(a->scratch);
     g.part = reinterpret_cast<float*>(g.count + ATTEND_COUNTERS);
   }
-  const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, k.nt, (hipStream_t)stream);
+  const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return SI_OK;
 }

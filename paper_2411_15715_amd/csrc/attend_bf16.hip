@@ -3,13 +3,13 @@
 
 namespace si {
 
-hipError_t launch_attend_bf16(const AttendArgs& g, int nt, hipStream_t stream) {
+hipError_t launch_attend_bf16(const AttendArgs& g, hipStream_t stream) {
   switch (g.c.head_dim) {
-    case 64: return launch_rows<SI_KV_BF16, 64, 4>(g, nt, stream);
-    case 96: return launch_rows<SI_KV_BF16, 96, 4>(g, nt, stream);
-    case 128: return launch_rows<SI_KV_BF16, 128, 4>(g, nt, stream);
-    case 192: return launch_rows<SI_KV_BF16, 192, 2>(g, nt, stream);
-    default: return launch_rows<SI_KV_BF16, 256, 2>(g, nt, stream);
+    case 64: return launch<SI_KV_BF16, 64>(g, stream);
+    case 96: return launch<SI_KV_BF16, 96>(g, stream);
+    case 128: return launch<SI_KV_BF16, 128>(g, stream);
+    case 192: return launch<SI_KV_BF16, 192>(g, stream);
+    default: return launch<SI_KV_BF16, 256>(g, stream);
   }
 }
 

@@ -7,33 +7,40 @@
 // tokens whose weights it has to hold for the second product: nothing passes through LDS or between lanes but the maximum of a row.
 // Running maximum m and sum l (base 2) per row; the waves of a block and the blocks of a split sequence are joined by
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m)
-// by the block that finishes last, in the order of the splits, so that the result does not depend on who that is.
+// The splits are joined in their order, by the block that finishes last or by a second kernel, so that the result does not depend on who does it.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kv_layout.h"
 
 namespace si {
 
-constexpr int ATTEND_WAVES = 4;
-constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
-constexpr int ATTEND_COUNTERS = 16384;  // units (sequence, kv head, row group) of a launch that may be split
+constexpr int ATTEND_COUNTERS = 256;    // units (sequence, kv head, row group) whose last block may join them
+constexpr int ATTEND_FEW = 4;           // splits that the last block joins
 
 struct AttendArgs {
   si_cache_t c;
   si_attend_t a;
   int layer;
   int rows;      // rows of a unit in all: n_new * heads per kv head
-  int groups;    // row groups
+  int groups;    // row groups: blocks that share a kv head
+  int tiles;     // waves of a block that share a stream of cache blocks, each with 16 rows of its own: a power of two
   int splits;    // parts that a sequence of max_len is cut into
   int chunk;     // cache blocks of a part, at least
   float scale2;  // scale * log2(e)
-  float* part;   // [unit][split][16 NT rows][D + 2]: o, then m, l of each row
+  int part_rows; // rows of a unit that the scratch has room for: min(rows, 16 tiles)
+  int last_joins; // the block that finishes last joins the splits of a unit; else the join kernel does
+  float* part;   // [unit][split][part_rows][D + 2]: o, then m, l of each row
   uint32_t* count;
 };
 
-hipError_t launch_attend_bf16(const AttendArgs& g, int nt, hipStream_t stream);
-hipError_t launch_attend_e4m3(const AttendArgs& g, int nt, hipStream_t stream);
+constexpr int ATTEND_WAVES = 4;  // of a block
+constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
+
+hipError_t launch_attend_bf16(const AttendArgs& g, hipStream_t stream);
+hipError_t launch_attend_e4m3(const AttendArgs& g, hipStream_t stream);
 
 #if defined(__HIPCC__)
 namespace {
@@ -89,16 +96,76 @@ __device__ __forceinline__ float2 get2(const float* p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-template <int TYPE, int D, int NT> struct Attend {
+// What the rows [row0, row_end) of a sequence's new tokens see, in positions and in blocks of B, and how that is cut
+struct Span {
+  int seq, len, window, first;  // first: where the sight of token 0 ends
+  int lo, hi, lo_all, hi_all;   // seen by some of the rows: [lo, hi), by all of them [lo_all, hi_all)
+  int fb, nb, chunk, active;    // first block and number of them; blocks of a split, splits (at least 1)
+  int why;
+  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int row0, int row_end, int B) {
+    // (scalar loads: nothing in this launch writes the lists)
+    typedef const int32_t __attribute__((address_space(4))) constant_t;
+    const si_cache_t& c = g.c;
+    seq = g.a.seqs ? ((constant_t*)(uintptr_t)g.a.seqs)[seq_i] : seq_i;
+    len = 0;
+    why = SI_CACHE_BAD_SEQ;
+    if (seq >= 0 && seq < c.n_seqs) {
+      const int most = c.max_pages * c.page_tokens;
+      len = ((constant_t*)(uintptr_t)c.lens)[seq];
+      why = len < 0 || len > most ? SI_CACHE_BAD_LEN : 0;
+      len = len < 0 ? 0 : min(len, most);
+    }
+    const int per = g.a.n_heads / c.n_kv_heads, t0 = row0 / per, t1 = (row_end - 1) / per;
+    window = g.a.window < len ? g.a.window : 0;
+    first = len - g.a.n_new + 1;
+    hi = max(0, first + t1);
+    hi_all = max(0, first + t0);
+    lo = window ? max(0, first + t0 - window) : 0;
+    lo_all = window ? max(0, first + t1 - window) : 0;
+    fb = lo / B;
+    nb = hi > lo ? (hi + B - 1) / B - fb : 0;
+    chunk = max(g.chunk, (nb + g.splits - 1) / g.splits);
+    active = max(1, (nb + chunk - 1) / chunk);
+  }
+};
+
+// what has been summed over some positions, for 4 elements of a row
+struct Sum {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  __device__ __forceinline__ void add(const f32x4& o2, float m2, float l2) {
+    const float m_new = fmaxf(m, m2), base = finite_base(m_new), f = pow2(m - base), h = pow2(m2 - base);
+    m = m_new;
+    l = l * f + l2 * h;
+    o = o * f + o2 * h;
+  }
+};
+
+__device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, const Sum& s, float scale_v) {
+  const int per = g.a.n_heads / g.c.n_kv_heads, j = row / per, head = kv * per + row % per;
+  const int64_t r = (int64_t)seq_i * g.a.n_new + j;
+  const float inv = s.l == 0.f ? 0.f : scale_v / s.l;
+  *reinterpret_cast<u32x2_a2*>(static_cast<uint16_t*>(g.a.out) + r * g.a.out_stride + (int64_t)head * g.c.head_dim + dim) =
+      u32x2{bf16_pair(s.o[0] * inv, s.o[1] * inv), bf16_pair(s.o[2] * inv, s.o[3] * inv)};
+  if (dim == 0 && g.a.lse) g.a.lse[r * g.a.n_heads + head] = s.l == 0.f ? -INFINITY : (s.m + log2f(s.l)) * 0.69314718055994531f;
+}
+
+// SHARED: several waves of a block read the same cache blocks (tiles > 1); their loads are to stay in the caches until the last of them has
+// come, the others go past them (each is right where it is: 131071 positions, one tile, 86 us with the hint and 97 without; 40 rows, 16 x 8000
+// positions, 128 with it and 110 without)
+template <int TYPE, int D, bool SHARED> struct Attend {
   static constexpr int E = TYPE == SI_KV_E4M3 ? 16 : 8, B = 4 * E, J = E / 4;  // J score tiles of 16 tokens
   static constexpr int NL = D / 16;                                           // loads of 16 bytes of K, and of V, a lane and block
   static constexpr int H = E / 8;                                             // operands of 8 elements in 16 bytes
-  static constexpr int ROWS = 16 * NT, PAD = D + 4;                           // (rows of 16 banks more: the four groups of lanes write side by side)
-  static constexpr int PART = ROWS * (D + 2);
+  static constexpr int WAVES = ATTEND_WAVES, THREADS = ATTEND_THREADS;
+  static constexpr int PAD = D + 4;                                           // (rows of 16 banks more: the four groups of lanes write side by side)
+  // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
+  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256 a wave has a SIMD for itself.
+  static constexpr int WAVES_PER_SIMD = D < 256 ? 2 : 1;
 
   struct Lds {
-    float o[ATTEND_WAVES][16][PAD];
-    float m[ATTEND_WAVES][16], l[ATTEND_WAVES][16];
+    float o[WAVES][16][PAD];
+    float m[WAVES][16], l[WAVES][16];
     uint32_t arrived;
   };
 
@@ -127,251 +194,225 @@ template <int TYPE, int D, int NT> struct Attend {
       }
     return bad;
   }
-
-  static __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, const f32x4& o, float m, float l, float scale_v) {
-    const int per = g.a.n_heads / g.c.n_kv_heads, j = row / per, head = kv * per + row % per;
-    const int64_t r = (int64_t)seq_i * g.a.n_new + j;
-    const float inv = l == 0.f ? 0.f : scale_v / l;
-    *reinterpret_cast<u32x2_a2*>(static_cast<uint16_t*>(g.a.out) + r * g.a.out_stride + (int64_t)head * D + dim) =
-        u32x2{bf16_pair(o[0] * inv, o[1] * inv), bf16_pair(o[2] * inv, o[3] * inv)};
-    if (dim == 0 && g.a.lse) g.a.lse[r * g.a.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  static __device__ __forceinline__ u32x4 load16(const char* p) {
+    if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(p);
+    else return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
   }
+  static __device__ __forceinline__ bf16x8 part_of(const u32x4& v, int h) { return E == 8 ? operand(v) : operand8(v[2 * h], v[2 * h + 1]); }
 
   static __device__ void run(const AttendArgs& g, Lds& s) {
     const si_cache_t& c = g.c;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), grp = lane / 16, col = lane % 16;
-    const int split = blockIdx.x, kv = blockIdx.y / g.groups, row0 = blockIdx.y % g.groups * ROWS, seq_i = blockIdx.z;
+    const int split = blockIdx.z, kv = blockIdx.x / g.groups, seq_i = blockIdx.y;
     const int per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
-    const int row_end = min(g.rows, row0 + ROWS);
-    const bool reports = blockIdx.y == 0 && threadIdx.x == 0;
+    // the block has the rows [block_row0, row_end), this wave 16 of them from row0 on; `streams` waves take the cache blocks in turn
+    const int tiles = SHARED ? g.tiles : 1, streams = WAVES / tiles, stream = wave / tiles;
+    const int block_row0 = blockIdx.x % g.groups * (16 * tiles), row0 = block_row0 + wave % tiles * 16, row_end = min(g.rows, block_row0 + 16 * tiles);
+    const Span sp(g, seq_i, block_row0, row_end, B);
+    if (sp.why && split == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(c.status, sp.why);
+    if (split >= sp.active) return;
+    const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all, active = sp.active;
+    const int b0 = sp.fb + split * sp.chunk, b1 = min(b0 + sp.chunk, sp.fb + sp.nb);
 
-    // what the rows of this group see: [lo, hi), every one of them [lo_all, hi_all)
-    const int seq = g.a.seqs ? g.a.seqs[seq_i] : seq_i;
-    int len = 0;
-    if (seq >= 0 && seq < c.n_seqs) {
-      len = c.lens[seq];
-      const int most = c.max_pages * c.page_tokens;
-      if (len < 0 || len > most) {
-        if (reports && split == 0) atomicOr(c.status, SI_CACHE_BAD_LEN);
-        len = len < 0 ? 0 : most;
-      }
-    } else if (reports && split == 0) {
-      atomicOr(c.status, SI_CACHE_BAD_SEQ);
-    }
-    const int window = g.a.window < len ? g.a.window : 0;
-    const int first = len - n_new + 1;  // where the sight of token 0 ends
-    const int hi = max(0, first + (row_end - 1) / per), hi_all = max(0, first + row0 / per);
-    const int lo = window ? max(0, first + row0 / per - window) : 0, lo_all = window ? max(0, first + (row_end - 1) / per - window) : 0;
-    const int fb = lo / B, nb = hi > lo ? (hi + B - 1) / B - fb : 0;
-    const int chunk = max(g.chunk, (nb + g.splits - 1) / g.splits), active = max(1, (nb + chunk - 1) / chunk);
-    if (split >= active) return;
-    const int b0 = fb + split * chunk, b1 = min(b0 + chunk, fb + nb);
-
-    const int32_t* table = c.table + (int64_t)max(seq, 0) * c.max_pages;  // (read where nb > 0 only)
-    const int64_t page_bytes = kv_page_elems(c) * (TYPE == SI_KV_E4M3 ? 1 : 2), block_bytes = 64 * D;
-    const char* k_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 0, kv) * (TYPE == SI_KV_E4M3 ? 1 : 2);
-    const char* v_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 1, kv) * (TYPE == SI_KV_E4M3 ? 1 : 2);
-    const int blocks_per_page = c.page_tokens / B;
-    const int k_lane = grp * (B * 16) + col * 16, v_lane = grp * (D * 16) + col * 16;
-
-    u32x4 q[NT][D / 32];
-    int q_lo[NT], q_hi[NT], q_tok[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int row = row0 + 16 * t + col, j = row / per;
-      const bool in = row < row_end;
-      q_tok[t] = in ? j : -1;
-      q_hi[t] = in ? max(0, first + j) : 0;
-      q_lo[t] = in && window ? max(0, first + j - window) : 0;
-      const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + ((int64_t)seq_i * n_new + j) * g.a.q_stride + (int64_t)(kv * per + row % per) * D;
+    // this lane's row of q, as the right operand; token of the row, or -1
+    const int row = row0 + col, tok = row < row_end ? row / per : -1;
+    u32x4 q[D / 32];
+    {
+      const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + ((int64_t)seq_i * n_new + row / per) * g.a.q_stride + (int64_t)(kv * per + row % per) * D;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         // operand x of K covers, in this lane, elements 32 x + 8 grp of a head (bf16), or half x % 2 of the 16 from 64 (x / 2) + 16 grp on
         const int dim = E == 8 ? 32 * x + 8 * grp : 64 * (x / 2) + 16 * grp + 8 * (x % 2);
-        q[t][x] = in ? u32x4(*reinterpret_cast<const u32x4_a2*>(p + dim)) : u32x4{0, 0, 0, 0};
+        q[x] = tok >= 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(p + dim)) : u32x4{0, 0, 0, 0};
       }
     }
     const float sc = g.scale2 * (TYPE == SI_KV_E4M3 && c.scale_k ? c.scale_k[kv] : 1.f);
     const float scale_v = TYPE == SI_KV_E4M3 && c.scale_v ? c.scale_v[kv] : 1.f;
 
-    f32x4 o[NT][NL];
-    float m[NT], l[NT];
+    f32x4 o[NL];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int i = 0; i < NL; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // page numbers of the wave's next 64 blocks, one a lane
-    int pages = 0;
-    auto page_of = [&](int turn) {
-      if (turn % 64 == 0) {
-        const int b = b0 + wave + ATTEND_WAVES * (turn + lane);
-        pages = b < b1 ? table[b / blocks_per_page] : 0;
-      }
-      const int p = __builtin_amdgcn_readlane(pages, turn % 64);
-      return p >= 0 && p < c.n_pages ? p : -1;
+    // Where a block of the stream lies: entry of the table and place in the page.  The page's number comes by a scalar load, which the loads of K
+    // and V in flight have nothing to do with (a vector load in their midst is waited for along with all of them); nothing in this
+    // launch writes the table.
+    const int32_t* table = c.table + (int64_t)max(sp.seq, 0) * c.max_pages;  // (read where nb > 0 only)
+    const int per_page = c.page_tokens / B, last_entry = (b1 - 1) / per_page;
+    struct Place { int entry, at; };
+    auto page_of = [&](const Place& w) {
+      typedef const int32_t __attribute__((address_space(4))) constant_t;
+      const int page = ((constant_t*)(uintptr_t)table)[min(w.entry, last_entry)];
+      return page >= 0 && page < c.n_pages ? page : -1;
     };
+    auto step = [&](Place w) {
+      w.at += streams;
+      while (w.at >= per_page) { w.at -= per_page; ++w.entry; }
+      return w;
+    };
+    constexpr int BYTES = TYPE == SI_KV_E4M3 ? 1 : 2;
+    const int64_t page_bytes = kv_page_elems(c) * BYTES;
+    const char* k_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 0, kv) * BYTES;
+    const char* v_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 1, kv) * BYTES;
+    const int k_lane = grp * (B * 16) + col * 16, v_lane = grp * (D * 16) + col * 16;
     u32x4 kf[NL], vf[NL];
-    auto load_k = [&](int page, int b) {
-      const char* p = k_base + max(page, 0) * page_bytes + (b % blocks_per_page) * block_bytes;
+    auto load_k = [&](int page, int at) {
+      const char* p = k_base + (uint32_t)max(page, 0) * page_bytes + at * (64 * D);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) kf[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + k_lane + (i / J) * (4 * B * 16) + (i % J) * 256));
+      for (int i = 0; i < NL; ++i) kf[i] = load16(p + k_lane + i / J * (4 * B * 16) + i % J * 256);
     };
-    auto load_v = [&](int page, int b) {
-      const char* p = v_base + max(page, 0) * page_bytes + (b % blocks_per_page) * block_bytes;
+    auto load_v = [&](int page, int at) {
+      const char* p = v_base + (uint32_t)max(page, 0) * page_bytes + at * (64 * D);
 #pragma unroll
-      for (int i = 0; i < NL; ++i) vf[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + v_lane + i * 256));
+      for (int i = 0; i < NL; ++i) vf[i] = load16(p + v_lane + i * 256);
     };
 
-    int turn = 0, b = b0 + wave, page = 0;
-    if (b < b1) {
-      page = page_of(0);
-      load_k(page, b);
-      load_v(page, b);
-    }
-    bool bad_page = false;
-    for (; b < b1; b += ATTEND_WAVES) {
-      // scores of the block: tile j, element i of this lane is token grp * E + 4 j + i
-      f32x4 x[NT][J];
+    // scores of a block: tile j, element i of this lane is token grp * E + 4 j + i
+    f32x4 x[J];
+    auto scores = [&] {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int j = 0; j < J; ++j) x[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < J; ++j) x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < NL; ++i)
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          const bf16x8 kk = E == 8 ? operand(kf[i]) : operand8(kf[i][2 * h], kf[i][2 * h + 1]);
+        for (int h = 0; h < H; ++h) x[i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(kf[i], h), operand(q[i / J * H + h]), x[i % J], 0, 0, 0);
+    };
+    // weights of the block, and what has been summed brought to its maximum; EDGE: some rows may not see some of its tokens.
+    // The weights are rounded to bf16, as operands are (2^-8 of each, the sum l takes them as they were: the error of out is that of a
+    // mean of roundings, below its own rounding)
+    u32x4 p[H];
+    auto weights = [&](auto EDGE, int t0) {
+      float top = -INFINITY;
+      const int see_hi = tok >= 0 ? max(0, first + tok) : 0, see_lo = window ? max(0, first + tok - window) : 0;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) x[t][i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(q[t][(i / J) * H + h]), x[t][i % J], 0, 0, 0);
-        }
-      const int b_next = b + ATTEND_WAVES;
-      int page_next = 0;
-      if (b_next < b1) {
-        page_next = page_of(++turn);
-        load_k(page_next, b_next);
-      }
-      const int t0 = b * B;
-      const bool seen = page >= 0;
-      bad_page |= !seen;
-      const bool edge = !seen || t0 < lo_all || t0 + B > hi_all;  // (not all rows see all tokens)
-      u32x4 p[NT][H];
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v = x[t][j][i] * sc;
-            if (edge) {
-              const int pos = t0 + grp * E + 4 * j + i;
-              v = seen && pos >= q_lo[t] && pos < q_hi[t] ? v : -INFINITY;
-            }
-            x[t][j][i] = v;
-            top = fmaxf(top, v);
+        for (int i = 0; i < 4; ++i) {
+          float v = x[j][i] * sc;
+          if constexpr (EDGE) {
+            const int pos = t0 + grp * E + 4 * j + i;
+            v = pos >= see_lo && pos < see_hi ? v : -INFINITY;
           }
-        const float m_new = fmaxf(m[t], max_of_row(top)), base = finite_base(m_new);
-        if (__any(m_new > m[t])) {
-          const float f = pow2(m[t] - base);
-          l[t] *= f;
-#pragma unroll
-          for (int i = 0; i < NL; ++i) o[t][i] *= f;
-          m[t] = m_new;
+          x[j][i] = v;
+          top = fmaxf(top, v);
         }
+      const float m_new = fmaxf(m, max_of_row(top)), base = finite_base(m_new);
+      if (__any(m_new > m)) {
+        const float f = pow2(m - base);
+        l *= f;
 #pragma unroll
-        for (int h = 0; h < H; ++h)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int j = 2 * h + w / 2, i = 2 * (w % 2);
-            const float a = pow2(x[t][j][i] - base), e = pow2(x[t][j][i + 1] - base);
-            l[t] += a + e;
-            p[t][h][w] = bf16_pair(a, e);
-          }
+        for (int i = 0; i < NL; ++i) o[i] *= f;
+        m = m_new;
       }
-      bool apart = false;
-      if (edge) {
-        // what no row sees may be anything: weight 0 times infinity would be NaN
-        const u32x4 keep = seen ? token_mask(t0 + grp * E, lo, hi) : u32x4{0, 0, 0, 0};
-        bool bad = false;
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int j = 2 * h + w / 2, i = 2 * (w % 2);
+          const float a = pow2(x[j][i] - base), e = pow2(x[j][i + 1] - base);
+          l += a + e;
+          p[h][w] = bf16_pair(a, e);
+        }
+    };
+    auto products = [&] {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int h = 0; h < H; ++h) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(vf[i], h), operand(p[h]), o[i], 0, 0, 0);
+    };
+    // the same where some rows may not see some tokens.  What no row sees may be anything (weight 0 times infinity would be NaN); what
+    // some of the tokens see and is not finite takes a product for each of them
+    auto products_at_edge = [&](int t0) {
+      const u32x4 keep = token_mask(t0 + grp * E, lo, hi);
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        vf[i] &= keep;
+        bad |= not_finite(vf[i]);
+      }
+      if (n_new == 1 || !__any(bad)) {
+        products();
+        return;
+      }
+      for (int j = row0 / per; j <= (min(row_end, row0 + 16) - 1) / per; ++j) {
+        const u32x4 mine = token_mask(t0 + grp * E, window ? max(0, first + j - window) : 0, max(0, first + j));
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          vf[i] &= keep;
-          bad |= not_finite(vf[i]);
-        }
-        apart = n_new > 1 && __any(bad);
-      }
-      if (!apart) {
+          const u32x4 v = vf[i] & mine;
+          f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < NL; ++i)
-#pragma unroll
-          for (int h = 0; h < H; ++h) {
-            const bf16x8 vv = E == 8 ? operand(vf[i]) : operand8(vf[i][2 * h], vf[i][2 * h + 1]);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) o[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, operand(p[t][h]), o[t][i], 0, 0, 0);
-          }
-      } else {
-        // a value that is not finite, seen by some of the tokens: one product for each of them
-        for (int j = row0 / per; j <= (row_end - 1) / per; ++j) {
-          const u32x4 keep = token_mask(t0 + grp * E, window ? max(0, first + j - window) : 0, max(0, first + j));
-#pragma unroll
-          for (int i = 0; i < NL; ++i) {
-            const u32x4 v = vf[i] & keep;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              f32x4 r = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(E == 8 ? operand(v) : operand8(v[2 * h], v[2 * h + 1]), operand(p[t][h]), r, 0, 0, 0);
-              if (q_tok[t] == j) o[t][i] += r;
-            }
-          }
+          for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[h]), r, 0, 0, 0);
+          if (tok == j) o[i] += r;
         }
       }
-      if (b_next < b1) load_v(page_next, b_next);
-      page = page_next;
-    }
-    if (bad_page && lane == 0) atomicOr(c.status, SI_CACHE_BAD_PAGE);
+    };
 
-    // the waves of the block, 16 rows at a time
-    const int unit = seq_i * gridDim.y + blockIdx.y;
-    float* part = g.part + ((int64_t)unit * g.splits + split) * PART;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if (t > 0) __syncthreads();
-      const float sum = sum_of_row(l[t]);
-      if (grp == 0) { s.m[wave][col] = m[t]; s.l[wave][col] = sum; }
-#pragma unroll
-      for (int i = 0; i < NL; ++i) *reinterpret_cast<f32x4*>(&s.o[wave][col][16 * i + 4 * grp]) = o[t][i];
-      __syncthreads();
-      for (int i = threadIdx.x; i < 16 * D / 4; i += ATTEND_THREADS) {
-        const int r = i / (D / 4), dim = i % (D / 4) * 4;
-        if (row0 + 16 * t + r >= row_end) continue;
-        float mm = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < ATTEND_WAVES; ++w) mm = fmaxf(mm, s.m[w][r]);
-        const float base = finite_base(mm);
-        float ll = 0.f;
-        f32x4 oo = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < ATTEND_WAVES; ++w) {
-          const float f = pow2(s.m[w][r] - base);
-          ll += s.l[w][r] * f;
-          oo += *reinterpret_cast<const f32x4*>(&s.o[w][r][dim]) * f;
+    // K of the next block is asked for when the scores of this one are formed, V when it has been multiplied: 8 to 16 KB of a wave are
+    // always on their way (heads of 128).  The last block has no next: written out, so that the loop's loads stand under no condition.
+    int b = b0 + stream;
+    if (b < b1 && row0 < row_end) {
+      bool bad_page = false;
+      const Place here{b / per_page, b % per_page};
+      Place next = step(here);
+      int page = page_of(here), next_page = page_of(next);
+      load_k(page, here.at);
+      load_v(page, here.at);
+      for (; b + streams < b1; b += streams) {
+        const int t0 = b * B;
+        const Place after = step(next);
+        const int after_page = page_of(after);
+        scores();
+        load_k(next_page, next.at);
+        if (page >= 0) {  // (a block whose page is not there is passed over)
+          if (t0 < lo_all || t0 + B > hi_all) {
+            weights(std::true_type{}, t0);
+            products_at_edge(t0);
+          } else {
+            weights(std::false_type{}, t0);
+            products();
+          }
         }
-        if (active == 1) {
-          write_row(g, seq_i, kv, row0 + 16 * t + r, dim, oo, mm, ll, scale_v);
-        } else {
-          float* to = part + (16 * t + r) * (D + 2);
-          put2(to + dim, oo[0], oo[1]);
-          put2(to + dim + 2, oo[2], oo[3]);
-          if (dim == 0) put2(to + D, mm, ll);
-        }
+        load_v(next_page, next.at);
+        bad_page |= page < 0;
+        page = next_page;
+        next_page = after_page;
+        next = after;
+      }
+      bad_page |= page < 0;
+      if (page >= 0) {
+        scores();
+        weights(std::true_type{}, b * B);
+        products_at_edge(b * B);
+      }
+      if (bad_page && lane == 0) atomicOr(c.status, SI_CACHE_BAD_PAGE);
+    }
+
+    // the streams of the block
+    l = sum_of_row(l);
+    if (grp == 0) { s.m[wave][col] = m; s.l[wave][col] = l; }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) *reinterpret_cast<f32x4*>(&s.o[wave][col][16 * i + 4 * grp]) = o[i];
+    __syncthreads();
+    const int unit = seq_i * gridDim.x + blockIdx.x, part_floats = g.part_rows * (D + 2), items = (row_end - block_row0) * (D / 4);
+    float* part = g.part + ((int64_t)unit * g.splits + split) * part_floats;
+    for (int i = threadIdx.x; i < items; i += THREADS) {
+      const int r = i / (D / 4), dim = i % (D / 4) * 4;
+      Sum sum;
+      for (int w = r / 16; w < WAVES; w += tiles) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % 16][dim]), s.m[w][r % 16], s.l[w][r % 16]);
+      float* to = part + r * (D + 2);
+      if (active == 1) {
+        write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
+      } else if (g.last_joins) {
+        put2(to + dim, sum.o[0], sum.o[1]);
+        put2(to + dim + 2, sum.o[2], sum.o[3]);
+        if (dim == 0) put2(to + D, sum.m, sum.l);
+      } else {
+        *reinterpret_cast<float2*>(to + dim) = make_float2(sum.o[0], sum.o[1]);
+        *reinterpret_cast<float2*>(to + dim + 2) = make_float2(sum.o[2], sum.o[3]);
+        if (dim == 0) *reinterpret_cast<float2*>(to + D) = make_float2(sum.m, sum.l);
       }
     }
-    if (active == 1) return;
+    if (active == 1 || !g.last_joins) return;
 
     // the splits of the unit: the last block to arrive joins them.  Its own stores have reached memory before it is counted
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -381,51 +422,80 @@ template <int TYPE, int D, int NT> struct Attend {
     if (s.arrived != (uint32_t)active - 1) return;
     asm volatile("" ::: "memory");
     if (threadIdx.x == 0) __hip_atomic_store(g.count + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float* parts = g.part + (int64_t)unit * g.splits * PART;
-    for (int i = threadIdx.x; i < (row_end - row0) * (D / 4); i += ATTEND_THREADS) {
+    const float* parts = g.part + (int64_t)unit * g.splits * part_floats;
+    for (int i = threadIdx.x; i < items; i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
-      float mm = -INFINITY, ll = 0.f;
-      f32x4 oo = {0.f, 0.f, 0.f, 0.f};
-      constexpr int AHEAD = 8;
-      for (int s0 = 0; s0 < active; s0 += AHEAD) {
-        float2 ml[AHEAD], v[AHEAD][2];
+      Sum sum;
+      float2 ml[ATTEND_FEW], v[ATTEND_FEW][2];  // (active <= splits <= ATTEND_FEW)
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const float* from = parts + (int64_t)min(s0 + k, active - 1) * PART + r * (D + 2);
-          ml[k] = get2(from + D);
-          v[k][0] = get2(from + dim);
-          v[k][1] = get2(from + dim + 2);
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          if (s0 + k >= active) break;
-          const float m_new = fmaxf(mm, ml[k].x), base = finite_base(m_new), f = pow2(mm - base), h = pow2(ml[k].x - base);
-          mm = m_new;
-          ll = ll * f + ml[k].y * h;
-          oo = oo * f + f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y} * h;
-        }
+      for (int k = 0; k < ATTEND_FEW; ++k) {
+        const float* from = parts + (int64_t)min(k, active - 1) * part_floats + r * (D + 2);
+        ml[k] = get2(from + D);
+        v[k][0] = get2(from + dim);
+        v[k][1] = get2(from + dim + 2);
       }
-      write_row(g, seq_i, kv, row0 + r, dim, oo, mm, ll, scale_v);
+#pragma unroll
+      for (int k = 0; k < ATTEND_FEW; ++k)
+        if (k < active) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, ml[k].x, ml[k].y);
+      write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
     }
   }
 };
 
-template <int TYPE, int D, int NT> __global__ __launch_bounds__(ATTEND_THREADS) void k_attend(AttendArgs g) {
-  __shared__ typename Attend<TYPE, D, NT>::Lds s;
-  Attend<TYPE, D, NT>::run(g, s);
+template <int TYPE, int D, bool SHARED> __global__ __launch_bounds__((Attend<TYPE, D, SHARED>::THREADS), (Attend<TYPE, D, SHARED>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
+  __shared__ typename Attend<TYPE, D, SHARED>::Lds s;
+  Attend<TYPE, D, SHARED>::run(g, s);
 }
 
-template <int TYPE, int D, int NT> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
-  hipLaunchKernelGGL((k_attend<TYPE, D, NT>), dim3(g.splits, g.c.n_kv_heads * g.groups, g.a.n), dim3(ATTEND_THREADS), 0, stream, g);
-  return hipGetLastError();
-}
-template <int TYPE, int D, int MOST> hipError_t launch_rows(const AttendArgs& g, int nt, hipStream_t stream) {
-  if (nt == 1) return launch<TYPE, D, 1>(g, stream);
-  if constexpr (MOST >= 4) {
-    if (nt == 3) return launch<TYPE, D, 3>(g, stream);
-    if (nt == 4) return launch<TYPE, D, 4>(g, stream);
+// Joins the splits of a unit: a block has one row, and its threads a share of the splits of 4 elements each.
+template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g, int B) {
+  constexpr int LANES = D / 4, SHARES = 256 / LANES;
+  __shared__ f32x4 s_o[SHARES][LANES];
+  __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
+  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, block_row0 = blockIdx.x % g.groups * (16 * g.tiles), r = blockIdx.z;
+  const int row_end = min(g.rows, block_row0 + 16 * g.tiles);
+  if (block_row0 + r >= row_end) return;
+  const Span sp(g, seq_i, block_row0, row_end, B);
+  if (sp.active == 1) return;  // (written already)
+  const int lane = threadIdx.x % LANES, share = threadIdx.x / LANES, part_floats = g.part_rows * (D + 2);
+  const float* from = g.part + (int64_t)(seq_i * gridDim.x + blockIdx.x) * g.splits * part_floats + r * (D + 2);
+  Sum sum;
+  if (share < SHARES) {
+    constexpr int AHEAD = 4;
+    for (int s0 = share; s0 < sp.active; s0 += AHEAD * SHARES) {
+      float2 v[AHEAD][3];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float* p = from + (int64_t)min(s0 + k * SHARES, sp.active - 1) * part_floats;
+        v[k][0] = *reinterpret_cast<const float2*>(p + 4 * lane);
+        v[k][1] = *reinterpret_cast<const float2*>(p + 4 * lane + 2);
+        v[k][2] = *reinterpret_cast<const float2*>(p + D);
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (s0 + k * SHARES < sp.active) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
+    }
+    s_o[share][lane] = sum.o; s_m[share][lane] = sum.m; s_l[share][lane] = sum.l;
   }
-  return launch<TYPE, D, 2>(g, stream);
+  __syncthreads();
+  if (share > 0) return;
+  for (int k = 1; k < min(SHARES, sp.active); ++k) sum.add(s_o[k][lane], s_m[k][lane], s_l[k][lane]);
+  write_row(g, seq_i, kv, block_row0 + r, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+}
+
+template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
+  // Blocks go to the dies in turn: heads first, so that a long sequence is spread over all of them (with the splits first, and 8 of them, the die that
+  // gets the last split of every sequence has nothing to do where most are short: 64 sequences of 1 .. 8000 positions 232 us, not 162), then
+  // sequences, then splits: the short ones end last.
+  const dim3 grid(g.c.n_kv_heads * g.groups, g.a.n, g.splits);
+  if (g.tiles > 1) hipLaunchKernelGGL((k_attend<TYPE, D, true>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else hipLaunchKernelGGL((k_attend<TYPE, D, false>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  if (g.splits > 1 && !g.last_joins) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_join<D>, dim3(grid.x, grid.y, g.part_rows), dim3(256), 0, stream, g, Attend<TYPE, D, true>::B);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace

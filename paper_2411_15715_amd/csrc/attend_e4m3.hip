@@ -3,12 +3,12 @@
 
 namespace si {
 
-hipError_t launch_attend_e4m3(const AttendArgs& g, int nt, hipStream_t stream) {
+hipError_t launch_attend_e4m3(const AttendArgs& g, hipStream_t stream) {
   switch (g.c.head_dim) {
-    case 64: return launch_rows<SI_KV_E4M3, 64, 4>(g, nt, stream);
-    case 128: return launch_rows<SI_KV_E4M3, 128, 4>(g, nt, stream);
-    case 192: return launch_rows<SI_KV_E4M3, 192, 2>(g, nt, stream);
-    default: return launch_rows<SI_KV_E4M3, 256, 2>(g, nt, stream);
+    case 64: return launch<SI_KV_E4M3, 64>(g, stream);
+    case 128: return launch<SI_KV_E4M3, 128>(g, stream);
+    case 192: return launch<SI_KV_E4M3, 192>(g, stream);
+    default: return launch<SI_KV_E4M3, 256>(g, stream);
   }
 }
 
