@@ -5,7 +5,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 namespace si {
 namespace {
@@ -27,14 +26,14 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   k.splits = 1;
   k.chunk = (int)std::max<int64_t>(1, blocks);
   k.part_rows = std::min(rows, 16 * k.tiles);
-  const int least = (getenv("ATT_MIN") ? atoi(getenv("ATT_MIN")) : 2) * (waves / k.tiles);
+  // about as many blocks as there are compute units, none with fewer than 2 cache blocks a wave: each more is a row's sums to write and read again
+  const int least = 2 * (waves / k.tiles);
   if (blocks > least) {
-    const int64_t want = std::max<int64_t>(1, (getenv("ATT_TARGET") ? atoi(getenv("ATT_TARGET")) : 256) / std::max<int64_t>(1, units));
+    const int64_t want = std::max<int64_t>(1, 256 / std::max<int64_t>(1, units));
     k.chunk = (int)std::max<int64_t>((blocks + want - 1) / want, least);
     k.splits = (int)((blocks + k.chunk - 1) / k.chunk);
   }
   k.last_joins = k.splits <= ATTEND_FEW && units <= ATTEND_COUNTERS;
-  if (getenv("ATT_JOIN")) k.last_joins = 0;
   if (k.splits > 1) k.scratch = (int64_t)ATTEND_COUNTERS * 4 + units * k.splits * k.part_rows * (c.head_dim + 2) * 4;
   return k;
 }
