@@ -10,31 +10,34 @@ namespace si {
 namespace {
 
 struct Cut {
-  int tiles, groups, splits, chunk, part_rows, last_joins;
-  int64_t scratch;
+  int tiles, groups, slices, part_rows, last_joins;
+  int64_t scratch, parted_at, part_at;
 };
 
-// Waves of a block that share cache blocks, row groups, and the parts that a sequence of max_len is cut into.
+// Waves of a block that share cache blocks, row groups, and the slices that a kv head's cache blocks are cut into.
 Cut cut(const si_cache_t& c, const si_attend_t& a) {
   Cut k{};
-  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, B = kv_block(c.type), waves = ATTEND_WAVES;
-  for (k.tiles = 1; k.tiles < tiles && k.tiles < waves;) k.tiles *= 2;
+  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, B = kv_block(c.type);
+  for (k.tiles = 1; k.tiles < tiles && k.tiles < ATTEND_WAVES;) k.tiles *= 2;
   k.groups = (tiles + k.tiles - 1) / k.tiles;
+  k.part_rows = std::min(rows, 16 * k.tiles);
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
-  const int64_t blocks = (seen + B - 1) / B, units = (int64_t)a.n * c.n_kv_heads * k.groups;
-  k.splits = 1;
-  k.chunk = (int)std::max<int64_t>(1, blocks);
-  k.part_rows = std::min(rows, 16 * k.tiles);
-  // about as many blocks as there are compute units, none with fewer than 2 cache blocks a wave: each more is a row's sums to write and read again
-  const int least = 2 * (waves / k.tiles);
-  if (blocks > least) {
-    const int64_t want = std::max<int64_t>(1, 256 / std::max<int64_t>(1, units));
-    k.chunk = (int)std::max<int64_t>((blocks + want - 1) / want, least);
-    k.splits = (int)((blocks + k.chunk - 1) / k.chunk);
+  const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B), units = (int64_t)c.n_kv_heads * k.groups;
+  // As many blocks as there are compute units, twice that where a slice holds several sequences (the next one's first loads have nothing beside
+  // them: 512 sequences of 64 positions 67 -> 38 us) and the waves of a block do not share their loads (40 rows: 114 -> 156 us).  Joining
+  // costs as much as five cache blocks a wave (517 positions, 17 blocks over 4 waves, 9.4 us whole, 10.4 in two); beyond, none has
+  // fewer than two a wave.
+  const int most = a.n * units > 256 && k.tiles < 4 ? 512 : 256, streams = ATTEND_WAVES / k.tiles;
+  const int64_t least = each <= 5 * streams ? each : 2 * streams;
+  k.slices = (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + least - 1) / least));
+  const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
+  k.last_joins = k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
+  if (k.slices > 1) {
+    k.parted_at = ATTEND_COUNTERS * 4;
+    k.part_at = k.parted_at + (a.n * units * 8 + 15) / 16 * 16;
+    k.scratch = k.part_at + units * k.slices * 2 * k.part_rows * (c.head_dim + 2) * 4;
   }
-  k.last_joins = k.splits <= ATTEND_FEW && units <= ATTEND_COUNTERS;
-  if (k.splits > 1) k.scratch = (int64_t)ATTEND_COUNTERS * 4 + units * k.splits * k.part_rows * (c.head_dim + 2) * 4;
   return k;
 }
 
@@ -50,8 +53,8 @@ int check_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
   if (a->window < 0 || a->max_len < 0) return set_error(SI_EINVAL, "%s: window %d or max_len %d is negative", who, a->window, a->max_len);
   if (!std::isfinite(a->scale)) return set_error(SI_EINVAL, "%s: scale is not finite", who);
   const Cut k = cut(*c, *a);
-  // (a launch has fewer than 2^32 threads and fewer than 2^16 blocks along its second index)
-  if ((int64_t)c->n_kv_heads * k.groups > 65535 || (int64_t)c->n_kv_heads * k.groups * a->n * k.splits >= ((int64_t)1 << 24))
+  // (a launch has fewer than 2^32 threads: of the joining kernel, a block for each row)
+  if ((int64_t)c->n_kv_heads * k.groups * std::max<int64_t>(k.slices, (int64_t)a->n * k.part_rows) >= ((int64_t)1 << 24))
     return set_error(SI_EINVAL, "%s: n * n_new * n_heads is too large for one call (%d, %d, %d)", who, a->n, a->n_new, a->n_heads);
   return SI_OK;
 }
@@ -79,11 +82,13 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
   if (a->n == 0) return SI_OK;
-  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.splits, k.chunk, 0.f, k.part_rows, k.last_joins, nullptr, nullptr};
+  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.slices, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
   g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
   if (k.scratch > 0) {
-    g.count = static_cast<uint32_t*>(a->scratch);
-    g.part = reinterpret_cast<float*>(g.count + ATTEND_COUNTERS);
+    char* p = static_cast<char*>(a->scratch);
+    g.count = reinterpret_cast<uint32_t*>(p);
+    g.parted = reinterpret_cast<int2*>(p + k.parted_at);
+    g.part = reinterpret_cast<float*>(p + k.part_at);
   }
   const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "attention launch failed: %s", hipGetErrorString(e));

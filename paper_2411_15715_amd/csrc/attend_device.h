@@ -5,9 +5,14 @@
 // operand order of these instructions, so a wave loads both from memory into the registers that multiply, 16 bytes a lane and
 // 1 KB in a run; and the tokens of a K block are placed so that the scores a lane receives are those of the
 // tokens whose weights it has to hold for the second product: nothing passes through LDS or between lanes but the maximum of a row.
-// Running maximum m and sum l (base 2) per row; the waves of a block and the blocks of a split sequence are joined by
+// Running maximum m and sum l (base 2) per row; the waves of a block and the parts of a sequence are joined by
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m)
-// The splits are joined in their order, by the block that finishes last or by a second kernel, so that the result does not depend on who does it.
+// in the order of the parts, so that the result does not depend on who does it.
+//
+// Who does what: the cache blocks of all sequences, one after the other, are cut into G equal slices, and each block of a kv head takes one:
+// the end of a sequence, some whole ones, the beginning of another, or a piece from the middle of a long one.  Every compute unit has the
+// same to read, however the lengths are spread, and a block leaves at most two unfinished sums.  (A block for each sequence, or for each
+// equal part of the longest: 64 sequences of 1 .. 8000 positions 192 and 178 us, 156 where all have 4000.)
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -17,27 +22,25 @@
 
 namespace si {
 
-constexpr int ATTEND_COUNTERS = 256;    // units (sequence, kv head, row group) whose last block may join them
-constexpr int ATTEND_FEW = 4;           // splits that the last block joins
+constexpr int ATTEND_WAVES = 4;         // of a block
+constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
+constexpr int ATTEND_COUNTERS = 16384;  // sequences times units (kv head, row group) whose parts the last block may join
 
 struct AttendArgs {
   si_cache_t c;
   si_attend_t a;
   int layer;
-  int rows;      // rows of a unit in all: n_new * heads per kv head
-  int groups;    // row groups: blocks that share a kv head
-  int tiles;     // waves of a block that share a stream of cache blocks, each with 16 rows of its own: a power of two
-  int splits;    // parts that a sequence of max_len is cut into
-  int chunk;     // cache blocks of a part, at least
-  float scale2;  // scale * log2(e)
-  int part_rows; // rows of a unit that the scratch has room for: min(rows, 16 tiles)
-  int last_joins; // the block that finishes last joins the splits of a unit; else the join kernel does
-  float* part;   // [unit][split][part_rows][D + 2]: o, then m, l of each row
-  uint32_t* count;
+  int rows;       // rows of a unit in all: n_new * heads per kv head
+  int groups;     // row groups: blocks that share a kv head
+  int tiles;      // waves of a block that share a stream of cache blocks, each with 16 rows of its own: a power of two
+  int slices;     // G
+  int part_rows;  // rows of a unit that the scratch has room for: min(rows, 16 tiles)
+  int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
+  float scale2;   // scale * log2(e)
+  uint32_t* count;  // [ATTEND_COUNTERS], of (sequence, unit); 0 between calls
+  int2* parted;     // [n][unit] first slice of a sequence and number of them
+  float* part;      // [unit][slice][2][part_rows][D + 2]: o, then m, l of each row; first the sum of a sequence that began before the slice
 };
-
-constexpr int ATTEND_WAVES = 4;  // of a block
-constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
 
 hipError_t launch_attend_bf16(const AttendArgs& g, hipStream_t stream);
 hipError_t launch_attend_e4m3(const AttendArgs& g, hipStream_t stream);
@@ -96,13 +99,13 @@ __device__ __forceinline__ float2 get2(const float* p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-// What the rows [row0, row_end) of a sequence's new tokens see, in positions and in blocks of B, and how that is cut
+// What the new tokens t0 .. t1 of a sequence see, in positions and in blocks of B
 struct Span {
   int seq, len, window, first;  // first: where the sight of token 0 ends
-  int lo, hi, lo_all, hi_all;   // seen by some of the rows: [lo, hi), by all of them [lo_all, hi_all)
-  int fb, nb, chunk, active;    // first block and number of them; blocks of a split, splits (at least 1)
+  int lo, hi, lo_all, hi_all;   // seen by some of them: [lo, hi), by all of them [lo_all, hi_all)
+  int fb, nb;                   // first block and number of them
   int why;
-  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int row0, int row_end, int B) {
+  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B) {
     // (scalar loads: nothing in this launch writes the lists)
     typedef const int32_t __attribute__((address_space(4))) constant_t;
     const si_cache_t& c = g.c;
@@ -115,7 +118,6 @@ struct Span {
       why = len < 0 || len > most ? SI_CACHE_BAD_LEN : 0;
       len = len < 0 ? 0 : min(len, most);
     }
-    const int per = g.a.n_heads / c.n_kv_heads, t0 = row0 / per, t1 = (row_end - 1) / per;
     window = g.a.window < len ? g.a.window : 0;
     first = len - g.a.n_new + 1;
     hi = max(0, first + t1);
@@ -124,8 +126,6 @@ struct Span {
     lo_all = window ? max(0, first + t1 - window) : 0;
     fb = lo / B;
     nb = hi > lo ? (hi + B - 1) / B - fb : 0;
-    chunk = max(g.chunk, (nb + g.splits - 1) / g.splits);
-    active = max(1, (nb + chunk - 1) / chunk);
   }
 };
 
@@ -166,7 +166,10 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   struct Lds {
     float o[WAVES][16][PAD];
     float m[WAVES][16], l[WAVES][16];
-    uint32_t arrived;
+    int64_t scan[WAVES];
+    int64_t begin;  // of the block's slice, from the first block of its first sequence
+    int first;      // that sequence
+    uint32_t arrived[2];
   };
 
   // words of 16 bytes of V of this lane (E tokens from t0 on) that lie in [lo, hi)
@@ -200,19 +203,103 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   }
   static __device__ __forceinline__ bf16x8 part_of(const u32x4& v, int h) { return E == 8 ? operand(v) : operand8(v[2 * h], v[2 * h + 1]); }
 
+  // sum over the block, and the sum of the threads before this one
+  static __device__ __forceinline__ int64_t scan(int64_t v, int64_t& before, Lds& s) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) s.scan[wave] = x;
+    __syncthreads();
+    int64_t total = 0;
+    before = x - v;
+    for (int w = 0; w < WAVES; ++w) {
+      if (w < wave) before += s.scan[w];
+      total += s.scan[w];
+    }
+    return total;
+  }
+
   static __device__ void run(const AttendArgs& g, Lds& s) {
+    const int tiles = SHARED ? g.tiles : 1, block_row0 = blockIdx.x % g.groups * (16 * tiles), row_end = min(g.rows, block_row0 + 16 * tiles);
+    const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
+    // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
+    // writes its rows.
+    auto blocks_of = [&](int k) { return (int64_t)max(1, Span(g, k, t0, t1, B).nb); };
+    const int mine = (n + THREADS - 1) / THREADS, k0 = min(n, (int)threadIdx.x * mine), k1 = min(n, k0 + mine);  // sequences that a thread counts
+    int64_t total = 0, before = 0, counted = 0;
+    if (n == 1) {
+      total = blocks_of(0);
+    } else {
+      for (int k = k0; k < k1; ++k) counted += blocks_of(k);
+      total = scan(counted, before, s);
+    }
+    const int64_t G = min<int64_t>(g.slices, total);  // (no slice without a block)
+    // (quotients by way of double: exact, as the dividends stay below 2^53, n below 2^16, blocks below 2^27, slices below 2^10)
+    auto quotient = [](int64_t x, int64_t y) { return (int64_t)((double)x / (double)y); };
+    auto slice_end = [&](int w) { return quotient((w + 1) * total, G); };
+    auto slice_of = [&](int64_t block) { return (int)quotient((block + 1) * G - 1, total); };  // the one whose end is the first beyond the block
+    int i = 0;
+    int64_t begin = slice_end(slice - 1), left = slice < G ? slice_end(slice) - begin : 0;
+    if (n > 1) {
+      if (before <= begin && begin < before + counted)
+        for (int k = k0; k < k1; ++k) {
+          const int64_t nb = blocks_of(k);
+          if (begin < before + nb) { s.first = k; s.begin = begin - before; break; }
+          before += nb;
+        }
+      __syncthreads();
+      i = __builtin_amdgcn_readfirstlane(s.first);
+      begin = __builtin_amdgcn_readfirstlane((int)s.begin);
+    }
+    // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
+    int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
+    for (; left > 0; ++i) {
+      const Span sp(g, i, t0, t1, B);
+      const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
+      if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
+      part(g, s, sp, i, tiles, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
+      if (g.slices > 1) {
+        const int64_t first_block = slice_end(slice) - left - off;
+        const int first = where_to < 0 ? slice : slice_of(first_block), parts = where_to < 0 ? 1 : slice_of(first_block + nb - 1) - first + 1;
+        if (where_to == 0) { un_seq[0] = i; un_first[0] = first; un_parts[0] = parts; }
+        if (where_to == 1) { un_seq[1] = i; un_first[1] = first; un_parts[1] = parts; }
+        if (off == 0 && !g.last_joins && threadIdx.x == 0) g.parted[(int64_t)i * gridDim.x + blockIdx.x] = make_int2(first, parts);
+      }
+      begin = 0;
+      left -= take;
+    }
+    if (g.last_joins && max(un_seq[0], un_seq[1]) >= 0) {
+      // The parts of a sequence: the last block to arrive joins them.  Its own sums have reached memory before it is counted
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (threadIdx.x < 2) {
+        const int seq_i = un_seq[threadIdx.x];
+        s.arrived[threadIdx.x] = seq_i < 0 ? 0 : __hip_atomic_fetch_add(g.count + seq_i * gridDim.x + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (un_seq[k] >= 0 && s.arrived[k] == (uint32_t)un_parts[k] - 1) {
+          if (threadIdx.x == 0) __hip_atomic_store(g.count + un_seq[k] * gridDim.x + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          join(g, un_seq[k], un_first[k], un_parts[k], block_row0, row_end);
+        }
+    }
+  }
+
+  // Blocks [b0, b1) of sequence seq_i; where_to: -1: they are all of it, 0 / 1: the unfinished sum at the slice's begin / end
+  static __device__ __forceinline__ void part(const AttendArgs& g, Lds& s, const Span& sp, int seq_i, int tiles, int block_row0, int row_end, int b0, int b1, int where_to) {
     const si_cache_t& c = g.c;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), grp = lane / 16, col = lane % 16;
-    const int split = blockIdx.z, kv = blockIdx.x / g.groups, seq_i = blockIdx.y;
-    const int per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
+    const int kv = blockIdx.x / g.groups, per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
     // the block has the rows [block_row0, row_end), this wave 16 of them from row0 on; `streams` waves take the cache blocks in turn
-    const int tiles = SHARED ? g.tiles : 1, streams = WAVES / tiles, stream = wave / tiles;
-    const int block_row0 = blockIdx.x % g.groups * (16 * tiles), row0 = block_row0 + wave % tiles * 16, row_end = min(g.rows, block_row0 + 16 * tiles);
-    const Span sp(g, seq_i, block_row0, row_end, B);
-    if (sp.why && split == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(c.status, sp.why);
-    if (split >= sp.active) return;
-    const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all, active = sp.active;
-    const int b0 = sp.fb + split * sp.chunk, b1 = min(b0 + sp.chunk, sp.fb + sp.nb);
+    const int streams = WAVES / tiles, stream = wave / tiles, row0 = block_row0 + wave % tiles * 16;
+    const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
     // this lane's row of q, as the right operand; token of the row, or -1
     const int row = row0 + col, tok = row < row_end ? row / per : -1;
@@ -393,14 +480,14 @@ template <int TYPE, int D, bool SHARED> struct Attend {
 #pragma unroll
     for (int i = 0; i < NL; ++i) *reinterpret_cast<f32x4*>(&s.o[wave][col][16 * i + 4 * grp]) = o[i];
     __syncthreads();
-    const int unit = seq_i * gridDim.x + blockIdx.x, part_floats = g.part_rows * (D + 2), items = (row_end - block_row0) * (D / 4);
-    float* part = g.part + ((int64_t)unit * g.splits + split) * part_floats;
+    const int items = (row_end - block_row0) * (D / 4);
+    float* sums = g.part + (((int64_t)blockIdx.x * g.slices + blockIdx.y) * 2 + max(where_to, 0)) * (g.part_rows * (D + 2));
     for (int i = threadIdx.x; i < items; i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
       Sum sum;
       for (int w = r / 16; w < WAVES; w += tiles) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % 16][dim]), s.m[w][r % 16], s.l[w][r % 16]);
-      float* to = part + r * (D + 2);
-      if (active == 1) {
+      float* to = sums + r * (D + 2);
+      if (where_to < 0) {
         write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
       } else if (g.last_joins) {
         put2(to + dim, sum.o[0], sum.o[1]);
@@ -412,32 +499,31 @@ template <int TYPE, int D, bool SHARED> struct Attend {
         if (dim == 0) *reinterpret_cast<float2*>(to + D) = make_float2(sum.m, sum.l);
       }
     }
-    if (active == 1 || !g.last_joins) return;
+    __syncthreads();
+  }
 
-    // the splits of the unit: the last block to arrive joins them.  Its own stores have reached memory before it is counted
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) s.arrived = __hip_atomic_fetch_add(g.count + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (s.arrived != (uint32_t)active - 1) return;
-    asm volatile("" ::: "memory");
-    if (threadIdx.x == 0) __hip_atomic_store(g.count + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float* parts = g.part + (int64_t)unit * g.splits * part_floats;
-    for (int i = threadIdx.x; i < items; i += THREADS) {
+  static __device__ __forceinline__ void join(const AttendArgs& g, int seq_i, int first, int parts, int block_row0, int row_end) {
+    const int kv = blockIdx.x / g.groups, part_floats = g.part_rows * (D + 2);
+    const float* sums = g.part + ((int64_t)blockIdx.x * g.slices + first) * 2 * part_floats;
+    for (int i = threadIdx.x; i < (row_end - block_row0) * (D / 4); i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
       Sum sum;
-      float2 ml[ATTEND_FEW], v[ATTEND_FEW][2];  // (active <= splits <= ATTEND_FEW)
+      constexpr int AHEAD = 8;  // (a trip to memory is about a microsecond)
+      for (int p0 = 0; p0 < parts; p0 += AHEAD) {
+        float2 v[AHEAD][3];
 #pragma unroll
-      for (int k = 0; k < ATTEND_FEW; ++k) {
-        const float* from = parts + (int64_t)min(k, active - 1) * part_floats + r * (D + 2);
-        ml[k] = get2(from + D);
-        v[k][0] = get2(from + dim);
-        v[k][1] = get2(from + dim + 2);
+        for (int k = 0; k < AHEAD; ++k) {
+          const int q = min(p0 + k, parts - 1);  // (all but the first hold the sequence from before)
+          const float* from = sums + (int64_t)(2 * q + (q == 0 ? 1 : 0)) * part_floats + r * (D + 2);
+          v[k][0] = get2(from + dim);
+          v[k][1] = get2(from + dim + 2);
+          v[k][2] = get2(from + D);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+          if (p0 + k < parts) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
       }
-#pragma unroll
-      for (int k = 0; k < ATTEND_FEW; ++k)
-        if (k < active) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, ml[k].x, ml[k].y);
-      write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
+      write_row(g, seq_i, kv, block_row0 + r, dim, sum, TYPE == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
     }
   }
 };
@@ -447,53 +533,52 @@ template <int TYPE, int D, bool SHARED> __global__ __launch_bounds__((Attend<TYP
   Attend<TYPE, D, SHARED>::run(g, s);
 }
 
-// Joins the splits of a unit: a block has one row, and its threads a share of the splits of 4 elements each.
-template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g, int B) {
+// Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
+template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   constexpr int LANES = D / 4, SHARES = 256 / LANES;
   __shared__ f32x4 s_o[SHARES][LANES];
   __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
-  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, block_row0 = blockIdx.x % g.groups * (16 * g.tiles), r = blockIdx.z;
-  const int row_end = min(g.rows, block_row0 + 16 * g.tiles);
-  if (block_row0 + r >= row_end) return;
-  const Span sp(g, seq_i, block_row0, row_end, B);
-  if (sp.active == 1) return;  // (written already)
+  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, row = blockIdx.x % g.groups * (16 * g.tiles) + blockIdx.z;
+  typedef const int32_t __attribute__((address_space(4))) constant_t;
+  const constant_t* parted = (const constant_t*)(uintptr_t)(g.parted + (int64_t)seq_i * gridDim.x + blockIdx.x);
+  const int first = parted[0], parts = parted[1];
+  if (row >= g.rows || parts == 1) return;  // (one part is written already)
   const int lane = threadIdx.x % LANES, share = threadIdx.x / LANES, part_floats = g.part_rows * (D + 2);
-  const float* from = g.part + (int64_t)(seq_i * gridDim.x + blockIdx.x) * g.splits * part_floats + r * (D + 2);
+  const float* from = g.part + ((int64_t)blockIdx.x * g.slices + first) * 2 * part_floats + blockIdx.z * (D + 2);
   Sum sum;
   if (share < SHARES) {
     constexpr int AHEAD = 4;
-    for (int s0 = share; s0 < sp.active; s0 += AHEAD * SHARES) {
+    for (int p0 = share; p0 < parts; p0 += AHEAD * SHARES) {
       float2 v[AHEAD][3];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        const float* p = from + (int64_t)min(s0 + k * SHARES, sp.active - 1) * part_floats;
+        const int q = min(p0 + k * SHARES, parts - 1);
+        const float* p = from + (int64_t)(2 * q + (q == 0 ? 1 : 0)) * part_floats;
         v[k][0] = *reinterpret_cast<const float2*>(p + 4 * lane);
         v[k][1] = *reinterpret_cast<const float2*>(p + 4 * lane + 2);
         v[k][2] = *reinterpret_cast<const float2*>(p + D);
       }
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
-        if (s0 + k * SHARES < sp.active) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
+        if (p0 + k * SHARES < parts) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
     }
     s_o[share][lane] = sum.o; s_m[share][lane] = sum.m; s_l[share][lane] = sum.l;
   }
   __syncthreads();
   if (share > 0) return;
-  for (int k = 1; k < min(SHARES, sp.active); ++k) sum.add(s_o[k][lane], s_m[k][lane], s_l[k][lane]);
-  write_row(g, seq_i, kv, block_row0 + r, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+  for (int k = 1; k < min(SHARES, parts); ++k) sum.add(s_o[k][lane], s_m[k][lane], s_l[k][lane]);
+  write_row(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
 }
 
 template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
-  // Blocks go to the dies in turn: heads first, so that a long sequence is spread over all of them (with the splits first, and 8 of them, the die that
-  // gets the last split of every sequence has nothing to do where most are short: 64 sequences of 1 .. 8000 positions 232 us, not 162), then
-  // sequences, then splits: the short ones end last.
-  const dim3 grid(g.c.n_kv_heads * g.groups, g.a.n, g.splits);
+  // (heads first: blocks go to the dies in turn, and all heads of a slice have the same to do)
+  const dim3 grid(g.c.n_kv_heads * g.groups, g.slices);
   if (g.tiles > 1) hipLaunchKernelGGL((k_attend<TYPE, D, true>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else hipLaunchKernelGGL((k_attend<TYPE, D, false>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  if (g.splits > 1 && !g.last_joins) {
+  if (g.slices > 1 && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_join<D>, dim3(grid.x, grid.y, g.part_rows), dim3(256), 0, stream, g, Attend<TYPE, D, true>::B);
+    hipLaunchKernelGGL(k_join<D>, dim3(grid.x, g.a.n, g.part_rows), dim3(256), 0, stream, g);
   }
   return hipGetLastError();
 }
