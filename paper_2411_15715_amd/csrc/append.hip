@@ -22,9 +22,9 @@ struct Args {
   si_append_t a;
   int layer;
   int per_block;    // tokens of a block of the q / k part
-  int qk_tokens;    // blocks of the q / k part along the tokens
-  int qk_columns;   // and along the units of a token
+  int qk_columns;   // blocks of the q / k part along the units of a token
   int v_columns;    // blocks of the v part along its columns
+  int v_blocks;     // and in all
 };
 
 __device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
@@ -46,8 +46,7 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
-__device__ __forceinline__ void load8(const uint16_t* p, float (&f)[8]) {
-  const u32x4 v = *reinterpret_cast<const u32x4_a2*>(p);
+__device__ __forceinline__ void widen8(const u32x4& v, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
 }
@@ -90,6 +89,7 @@ template <int TYPE> __device__ __forceinline__ void store_k1(const Args& g, cons
 
 // q and k of per_block tokens.  A thread takes 16 elements of a head: with rot_dim a multiple of 16 the two vectors that turn into each
 // other (or 16 neighbours), so that every element is read once and q may be turned in place; else single pairs and single elements.
+// What a thread needs first is on its way while the angles are formed, and what it needs next while it turns what it has.
 template <int TYPE> __device__ void qk_part(const Args& g, int block) {
   __shared__ float2 s_turn[MAX_TOKENS][MAX_ANGLES];
   __shared__ Token s_token[MAX_TOKENS];
@@ -97,6 +97,41 @@ template <int TYPE> __device__ void qk_part(const Args& g, int block) {
   const si_append_t& a = g.a;
   const int d = g.c.head_dim, half = a.rot_dim / 2, tid = threadIdx.x;
   const int t0 = block / g.qk_columns * g.per_block, n = min(g.per_block, a.n_tokens - t0), column = block % g.qk_columns;
+  const int n_heads = a.q ? a.n_heads : 0, heads = n_heads + g.c.n_kv_heads;
+  const bool wide = a.rot_dim % 16 == 0;
+  const int per_head = wide ? d / 16 : half + (d - a.rot_dim);
+  const uint32_t inv = (uint32_t)(0x100000000ull / per_head) + 1;  // u / per_head = umulhi(u, inv) while u * per_head < 2^32
+  const int units = heads * per_head, span = (units + g.qk_columns - 1) / g.qk_columns;
+  const int u0 = column * span, u1 = min(units, u0 + span), all = max(0, u1 - u0) * n;
+
+  struct Unit {
+    u32x4 x, y;
+    int t, head, j;  // token of the block, head (k: after q's), unit of the head
+  };
+  auto source = [&](const Unit& k) {
+    const bool is_q = k.head < n_heads;
+    return static_cast<const uint16_t*>(is_q ? a.q : a.k) + (int64_t)(t0 + k.t) * (is_q ? a.q_stride : a.k_stride) + (is_q ? k.head : k.head - n_heads) * d;
+  };
+  // first elements of the two vectors of a unit
+  auto dim0 = [&](int j) { return j < a.rot_dim / 16 && !a.rot_pairs ? 8 * j : 16 * j; };
+  auto dim1 = [&](int j) { return j < a.rot_dim / 16 && !a.rot_pairs ? 8 * j + half : 16 * j + 8; };
+  auto fetch = [&](int f) {
+    Unit k;
+    k.t = 0;
+    int u = f;
+    while (u >= u1 - u0) { u -= u1 - u0; ++k.t; }
+    u += u0;
+    k.head = (int)__umulhi((uint32_t)u, inv);
+    k.j = u - k.head * per_head;
+    if (wide) {
+      const uint16_t* p = source(k);
+      k.x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(p + dim0(k.j)));
+      k.y = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(p + dim1(k.j)));
+    }
+    return k;
+  };
+  Unit next;
+  if (tid < all) next = fetch(tid);
   for (int i = tid; i < n * half; i += THREADS) s_turn[i / half][i % half] = turn(a.pos[t0 + i / half], a.inv_freq[i % half]);
   if (tid < n) {
     const int seq = a.seq[t0 + tid], pos = a.pos[t0 + tid];
@@ -115,65 +150,54 @@ template <int TYPE> __device__ void qk_part(const Args& g, int block) {
     s_token[tid] = t;
   }
   __syncthreads();
-  const int n_heads = a.q ? a.n_heads : 0, heads = n_heads + g.c.n_kv_heads;
-  const bool wide = a.rot_dim % 16 == 0;
-  const int per_head = wide ? d / 16 : half + (d - a.rot_dim);
-  const uint32_t inv = (uint32_t)(0x100000000ull / per_head) + 1;  // u / per_head = umulhi(u, inv) while u * per_head < 2^32
-  const int units = heads * per_head, span = (units + g.qk_columns - 1) / g.qk_columns;
-  const int u0 = column * span, u1 = min(units, u0 + span);
-  for (int t = 0; t < n; ++t) {
-    const Token tok = s_token[t];
-    for (int u = u0 + tid; u < u1; u += THREADS) {
-      const int h = (int)__umulhi((uint32_t)u, inv), j = u - h * per_head;
-      const bool is_q = h < n_heads;
-      const int head = is_q ? h : h - n_heads;
-      if (!is_q && tok.k < 0) continue;
-      const uint16_t* src = static_cast<const uint16_t*>(is_q ? a.q : a.k) + (int64_t)(t0 + t) * (is_q ? a.q_stride : a.k_stride) + head * d;
-      uint16_t* dst = static_cast<uint16_t*>(a.q_out) + (int64_t)(t0 + t) * a.q_out_stride + head * d;
-      if (wide) {
-        const bool turned = j < a.rot_dim / 16;
-        const int d0 = turned && !a.rot_pairs ? 8 * j : 16 * j, d1 = turned && !a.rot_pairs ? d0 + half : d0 + 8;
-        float x[8], y[8];
-        load8(src + d0, x);
-        load8(src + d1, y);
-        if (turned) {
+  for (int f = tid; f < all; f += THREADS) {
+    const Unit k = next;
+    if (f + THREADS < all) next = fetch(f + THREADS);
+    const Token tok = s_token[k.t];
+    const bool is_q = k.head < n_heads;
+    const int head = is_q ? k.head : k.head - n_heads, j = k.j;
+    if (!is_q && tok.k < 0) continue;
+    uint16_t* dst = static_cast<uint16_t*>(a.q_out) + (int64_t)(t0 + k.t) * a.q_out_stride + head * d;
+    if (wide) {
+      float x[8], y[8];
+      widen8(k.x, x);
+      widen8(k.y, y);
+      if (j < a.rot_dim / 16) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 cs = s_turn[t][8 * j + i];
-            float& p = a.rot_pairs ? (i < 4 ? x[(2 * i) % 8] : y[(2 * i) % 8]) : x[i];
-            float& q = a.rot_pairs ? (i < 4 ? x[(2 * i + 1) % 8] : y[(2 * i + 1) % 8]) : y[i];
-            const float p0 = p, q0 = q;
-            p = p0 * cs.x - q0 * cs.y;
-            q = q0 * cs.x + p0 * cs.y;
-          }
+        for (int i = 0; i < 8; ++i) {
+          const float2 cs = s_turn[k.t][8 * j + i];
+          float& p = a.rot_pairs ? (i < 4 ? x[(2 * i) % 8] : y[(2 * i) % 8]) : x[i];
+          float& q = a.rot_pairs ? (i < 4 ? x[(2 * i + 1) % 8] : y[(2 * i + 1) % 8]) : y[i];
+          const float p0 = p, q0 = q;
+          p = p0 * cs.x - q0 * cs.y;
+          q = q0 * cs.x + p0 * cs.y;
         }
-        if (is_q) {
-          if (tok.k < 0)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
-          *reinterpret_cast<u32x4_a2*>(dst + d0) = pack8(x);
-          *reinterpret_cast<u32x4_a2*>(dst + d1) = pack8(y);
-        } else {
-          store_k<TYPE>(g, tok, head, d0, x);
-          store_k<TYPE>(g, tok, head, d1, y);
-        }
+      }
+      if (is_q) {
+        const bool out = tok.k < 0;
+        *reinterpret_cast<u32x4_a2*>(dst + dim0(j)) = out ? u32x4{0, 0, 0, 0} : pack8(x);
+        *reinterpret_cast<u32x4_a2*>(dst + dim1(j)) = out ? u32x4{0, 0, 0, 0} : pack8(y);
       } else {
-        const bool turned = j < half;
-        const int d0 = turned ? (a.rot_pairs ? 2 * j : j) : j + half, d1 = a.rot_pairs ? d0 + 1 : d0 + half;
-        float x = widen(src[d0]), y = turned ? widen(src[d1]) : 0.f;
-        if (turned) {
-          const float2 cs = s_turn[t][j];
-          const float x0 = x;
-          x = x0 * cs.x - y * cs.y;
-          y = y * cs.x + x0 * cs.y;
-        }
-        if (is_q) {
-          dst[d0] = tok.k < 0 ? 0 : bf16_bits(x);
-          if (turned) dst[d1] = tok.k < 0 ? 0 : bf16_bits(y);
-        } else {
-          store_k1<TYPE>(g, tok, head, d0, x);
-          if (turned) store_k1<TYPE>(g, tok, head, d1, y);
-        }
+        store_k<TYPE>(g, tok, head, dim0(j), x);
+        store_k<TYPE>(g, tok, head, dim1(j), y);
+      }
+    } else {
+      const bool turned = j < half;
+      const int d0 = turned ? (a.rot_pairs ? 2 * j : j) : j + half, d1 = a.rot_pairs ? d0 + 1 : d0 + half;
+      const uint16_t* src = source(k);
+      float x = widen(src[d0]), y = turned ? widen(src[d1]) : 0.f;
+      if (turned) {
+        const float2 cs = s_turn[k.t][j];
+        const float x0 = x;
+        x = x0 * cs.x - y * cs.y;
+        y = y * cs.x + x0 * cs.y;
+      }
+      if (is_q) {
+        dst[d0] = tok.k < 0 ? 0 : bf16_bits(x);
+        if (turned) dst[d1] = tok.k < 0 ? 0 : bf16_bits(y);
+      } else {
+        store_k1<TYPE>(g, tok, head, d0, x);
+        if (turned) store_k1<TYPE>(g, tok, head, d1, y);
       }
     }
   }
@@ -246,23 +270,25 @@ template <int TYPE> __device__ void v_part(const Args& g, int block) {
 }
 
 template <int TYPE> __global__ __launch_bounds__(THREADS) void k_append(Args g) {
-  const int qk = g.qk_tokens * g.qk_columns;
-  if ((int)blockIdx.x < qk) qk_part<TYPE>(g, blockIdx.x);
-  else v_part<TYPE>(g, blockIdx.x - qk);
+  // (v first: its blocks have the longer way from load to store)
+  if ((int)blockIdx.x < g.v_blocks) v_part<TYPE>(g, blockIdx.x);
+  else qk_part<TYPE>(g, blockIdx.x - g.v_blocks);
 }
 
 bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 hipError_t launch_append(const si_cache_t& c, int layer, const si_append_t& a, hipStream_t stream) {
-  Args g{c, a, layer, 1, 0, 1, 0};
-  const int units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * c.head_dim / 16;
-  // few tokens: a block has one of them and 256 threads' worth of its heads; many: 4, whose angles it forms once for all heads
-  if (a.n_tokens >= 1024) g.per_block = MAX_TOKENS;
-  else g.qk_columns = std::max(1, (units + THREADS - 1) / THREADS);
-  g.qk_tokens = (a.n_tokens + g.per_block - 1) / g.per_block;
-  g.v_columns = (c.n_kv_heads * c.head_dim + THREADS - 1) / THREADS;
+  Args g{c, a, layer, 1, 1, 0, 0};
+  const int per_head = a.rot_dim % 16 == 0 ? c.head_dim / 16 : c.head_dim - a.rot_dim / 2, units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * per_head;
+  // A block has up to four units a thread, of one token or of up to 4 where these have few (4099 tokens of 576 units: 51 us with the angles formed
+  // by two blocks of a token, 39 by one); with few tokens one unit a thread (what waits there is memory, not the threads)
+  const int want = THREADS * (a.n_tokens >= 256 ? 4 : 1);
+  if (units >= want) g.qk_columns = (units + want - 1) / want;
+  else if (a.n_tokens >= 256) g.per_block = std::min(MAX_TOKENS, want / units);
   const int E = kv_vec(c.type);
-  const int64_t blocks = (int64_t)g.qk_tokens * g.qk_columns + (int64_t)((a.n_tokens + E - 1) / E) * g.v_columns;
+  g.v_columns = (c.n_kv_heads * c.head_dim + THREADS - 1) / THREADS;
+  g.v_blocks = (a.n_tokens + E - 1) / E * g.v_columns;
+  const int64_t blocks = (int64_t)((a.n_tokens + g.per_block - 1) / g.per_block) * g.qk_columns + g.v_blocks;
   if (c.type == SI_KV_BF16) hipLaunchKernelGGL(k_append<SI_KV_BF16>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
   else hipLaunchKernelGGL(k_append<SI_KV_E4M3>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
   return hipGetLastError();
