@@ -24,11 +24,13 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
   const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B), units = (int64_t)c.n_kv_heads * k.groups;
-  // As many blocks as there are compute units, twice that where a slice holds several sequences (the next one's first loads have nothing beside
-  // them: 512 sequences of 64 positions 67 -> 38 us) and the waves of a block do not share their loads (40 rows: 114 -> 156 us).  Joining
-  // costs as much as five cache blocks a wave (517 positions, 17 blocks over 4 waves, 9.4 us whole, 10.4 in two); beyond, none has
-  // fewer than two a wave.
-  const int most = a.n * units > 256 && k.tiles < 4 ? 512 : 256, streams = ATTEND_WAVES / k.tiles;
+  // As many blocks as there are compute units; twice that where a slice holds several sequences (the next one's first loads have nothing beside
+  // them: 512 sequences of 64 positions 57 -> 38 us) or the waves of a block share their loads and wait for each other (40 rows over
+  // 16 x 8000 positions 119 -> 106 us) and two blocks fit a unit.  Else it is one more round of sums to write and read (131071 positions 86
+  // against 88 us).  Joining costs as much as five cache blocks a wave (517 positions, 17 blocks over 4 waves: 9.4 us whole, 10.4 in two
+  // slices); beyond, no slice has fewer than two a wave.
+  const bool twice = c.head_dim <= 128 && (k.tiles > 1 || a.n * units > 256);
+  const int most = twice ? 512 : 256, streams = ATTEND_WAVES / k.tiles;
   const int64_t least = each <= 5 * streams ? each : 2 * streams;
   k.slices = (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + least - 1) / least));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;

@@ -32,7 +32,7 @@ struct AttendArgs {
   int layer;
   int rows;       // rows of a unit in all: n_new * heads per kv head
   int groups;     // row groups: blocks that share a kv head
-  int tiles;      // waves of a block that share a stream of cache blocks, each with 16 rows of its own: a power of two
+  int tiles;      // waves of a block that share a stream of cache blocks, each with 16 rows of its own: 1, 2 or 4
   int slices;     // G
   int part_rows;  // rows of a unit that the scratch has room for: min(rows, 16 tiles)
   int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
@@ -150,10 +150,15 @@ __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv
   if (dim == 0 && g.a.lse) g.a.lse[r * g.a.n_heads + head] = s.l == 0.f ? -INFINITY : (s.m + log2f(s.l)) * 0.69314718055994531f;
 }
 
-// SHARED: several waves of a block read the same cache blocks (tiles > 1); their loads are to stay in the caches until the last of them has
-// come, the others go past them (each is right where it is: 131071 positions, one tile, 86 us with the hint and 97 without; 40 rows, 16 x 8000
-// positions, 128 with it and 110 without)
-template <int TYPE, int D, bool SHARED> struct Attend {
+// s_waitcnt vmcnt(n) alone, n < 64
+template <int N> __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 0xf) | (((N >> 4) & 3) << 14)); }
+
+// TILES waves of a block have 16 rows each and go through the same cache blocks; 4 / TILES streams of them take these in turn.  Alone (TILES == 1)
+// a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97).  Several read them from LDS, into
+// which the block loads each cache block once, without a detour through registers: S stages of a block for each stream.  (Each
+// wave loading for itself, TILES requests for every line at the caches: 24 rows over 16 x 8000 positions 108 us, this way 97.)
+template <int TYPE, int D, int TILES> struct Attend {
+  static constexpr bool SHARED = TILES > 1;
   static constexpr int E = TYPE == SI_KV_E4M3 ? 16 : 8, B = 4 * E, J = E / 4;  // J score tiles of 16 tokens
   static constexpr int NL = D / 16;                                           // loads of 16 bytes of K, and of V, a lane and block
   static constexpr int H = E / 8;                                             // operands of 8 elements in 16 bytes
@@ -163,9 +168,18 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256 a wave has a SIMD for itself.
   static constexpr int WAVES_PER_SIMD = D < 256 ? 2 : 1;
 
+  static constexpr int STREAMS = WAVES / TILES, BLOCK_BYTES = 128 * D, STAGE = STREAMS * BLOCK_BYTES;
+  static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;  // (two blocks a compute unit, where heads are no longer than 128)
+  static constexpr int PIECES = STAGE / 1024 / WAVES;                  // loads of a stage by each wave
+
   struct Lds {
-    float o[WAVES][16][PAD];
-    float m[WAVES][16], l[WAVES][16];
+    union {
+      struct {
+        float o[WAVES][16][PAD];
+        float m[WAVES][16], l[WAVES][16];
+      };
+      char ring[SHARED ? S * STAGE : 16];
+    };
     int64_t scan[WAVES];
     int64_t begin;  // of the block's slice, from the first block of its first sequence
     int first;      // that sequence
@@ -197,9 +211,10 @@ template <int TYPE, int D, bool SHARED> struct Attend {
       }
     return bad;
   }
-  static __device__ __forceinline__ u32x4 load16(const char* p) {
-    if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(p);
-    else return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  static __device__ __forceinline__ u32x4 load16(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+  // 1 KB from the lanes' addresses to LDS, on its way until waited for
+  static __device__ __forceinline__ void load_lds(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from, (void __attribute__((address_space(3)))*)to, 16, 0, 2 /* nt */);
   }
   static __device__ __forceinline__ bf16x8 part_of(const u32x4& v, int h) { return E == 8 ? operand(v) : operand8(v[2 * h], v[2 * h + 1]); }
 
@@ -225,7 +240,7 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   }
 
   static __device__ void run(const AttendArgs& g, Lds& s) {
-    const int tiles = SHARED ? g.tiles : 1, block_row0 = blockIdx.x % g.groups * (16 * tiles), row_end = min(g.rows, block_row0 + 16 * tiles);
+    const int block_row0 = blockIdx.x % g.groups * (16 * TILES), row_end = min(g.rows, block_row0 + 16 * TILES);
     const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
@@ -262,7 +277,7 @@ template <int TYPE, int D, bool SHARED> struct Attend {
       const Span sp(g, i, t0, t1, B);
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
-      part(g, s, sp, i, tiles, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
+      part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
       if (g.slices > 1) {
         const int64_t first_block = slice_end(slice) - left - off;
         const int first = where_to < 0 ? slice : slice_of(first_block), parts = where_to < 0 ? 1 : slice_of(first_block + nb - 1) - first + 1;
@@ -293,12 +308,12 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   }
 
   // Blocks [b0, b1) of sequence seq_i; where_to: -1: they are all of it, 0 / 1: the unfinished sum at the slice's begin / end
-  static __device__ __forceinline__ void part(const AttendArgs& g, Lds& s, const Span& sp, int seq_i, int tiles, int block_row0, int row_end, int b0, int b1, int where_to) {
+  static __device__ __forceinline__ void part(const AttendArgs& g, Lds& s, const Span& sp, int seq_i, int block_row0, int row_end, int b0, int b1, int where_to) {
     const si_cache_t& c = g.c;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), grp = lane / 16, col = lane % 16;
     const int kv = blockIdx.x / g.groups, per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
-    // the block has the rows [block_row0, row_end), this wave 16 of them from row0 on; `streams` waves take the cache blocks in turn
-    const int streams = WAVES / tiles, stream = wave / tiles, row0 = block_row0 + wave % tiles * 16;
+    // the block has the rows [block_row0, row_end), this wave 16 of them from row0 on; STREAMS waves take the cache blocks in turn
+    const int stream = wave / TILES, row0 = block_row0 + wave % TILES * 16;
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
     // this lane's row of q, as the right operand; token of the row, or -1
@@ -332,8 +347,8 @@ template <int TYPE, int D, bool SHARED> struct Attend {
       const int page = ((constant_t*)(uintptr_t)table)[min(w.entry, last_entry)];
       return page >= 0 && page < c.n_pages ? page : -1;
     };
-    auto step = [&](Place w) {
-      w.at += streams;
+    auto step = [&](Place w, int by) {
+      w.at += by;
       while (w.at >= per_page) { w.at -= per_page; ++w.entry; }
       return w;
     };
@@ -342,7 +357,8 @@ template <int TYPE, int D, bool SHARED> struct Attend {
     const char* k_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 0, kv) * BYTES;
     const char* v_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 1, kv) * BYTES;
     const int k_lane = grp * (B * 16) + col * 16, v_lane = grp * (D * 16) + col * 16;
-    u32x4 kf[NL], vf[NL];
+    const char *k_lds = nullptr, *v_lds = nullptr;  // SHARED: the block in work
+    u32x4 kf[SHARED ? 1 : NL], vf[SHARED ? 1 : NL];
     auto load_k = [&](int page, int at) {
       const char* p = k_base + (uint32_t)max(page, 0) * page_bytes + at * (64 * D);
 #pragma unroll
@@ -353,6 +369,14 @@ template <int TYPE, int D, bool SHARED> struct Attend {
 #pragma unroll
       for (int i = 0; i < NL; ++i) vf[i] = load16(p + v_lane + i * 256);
     };
+    auto k_of = [&](int i) {
+      if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(k_lds + k_lane + i / J * (4 * B * 16) + i % J * 256);
+      else return kf[i];
+    };
+    auto v_of = [&](int i) {
+      if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(v_lds + v_lane + i * 256);
+      else return vf[i];
+    };
 
     // scores of a block: tile j, element i of this lane is token grp * E + 4 j + i
     f32x4 x[J];
@@ -360,9 +384,11 @@ template <int TYPE, int D, bool SHARED> struct Attend {
 #pragma unroll
       for (int j = 0; j < J; ++j) x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NL; ++i)
+      for (int i = 0; i < NL; ++i) {
+        const u32x4 k = k_of(i);
 #pragma unroll
-        for (int h = 0; h < H; ++h) x[i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(kf[i], h), operand(q[i / J * H + h]), x[i % J], 0, 0, 0);
+        for (int h = 0; h < H; ++h) x[i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(k, h), operand(q[i / J * H + h]), x[i % J], 0, 0, 0);
+      }
     };
     // weights of the block, and what has been summed brought to its maximum; EDGE: some rows may not see some of its tokens.
     // The weights are rounded to bf16, as operands are (2^-8 of each, the sum l takes them as they were: the error of out is that of a
@@ -401,31 +427,33 @@ template <int TYPE, int D, bool SHARED> struct Attend {
           p[h][w] = bf16_pair(a, e);
         }
     };
-    auto products = [&] {
+    auto products = [&](auto EDGE, const u32x4& keep) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i)
+      for (int i = 0; i < NL; ++i) {
+        u32x4 v = v_of(i);
+        if constexpr (EDGE) v &= keep;
 #pragma unroll
-        for (int h = 0; h < H; ++h) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(vf[i], h), operand(p[h]), o[i], 0, 0, 0);
+        for (int h = 0; h < H; ++h) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[h]), o[i], 0, 0, 0);
+      }
     };
     // the same where some rows may not see some tokens.  What no row sees may be anything (weight 0 times infinity would be NaN); what
     // some of the tokens see and is not finite takes a product for each of them
     auto products_at_edge = [&](int t0) {
       const u32x4 keep = token_mask(t0 + grp * E, lo, hi);
       bool bad = false;
+      if (n_new > 1) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        vf[i] &= keep;
-        bad |= not_finite(vf[i]);
+        for (int i = 0; i < NL; ++i) bad |= not_finite(v_of(i) & keep);
       }
-      if (n_new == 1 || !__any(bad)) {
-        products();
+      if (!__any(bad)) {
+        products(std::true_type{}, keep);
         return;
       }
       for (int j = row0 / per; j <= (min(row_end, row0 + 16) - 1) / per; ++j) {
         const u32x4 mine = token_mask(t0 + grp * E, window ? max(0, first + j - window) : 0, max(0, first + j));
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          const u32x4 v = vf[i] & mine;
+          const u32x4 v = v_of(i) & mine;
           f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[h]), r, 0, 0, 0);
@@ -433,46 +461,94 @@ template <int TYPE, int D, bool SHARED> struct Attend {
         }
       }
     };
+    auto weigh = [&](int t0) {  // after the scores; the main path and that of the edges
+      if (t0 < lo_all || t0 + B > hi_all) {
+        weights(std::true_type{}, t0);
+        products_at_edge(t0);
+      } else {
+        weights(std::false_type{}, t0);
+        products(std::false_type{}, u32x4{});
+      }
+    };
 
-    // K of the next block is asked for when the scores of this one are formed, V when it has been multiplied: 8 to 16 KB of a wave are
-    // always on their way (heads of 128).  The last block has no next: written out, so that the loop's loads stand under no condition.
-    int b = b0 + stream;
-    if (b < b1 && row0 < row_end) {
-      bool bad_page = false;
-      const Place here{b / per_page, b % per_page};
-      Place next = step(here);
-      int page = page_of(here), next_page = page_of(next);
-      load_k(page, here.at);
-      load_v(page, here.at);
-      for (; b + streams < b1; b += streams) {
-        const int t0 = b * B;
-        const Place after = step(next);
-        const int after_page = page_of(after);
-        scores();
-        load_k(next_page, next.at);
-        if (page >= 0) {  // (a block whose page is not there is passed over)
-          if (t0 < lo_all || t0 + B > hi_all) {
-            weights(std::true_type{}, t0);
-            products_at_edge(t0);
-          } else {
-            weights(std::false_type{}, t0);
-            products();
+    bool bad_page = false;
+    if constexpr (SHARED) {
+      const int turns = (b1 - b0 + STREAMS - 1) / STREAMS;
+      uint32_t missing = 0;  // bit turn * STREAMS + stream, modulo 32: the block's page is not there
+      Place front{b0 / per_page, b0 % per_page};
+      // (S stages at most hold 4 x 2 bits)
+      auto issue = [&](int turn) {
+#pragma unroll
+        for (int st = 0; st < STREAMS; ++st) {
+          const int page = page_of(front);
+          const uint32_t bit = 1u << ((turn * STREAMS + st) % 32);
+          missing = page < 0 ? missing | bit : missing & ~bit;
+          const int64_t at = (uint32_t)max(page, 0) * page_bytes + front.at * (64 * D);
+          char* to = s.ring + turn % S * STAGE + st * BLOCK_BYTES;
+#pragma unroll
+          for (int q4 = 0; q4 < PIECES / STREAMS; ++q4) {
+            const int piece = WAVES * q4 + wave;  // of the block: K, then V
+            load_lds((piece < D / 16 ? k_base + at + piece * 1024 : v_base + at + (piece - D / 16) * 1024) + lane * 16, to + piece * 1024);
+          }
+          if (b0 + turn * STREAMS + st < b1 - 1) front = step(front, 1);  // (beyond the last block: that one again)
+        }
+      };
+      for (int turn = 0; turn < min(S - 1, turns); ++turn) issue(turn);
+      for (int turn = 0; turn < turns; ++turn) {
+        const int younger = min(S - 2, turns - 1 - turn);  // stages asked for after this one
+        if (younger >= 2) wait_vmcnt<2 * PIECES>();
+        else if (younger == 1) wait_vmcnt<PIECES>();
+        else wait_vmcnt<0>();
+        // everybody's loads of this stage have arrived, and what was read of the one before has been used
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int b = b0 + turn * STREAMS + stream;
+        const bool here = !(missing >> ((turn * STREAMS + stream) % 32) & 1);
+        if (turn + S - 1 < turns) issue(turn + S - 1);
+        if (b < b1 && row0 < row_end) {
+          bad_page |= !here;
+          k_lds = s.ring + turn % S * STAGE + stream * BLOCK_BYTES;
+          v_lds = k_lds + 64 * D;
+          if (here) {
+            scores();
+            weigh(b * B);
           }
         }
-        load_v(next_page, next.at);
+      }
+      if (turns > 0) __syncthreads();  // (the ring's memory is used anew)
+    } else {
+      // K of the next block is asked for when the scores of this one are formed, V when it has been multiplied: 8 to 16 KB of a wave are
+      // always on their way (heads of 128).  The last block has no next: written out, so that the loop's loads stand under no condition.
+      int b = b0 + stream;
+      if (b < b1) {
+        const Place here{b / per_page, b % per_page};
+        Place next = step(here, STREAMS);
+        int page = page_of(here), next_page = page_of(next);
+        load_k(page, here.at);
+        load_v(page, here.at);
+        for (; b + STREAMS < b1; b += STREAMS) {
+          const Place after = step(next, STREAMS);
+          const int after_page = page_of(after);
+          scores();
+          load_k(next_page, next.at);
+          if (page >= 0) weigh(b * B);  // (a block whose page is not there is passed over)
+          load_v(next_page, next.at);
+          bad_page |= page < 0;
+          page = next_page;
+          next_page = after_page;
+          next = after;
+        }
         bad_page |= page < 0;
-        page = next_page;
-        next_page = after_page;
-        next = after;
+        if (page >= 0) {
+          scores();
+          weights(std::true_type{}, b * B);
+          products_at_edge(b * B);
+        }
       }
-      bad_page |= page < 0;
-      if (page >= 0) {
-        scores();
-        weights(std::true_type{}, b * B);
-        products_at_edge(b * B);
-      }
-      if (bad_page && lane == 0) atomicOr(c.status, SI_CACHE_BAD_PAGE);
     }
+    if (bad_page && lane == 0) atomicOr(c.status, SI_CACHE_BAD_PAGE);
 
     // the streams of the block
     l = sum_of_row(l);
@@ -485,7 +561,7 @@ template <int TYPE, int D, bool SHARED> struct Attend {
     for (int i = threadIdx.x; i < items; i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
       Sum sum;
-      for (int w = r / 16; w < WAVES; w += tiles) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % 16][dim]), s.m[w][r % 16], s.l[w][r % 16]);
+      for (int w = r / 16; w < WAVES; w += TILES) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % 16][dim]), s.m[w][r % 16], s.l[w][r % 16]);
       float* to = sums + r * (D + 2);
       if (where_to < 0) {
         write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
@@ -528,9 +604,9 @@ template <int TYPE, int D, bool SHARED> struct Attend {
   }
 };
 
-template <int TYPE, int D, bool SHARED> __global__ __launch_bounds__((Attend<TYPE, D, SHARED>::THREADS), (Attend<TYPE, D, SHARED>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
-  __shared__ typename Attend<TYPE, D, SHARED>::Lds s;
-  Attend<TYPE, D, SHARED>::run(g, s);
+template <int TYPE, int D, int TILES> __global__ __launch_bounds__((Attend<TYPE, D, TILES>::THREADS), (Attend<TYPE, D, TILES>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
+  __shared__ typename Attend<TYPE, D, TILES>::Lds s;
+  Attend<TYPE, D, TILES>::run(g, s);
 }
 
 // Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
@@ -573,8 +649,9 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
 template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
   // (heads first: blocks go to the dies in turn, and all heads of a slice have the same to do)
   const dim3 grid(g.c.n_kv_heads * g.groups, g.slices);
-  if (g.tiles > 1) hipLaunchKernelGGL((k_attend<TYPE, D, true>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else hipLaunchKernelGGL((k_attend<TYPE, D, false>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  if (g.tiles == 1) hipLaunchKernelGGL((k_attend<TYPE, D, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.tiles == 2) hipLaunchKernelGGL((k_attend<TYPE, D, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else hipLaunchKernelGGL((k_attend<TYPE, D, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   if (g.slices > 1 && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
