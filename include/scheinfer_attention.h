@@ -184,7 +184,7 @@ int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc
  * cache->refs and cache->scratch are needed.
  * Errors: SI_EINVAL (NULL or misaligned pointer, n negative or above SI_CACHE_MAX_LIST, bad cache descriptor), SI_EHIP.  n == 0 is a no-op.
  */
-#define SI_CACHE_MAX_LIST 2048
+#define SI_CACHE_MAX_LIST 1024
 
 /* Bytes of cache->scratch, or a negative SI_E* code (host only; pages and tables may be NULL). */
 int64_t si_cache_scratch_bytes(const si_cache_t* cache);

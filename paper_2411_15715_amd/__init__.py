@@ -33,7 +33,7 @@ SI_F32, SI_BF16 = 0, 1
 SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
 SI_NORM_MAX_D = 32768
 SI_KV_BF16, SI_KV_E4M3 = 0, 1
-SI_CACHE_MAX_LIST = 2048
+SI_CACHE_MAX_LIST = 1024
 SI_CACHE_BAD_SEQ, SI_CACHE_BAD_LEN, SI_CACHE_BAD_PAGE, SI_CACHE_NO_PAGES, SI_CACHE_NO_ROOM = 1, 2, 4, 8, 16
 
 

@@ -1,5 +1,7 @@
-// Moves of the cache's pages.  The tables are small and every decision (which page is free, who shares what) depends on all of them, so one
-// block makes it, with prefix sums instead of counters, and later launches copy what it has listed.
+// Moves of the cache's pages.  Every decision (which page is free, who shares what) depends on all of the small tables, so a block makes it
+// alone, with prefix sums instead of counters.  Where pages are copied, all blocks of a launch make the same decisions, each copies its
+// share (into pages that are free: nobody minds, whatever comes after), and the block that finishes last, when nobody reads the tables any
+// more, writes them: one launch, and no block waits for another.
 #include "si_internal.h"
 #include "si_error.h"
 #include "kv_layout.h"
@@ -21,27 +23,18 @@ constexpr int COPY_THREADS = 256;
 constexpr int COPY_BYTES = 65536;     // of a page that a block copies
 
 // scratch of a cache
-struct Head { int32_t groups, used, pad[14]; };
-struct Group { int32_t src, first, count, pad; };  // one page that is copied, to dst[first] .. dst[first + count - 1]
+struct Head { uint32_t arrived; int32_t used, pad[14]; };  // arrived: 0 between calls
 struct Scratch {
   Head* head;
-  int32_t* mark;   // [n_seqs] 1: named by the running call; 0 between calls
-  Group* group;    // [SI_CACHE_MAX_LIST]
-  int32_t* dst;    // [SI_CACHE_MAX_LIST]
   int32_t* list;   // [n_pages] free pages; pages that move: holes
   int32_t* place;  // [n_pages] new number of a page
 };
 __host__ __device__ inline int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
-int64_t scratch_bytes(const si_cache_t& c) {
-  return sizeof(Head) + round16(4ll * c.n_seqs) + SI_CACHE_MAX_LIST * (sizeof(Group) + 4) + 2 * round16(4ll * c.n_pages);
-}
+int64_t scratch_bytes(const si_cache_t& c) { return sizeof(Head) + 2 * round16(4ll * c.n_pages); }
 Scratch scratch_of(const si_cache_t& c) {
   char* p = static_cast<char*>(c.scratch);
   Scratch s;
   s.head = reinterpret_cast<Head*>(p); p += sizeof(Head);
-  s.mark = reinterpret_cast<int32_t*>(p); p += round16(4ll * c.n_seqs);
-  s.group = reinterpret_cast<Group*>(p); p += SI_CACHE_MAX_LIST * sizeof(Group);
-  s.dst = reinterpret_cast<int32_t*>(p); p += SI_CACHE_MAX_LIST * 4;
   s.list = reinterpret_cast<int32_t*>(p); p += round16(4ll * c.n_pages);
   s.place = reinterpret_cast<int32_t*>(p);
   return s;
@@ -85,20 +78,20 @@ __device__ __forceinline__ int free_bits(const int32_t* refs, int n_pages, int a
   return bits;
 }
 
-// The first `need` free pages into `list`; returns how many there are, counted up to at least `need`
-__device__ int list_free(const si_cache_t& c, int need, int32_t* list, int (&w)[WAVES]) {
+// The first `need` free pages into `list`; returns how many there are, counted up to at least `need`.  bits: free_bits of the thread's first pages
+__device__ int list_free(const si_cache_t& c, int need, int bits, int32_t* list, int (&w)[WAVES]) {
   int found = 0;
   for (int at0 = 0; at0 < c.n_pages && found < need; at0 += BOOK * PER_THREAD) {
     const int at = at0 + threadIdx.x * PER_THREAD;
-    int bits = at < c.n_pages ? free_bits(c.refs, c.n_pages, at) : 0, total;
-    int rank = found + block_scan(__popc(bits), total, w);
+    if (at0 > 0) bits = at < c.n_pages ? free_bits(c.refs, c.n_pages, at) : 0;
+    int total, rank = found + block_scan(__popc(bits), total, w);
     for (; bits && rank < need; bits &= bits - 1, ++rank) list[rank] = at + __ffs(bits) - 1;
     found += total;
   }
   return found;
 }
 
-// largest e < n with prefix[e] <= f, entries that add nothing passed over (prefix[n] > f)
+// largest e < n with prefix[e] <= f (entries that add nothing are passed over, as prefix[n] > f)
 __device__ __forceinline__ int entry_of(const int* prefix, int n, int f) {
   int lo = 0, hi = n;
   while (hi - lo > 1) {
@@ -109,67 +102,114 @@ __device__ __forceinline__ int entry_of(const int* prefix, int n, int f) {
   return lo;
 }
 
-constexpr int LIST = SI_CACHE_MAX_LIST;
+static_assert(SI_CACHE_MAX_LIST == BOOK, "a thread for each entry of a list");
+constexpr int SHORT_LIST = 4096;  // free pages that are listed in LDS
 struct BookLds {
   int w[WAVES];
-  int seq[LIST], len[LIST];
-  int src[LIST];          // page that is copied for the entry, or -1
-  int need[LIST + 1];     // prefix sums: pages taken
-  int put[LIST + 1];      // tokens added (extend), pages named (fork)
-  int first[LIST];
-  int why;
+  int64_t w2[2][WAVES];
+  int seq[BOOK], len[BOOK];
+  int need[BOOK + 1];     // prefix sums: pages taken
+  int put[BOOK + 1];      // tokens added (extend), pages named (fork)
+  int src[BOOK];          // page that is copied for the entry, or -1
+  int first[BOOK];        // of the entries with this source
+  int g_src[BOOK], g_first[BOOK], g_count[BOOK];  // one source each, copied to dst[first] .. dst[first + count - 1]
+  int dst[BOOK];
+  int list[SHORT_LIST];
+  int groups, why;
+  uint32_t arrived;
 };
 
-// exclusive prefix sums of v[0 .. n) in place, v[n] = total; false (and v left as it may be) where a sum passes `most`
-__device__ bool prefix_list(int* v, int n, int most, int (&w)[WAVES]) {
-  int64_t carry = 0;
-  for (int e0 = 0; e0 < n; e0 += BOOK) {
-    const int e = e0 + threadIdx.x, x = e < n ? v[e] : 0;
-    // (every entry is at most `most`: cut so that a sum over the block stays in 31 bits, and look at the sum in 64)
-    int hi_total, lo_total;
-    const int hi = block_scan(x >> 12, hi_total, w), lo = block_scan(x & 0xfff, lo_total, w);
-    const int64_t at = carry + ((int64_t)hi << 12) + lo;
-    carry += ((int64_t)hi_total << 12) + lo_total;
-    if (carry > most) return false;
-    __syncthreads();
-    if (e < n) v[e] = (int)at;
+// s.need and s.put become the prefix sums of the entries' a and b, with the totals behind them; false where a total does not fit 31 bits
+__device__ bool prefix_lists(BookLds& s, int n, int a, int b) {
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  int64_t x = a, y = b;
+#pragma unroll
+  for (int d = 1; d < WAVE; d *= 2) {
+    const int64_t x2 = __shfl_up(x, d), y2 = __shfl_up(y, d);
+    if (lane >= d) { x += x2; y += y2; }
   }
-  if (threadIdx.x == 0) v[n] = (int)carry;
+  if (lane == WAVE - 1) { s.w2[0][wave] = x; s.w2[1][wave] = y; }
+  __syncthreads();
+  int64_t before_x = 0, before_y = 0, all_x = 0, all_y = 0;
+  for (int i = 0; i < WAVES; ++i) {
+    if (i < wave) { before_x += s.w2[0][i]; before_y += s.w2[1][i]; }
+    all_x += s.w2[0][i];
+    all_y += s.w2[1][i];
+  }
+  if (all_x > 0x7fffffff || all_y > 0x7fffffff) return false;
+  if ((int)threadIdx.x < n) { s.need[threadIdx.x] = (int)(before_x + x - a); s.put[threadIdx.x] = (int)(before_y + y - b); }
+  if (threadIdx.x == 0) { s.need[n] = (int)all_x; s.put[n] = (int)all_y; }
   __syncthreads();
   return true;
 }
 
-// Entries with the same source next to each other, so that a source is read once: s.src[e] is copied to the page that `dst(e)` names.
-template <class F> __device__ void list_copies(BookLds& s, int n, const Scratch& x, F dst) {
-  for (int e = threadIdx.x; e < n; e += BOOK) {
-    int f = e;
-    if (s.src[e] >= 0)
-      for (f = 0; s.src[f] != s.src[e]; ++f) {}
-    s.first[e] = s.src[e] >= 0 ? f : -1;
-  }
+// Number of entries i < end with v[i] == x
+__device__ __forceinline__ int equals(const int* v, int end, int x) {
+  int k = 0;
+  for (int i = 0; i < end; ++i) k += v[i] == x;
+  return k;
+}
+
+// Entries with the same source next to each other, so that a source is read once: s.src[e] is copied to `dst` of the thread's entry
+__device__ void list_copies(BookLds& s, int n, int dst) {
+  const int e = threadIdx.x, src = e < n ? s.src[e] : -1;
+  int f = e;
+  if (src >= 0)
+    for (f = 0; s.src[f] != src; ++f) {}
+  if (e < n) s.first[e] = src >= 0 ? f : -1;
+  if (e == 0) s.groups = 0;
   __syncthreads();
-  for (int e = threadIdx.x; e < n; e += BOOK) {
-    const int mine = s.first[e];
-    if (mine < 0) continue;
+  if (src >= 0) {
     int before = 0, rank = 0, count = 0, groups_before = 0;
     for (int i = 0; i < n; ++i) {
-      const int f = s.first[i];
-      before += f >= 0 && f < mine;
-      groups_before += f == i && f < mine;
-      count += f == mine;
-      rank += f == mine && i < e;
+      const int o = s.first[i];
+      before += o >= 0 && o < f;
+      groups_before += o == i && o < f;
+      count += o == f;
+      rank += o == f && i < e;
     }
-    x.dst[before + rank] = dst(e);
-    if (mine == e) x.group[groups_before] = Group{s.src[e], before, count, 0};
+    s.dst[before + rank] = dst;
+    if (f == e) {
+      s.g_src[groups_before] = src; s.g_first[groups_before] = before; s.g_count[groups_before] = count;
+      atomicAdd(&s.groups, 1);
+    }
   }
-  // the number of groups
-  int groups = 0, total = 0;
-  for (int e0 = 0; e0 < n; e0 += BOOK) {
-    const int e = e0 + threadIdx.x;
-    block_scan(e < n && s.first[e] == e, total, s.w);
-    groups += total;
+  __syncthreads();
+}
+
+// bytes [at, end) of one page to `count` others; `dst(i)` is the first byte of the i-th
+template <int THREADS, class F> __device__ __forceinline__ void copy_run(const char* src, int64_t at, int64_t end, int count, F dst) {
+  constexpr int STEP = THREADS * 16, N = 4;
+  for (at += threadIdx.x * 16; at < end; at += N * STEP) {
+    u32x4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (at + i * STEP < end) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + at + i * STEP));
+    for (int k = 0; k < count; ++k) {
+      char* to = dst(k);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (at + i * STEP < end) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(to + at + i * STEP));
+    }
   }
-  if (threadIdx.x == 0) x.head->groups = groups;
+}
+// this block's share of the listed copies
+__device__ void copy_share(const BookLds& s, char* pages, int64_t page_bytes, int parts) {
+  for (int64_t i = blockIdx.x; i < (int64_t)s.groups * parts; i += gridDim.x) {
+    const int q = (int)(i / parts), first = s.g_first[q];
+    const int64_t at = i % parts * COPY_BYTES;
+    copy_run<BOOK>(pages + s.g_src[q] * page_bytes, at, min(page_bytes, at + COPY_BYTES), s.g_count[q], [&](int k) { return pages + s.dst[first + k] * page_bytes; });
+  }
+}
+// the block that finishes last goes on
+__device__ bool last_block(BookLds& s, Head* head) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s.arrived = __hip_atomic_fetch_add(&head->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (s.arrived == gridDim.x - 1) __hip_atomic_store(&head->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return s.arrived == gridDim.x - 1;
 }
 
 __global__ __launch_bounds__(WAVE) void k_trim(si_cache_t c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ keep) {
@@ -203,89 +243,86 @@ struct ExtendArgs {
   Scratch x;
   const int32_t *seqs, *counts;
   int32_t *seq_out, *pos_out;
-  int n, n_new, capacity;
+  int n, n_new, capacity, parts;
+  int64_t page_bytes;
 };
 
 __global__ __launch_bounds__(BOOK) void k_extend(ExtendArgs g) {
   __shared__ BookLds s;
   const si_cache_t& c = g.c;
-  const int tid = threadIdx.x, page = c.page_tokens;
-  if (tid == 0) { s.why = 0; g.x.head->groups = 0; }
-  __syncthreads();
-  int why = 0;
-  for (int e = tid; e < g.n; e += BOOK) {
-    const int seq = g.seqs[e], m = g.counts ? g.counts[e] : g.n_new;
-    int len = 0, need = 0, src = -1;
+  const int e = threadIdx.x, page = c.page_tokens, n = g.n;
+  const int bits = e * PER_THREAD < c.n_pages ? free_bits(c.refs, c.n_pages, e * PER_THREAD) : 0;
+  if (e == 0) { s.why = 0; s.groups = 0; }
+  int why = 0, seq = -1, m = 0, len = 0, need = 0, src = -1, shared = 0;
+  if (e < n) {
+    seq = g.seqs[e];
+    m = g.counts ? g.counts[e] : g.n_new;
     if (seq < 0 || seq >= c.n_seqs) {
-      why |= SI_CACHE_BAD_SEQ;
+      why = SI_CACHE_BAD_SEQ;
     } else {
-      if (atomicExch(g.x.mark + seq, 1) != 0) why |= SI_CACHE_BAD_SEQ;
       len = c.lens[seq];
       if (len < 0 || m < 0 || (int64_t)len + m > (int64_t)c.max_pages * page) {
-        why |= SI_CACHE_BAD_LEN;
+        why = SI_CACHE_BAD_LEN;
       } else {
         need = ceil_div(len + m, page) - ceil_div(len, page);
         if (m > 0 && len % page > 0) {
           const int last = c.table[(int64_t)seq * c.max_pages + len / page];
-          if (last < 0 || last >= c.n_pages) why |= SI_CACHE_BAD_PAGE;
-          else if (c.refs[last] > 1) src = last;
+          if (last < 0 || last >= c.n_pages) why = SI_CACHE_BAD_PAGE;
+          else if ((shared = c.refs[last] - 1) > 0) src = last;
         }
       }
     }
-    s.seq[e] = seq; s.len[e] = len; s.need[e] = need; s.put[e] = max(m, 0); s.src[e] = src;
+    s.seq[e] = seq; s.len[e] = len; s.src[e] = src;
+  }
+  const bool some = __syncthreads_or(src >= 0);
+  if (e < n && equals(s.seq, e, seq) > 0) why |= SI_CACHE_BAD_SEQ;
+  if (some) {
+    // a shared last page: whoever comes after all of its other sharers keeps it
+    if (src >= 0 && equals(s.src, e, src) >= shared) src = -1;
+    __syncthreads();
+    if (e < n) s.src[e] = src;
+    need += src >= 0;
   }
   if (why) atomicOr(&s.why, why);
-  __syncthreads();
-  // a shared last page: whoever comes after all of its other sharers keeps it
-  for (int e = tid; e < g.n; e += BOOK) {
-    const int src = s.src[e];
-    int before = 0;
-    if (src >= 0) {
-      for (int i = 0; i < e; ++i) before += s.src[i] == src;
-    }
-    s.first[e] = src >= 0 && before < c.refs[src] - 1;
-  }
-  __syncthreads();
-  for (int e = tid; e < g.n; e += BOOK) {
-    if (s.first[e]) s.need[e] += 1;
-    else s.src[e] = -1;
-  }
-  __syncthreads();
-  bool ok = s.why == 0;
-  int tokens = 0, pages = 0;
-  if (ok && !prefix_list(s.put, g.n, 0x7fffffff, s.w)) { ok = false; why = SI_CACHE_NO_ROOM; }
-  if (ok && !prefix_list(s.need, g.n, 0x7fffffff, s.w)) { ok = false; why = SI_CACHE_NO_PAGES; }
+  bool ok = prefix_lists(s, n, need, why ? 0 : m);
+  why = ok ? 0 : SI_CACHE_NO_ROOM;
+  ok = ok && s.why == 0;
+  int pages = 0, tokens = 0;
+  int32_t* list = s.list;
   if (ok) {
-    tokens = s.put[g.n];
-    pages = s.need[g.n];
+    pages = s.need[n];
+    tokens = s.put[n];
+    if (pages > SHORT_LIST) list = g.x.list;  // (every block writes the same)
     if (g.seq_out && tokens > g.capacity) { ok = false; why = SI_CACHE_NO_ROOM; }
-    else if (pages > 0 && list_free(c, pages, g.x.list, s.w) < pages) { ok = false; why = SI_CACHE_NO_PAGES; }
+    else if (pages > 0 && list_free(c, pages, bits, list, s.w) < pages) { ok = false; why = SI_CACHE_NO_PAGES; }
   }
   __syncthreads();
+  if (ok && some) {
+    list_copies(s, n, e < n ? list[min(s.need[e], pages - 1)] : 0);
+    copy_share(s, static_cast<char*>(c.pages), g.page_bytes, g.parts);
+  }
+  if (!last_block(s, g.x.head)) return;
   if (ok) {
-    for (int f = tid; f < pages; f += BOOK) {
-      const int e = entry_of(s.need, g.n, f), k = f - s.need[e], p = g.x.list[f];
-      const int j = s.src[e] >= 0 ? s.len[e] / page + k : ceil_div(s.len[e], page) + k;
-      c.table[(int64_t)s.seq[e] * c.max_pages + j] = p;
+    for (int f = e; f < pages; f += BOOK) {
+      const int i = entry_of(s.need, n, f), k = f - s.need[i], p = list[f];
+      const int j = s.src[i] >= 0 ? s.len[i] / page + k : ceil_div(s.len[i], page) + k;
+      c.table[(int64_t)s.seq[i] * c.max_pages + j] = p;
       c.refs[p] = 1;
-      if (s.src[e] >= 0 && k == 0) atomicSub(c.refs + s.src[e], 1);
+      if (s.src[i] >= 0 && k == 0) atomicSub(c.refs + s.src[i], 1);
     }
-    for (int e = tid; e < g.n; e += BOOK) c.lens[s.seq[e]] = s.len[e] + s.put[e + 1] - s.put[e];
-    list_copies(s, g.n, g.x, [&](int e) { return g.x.list[s.need[e]]; });
-  } else if (tid == 0) {
+    if (e < n) c.lens[seq] = len + m;
+  } else if (e == 0) {
     atomicOr(c.status, why | s.why);
   }
-  for (int e = tid; e < g.n; e += BOOK)
-    if (s.seq[e] >= 0 && s.seq[e] < c.n_seqs) g.x.mark[s.seq[e]] = 0;
   if (g.seq_out)
-    for (int f = tid; f < g.capacity; f += BOOK) {
-      int seq = -1, pos = -1;
+    for (int f = e; f < g.capacity; f += BOOK) {
+      int to = -1, pos = -1;
       if (f < tokens && ok) {
-        const int e = g.counts ? entry_of(s.put, g.n, f) : f / g.n_new;
-        seq = s.seq[e];
-        pos = s.len[e] + f - s.put[e];
+        const int i = g.counts ? entry_of(s.put, n, f) : f / g.n_new;
+        to = s.seq[i];
+        pos = s.len[i] + f - s.put[i];
       }
-      g.seq_out[f] = seq;
+      g.seq_out[f] = to;
       g.pos_out[f] = pos;
     }
 }
@@ -294,107 +331,83 @@ struct ForkArgs {
   si_cache_t c;
   Scratch x;
   const int32_t *parents, *children;
-  int n;
+  int n, parts;
+  int64_t page_bytes;
 };
 
 __global__ __launch_bounds__(BOOK) void k_fork(ForkArgs g) {
   __shared__ BookLds s;  // seq: child, len: parent's, put: pages of the parent
   const si_cache_t& c = g.c;
-  const int tid = threadIdx.x, page = c.page_tokens;
-  if (tid == 0) { s.why = 0; g.x.head->groups = 0; }
-  __syncthreads();
-  int why = 0;
-  for (int e = tid; e < g.n; e += BOOK) {
-    const int a = g.parents[e], b = g.children[e];
-    if (a < 0 || a >= c.n_seqs || b < 0 || b >= c.n_seqs || atomicExch(g.x.mark + b, 1) != 0) why = SI_CACHE_BAD_SEQ;
-    s.seq[e] = b; s.first[e] = a;
-  }
-  if (why) atomicOr(&s.why, why);
-  __syncthreads();
-  // Sequence numbers, then lengths: each is looked at only where what came before is in order, which is the same for all threads
-  auto step = [&](auto&& look) {
-    const bool go_on = s.why == 0;
-    why = 0;
-    if (go_on)
-      for (int e = tid; e < g.n; e += BOOK) look(e);
-    __syncthreads();
-    if (why) atomicOr(&s.why, why);
-    __syncthreads();
-  };
-  step([&](int e) {
-    if (__hip_atomic_load(g.x.mark + s.first[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0) why |= SI_CACHE_BAD_SEQ;  // a parent that is a child
-  });
-  step([&](int e) {
-    int len = c.lens[s.first[e]];
-    if (c.lens[s.seq[e]] != 0 || len < 0 || len > c.max_pages * page) { why |= SI_CACHE_BAD_LEN; len = 0; }
-    s.len[e] = len; s.put[e] = ceil_div(len, page); s.need[e] = len % page > 0; s.src[e] = -1;
-  });
-  bool ok = s.why == 0;
-  int pages = 0, named = 0;
-  if (ok && !(prefix_list(s.put, g.n, 0x7fffffff, s.w) && prefix_list(s.need, g.n, 0x7fffffff, s.w))) { ok = false; why = SI_CACHE_NO_PAGES; }
-  if (ok) {
-    named = s.put[g.n];
-    pages = s.need[g.n];
-    why = 0;
-    for (int f = tid; f < named; f += BOOK) {
-      const int e = entry_of(s.put, g.n, f), j = f - s.put[e], p = c.table[(int64_t)s.first[e] * c.max_pages + j];
-      if (p < 0 || p >= c.n_pages) why |= SI_CACHE_BAD_PAGE;
-      else if (j == s.len[e] / page) s.src[e] = p;
-    }
-    if (why) atomicOr(&s.why, why);
-    __syncthreads();
-    ok = s.why == 0;
-    if (ok && pages > 0 && list_free(c, pages, g.x.list, s.w) < pages) { ok = false; why = SI_CACHE_NO_PAGES; }
-  }
-  __syncthreads();
-  if (ok) {
-    for (int f = tid; f < named; f += BOOK) {
-      const int e = entry_of(s.put, g.n, f), j = f - s.put[e];
-      int p;
-      if (j == s.len[e] / page) {
-        p = g.x.list[s.need[e]];
-        c.refs[p] = 1;
-      } else {
-        p = c.table[(int64_t)s.first[e] * c.max_pages + j];
-        atomicAdd(c.refs + p, 1);
+  const int e = threadIdx.x, page = c.page_tokens, n = g.n;
+  const int bits = e * PER_THREAD < c.n_pages ? free_bits(c.refs, c.n_pages, e * PER_THREAD) : 0;
+  if (e == 0) { s.why = 0; s.groups = 0; }
+  int bad_seq = 0, bad_len = 0, bad_page = 0, a = -1, b = -1, len = 0, src = -1;
+  if (e < n) {
+    a = g.parents[e];
+    b = g.children[e];
+    bad_seq = a < 0 || a >= c.n_seqs || b < 0 || b >= c.n_seqs;
+    if (!bad_seq) {
+      len = c.lens[a];
+      bad_len = c.lens[b] != 0 || len < 0 || len > c.max_pages * page;
+      if (!bad_len && len % page > 0) {
+        src = c.table[(int64_t)a * c.max_pages + len / page];
+        bad_page = src < 0 || src >= c.n_pages;
       }
-      c.table[(int64_t)s.seq[e] * c.max_pages + j] = p;
+      if (bad_len || bad_page) { len = 0; src = -1; }
     }
-    for (int e = tid; e < g.n; e += BOOK) c.lens[s.seq[e]] = s.len[e];
-    __syncthreads();  // (first[] is used anew)
-    list_copies(s, g.n, g.x, [&](int e) { return g.x.list[s.need[e]]; });
-  } else if (tid == 0) {
-    atomicOr(c.status, why | s.why);
+    s.seq[e] = b; s.len[e] = len; s.src[e] = src;
   }
   __syncthreads();
-  for (int e = tid; e < g.n; e += BOOK)
-    if (s.seq[e] >= 0 && s.seq[e] < c.n_seqs) g.x.mark[s.seq[e]] = 0;
-}
-
-// bytes [at, end) of one page to `count` others; `dst(i)` is the first byte of the i-th
-template <class F> __device__ __forceinline__ void copy_run(const char* src, int64_t at, int64_t end, int count, F dst) {
-  constexpr int STEP = COPY_THREADS * 16, N = 4;
-  for (at += threadIdx.x * 16; at < end; at += N * STEP) {
-    u32x4 v[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (at + i * STEP < end) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + at + i * STEP));
-    for (int k = 0; k < count; ++k) {
-      char* to = dst(k);
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (at + i * STEP < end) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(to + at + i * STEP));
+  if (e < n && !bad_seq) bad_seq = equals(s.seq, e, b) > 0 || equals(s.seq, n, a) > 0;  // named twice, or parent and child
+  bad_seq = __syncthreads_or(bad_seq);
+  bad_len = __syncthreads_or(bad_len);
+  bad_page = __syncthreads_or(bad_page);
+  // (sequence numbers, then lengths, then pages: each counts only where what comes before is in order)
+  int why = bad_seq ? SI_CACHE_BAD_SEQ : bad_len ? SI_CACHE_BAD_LEN : bad_page ? SI_CACHE_BAD_PAGE : 0;
+  bool ok = why == 0;
+  int32_t* list = s.list;  // (at most one page an entry)
+  int pages = 0, named = 0;
+  if (ok) {
+    if (e < n) s.first[e] = a;
+    ok = prefix_lists(s, n, src >= 0, ceil_div(len, page));
+    why = SI_CACHE_NO_PAGES;
+  }
+  if (ok) {
+    pages = s.need[n];
+    named = s.put[n];
+    for (int f = e; f < named; f += BOOK) {
+      const int i = entry_of(s.put, n, f), p = c.table[(int64_t)s.first[i] * c.max_pages + f - s.put[i]];
+      if (p < 0 || p >= c.n_pages) bad_page = 1;
     }
+    bad_page = __syncthreads_or(bad_page);
+    if (bad_page) why = SI_CACHE_BAD_PAGE;
+    ok = !bad_page && (pages == 0 || list_free(c, pages, bits, list, s.w) >= pages);
   }
-}
-
-// grid: parts of a page x groups (any number of blocks along them)
-__global__ __launch_bounds__(COPY_THREADS) void k_copy_groups(char* pages, int64_t page_bytes, Scratch x) {
-  const int64_t at = (int64_t)blockIdx.x * COPY_BYTES, end = min(page_bytes, at + COPY_BYTES);
-  for (int i = blockIdx.y; i < x.head->groups; i += gridDim.y) {
-    const Group q = x.group[i];
-    copy_run(pages + q.src * page_bytes, at, end, q.count, [&](int k) { return pages + x.dst[q.first + k] * page_bytes; });
+  __syncthreads();
+  if (ok && pages > 0) {
+    list_copies(s, n, e < n ? list[min(s.need[e], pages - 1)] : 0);
+    copy_share(s, static_cast<char*>(c.pages), g.page_bytes, g.parts);
   }
+  if (!last_block(s, g.x.head)) return;
+  if (!ok) {
+    if (e == 0) atomicOr(c.status, why);
+    return;
+  }
+  if (e < n) s.first[e] = a;  // (list_copies has had it)
+  __syncthreads();
+  for (int f = e; f < named; f += BOOK) {
+    const int i = entry_of(s.put, n, f), j = f - s.put[i];
+    int p;
+    if (j == s.len[i] / page) {
+      p = list[s.need[i]];
+      c.refs[p] = 1;
+    } else {
+      p = c.table[(int64_t)s.first[i] * c.max_pages + j];
+      atomicAdd(c.refs + p, 1);
+    }
+    c.table[(int64_t)s.seq[i] * c.max_pages + j] = p;
+  }
+  if (e < n) c.lens[b] = len;
 }
 
 __global__ __launch_bounds__(BOOK) void k_places(si_cache_t c, Scratch x, int room, int32_t* n_used) {
@@ -445,7 +458,7 @@ __global__ __launch_bounds__(COPY_THREADS) void k_compact(CompactArgs g) {
     if (place < 0 || (place == p && g.to.pages == g.c.pages)) return;
     const int64_t at = (int64_t)(blockIdx.x % g.parts) * COPY_BYTES;
     char* to = static_cast<char*>(g.to.pages) + place * page_bytes;
-    copy_run(static_cast<const char*>(g.c.pages) + p * page_bytes, at, min(page_bytes, at + COPY_BYTES), 1, [&](int) { return to; });
+    copy_run<COPY_THREADS>(static_cast<const char*>(g.c.pages) + p * page_bytes, at, min(page_bytes, at + COPY_BYTES), 1, [&](int) { return to; });
     return;
   }
   const int64_t first = (blockIdx.x - g.copy_blocks) * COPY_THREADS + threadIdx.x, step = (gridDim.x - g.copy_blocks) * COPY_THREADS;
@@ -487,10 +500,8 @@ int done(const char* who) {
 int64_t page_bytes(const si_cache_t& c) { return kv_page_elems(c) * kv_elem_bytes(c.type); }
 int parts_of(const si_cache_t& c) { return (int)((page_bytes(c) + COPY_BYTES - 1) / COPY_BYTES); }
 
-void copy_groups(const si_cache_t& c, const Scratch& x, int n, hipStream_t stream) {
-  const int parts = parts_of(c);
-  hipLaunchKernelGGL(k_copy_groups, dim3(parts, std::max(1, std::min(n, 4096 / std::min(parts, 4096)))), dim3(COPY_THREADS), 0, stream, static_cast<char*>(c.pages), page_bytes(c), x);
-}
+// Blocks of a launch that may copy a page for each of n entries: a compute unit each, unless the pages are small
+int copy_blocks(const si_cache_t& c, int n) { return (int)std::max<int64_t>(1, std::min<int64_t>(256, (int64_t)n * parts_of(c))); }
 
 }  // namespace
 }  // namespace si
@@ -520,10 +531,8 @@ extern "C" int si_cache_extend(const si_cache_t* c, const int32_t* seqs, int32_t
   if ((seq_out == nullptr) != (pos_out == nullptr) || misaligned(seq_out, 4) || misaligned(pos_out, 4)) return set_error(SI_EINVAL, "%s: one of seq_out and pos_out is NULL, or misaligned", who);
   if (capacity < 0) return set_error(SI_EINVAL, "%s: capacity %d", who, capacity);
   if (n == 0) return SI_OK;
-  ExtendArgs g{*c, scratch_of(*c), seqs, counts, seq_out, pos_out, n, n_new, capacity};
-  hipLaunchKernelGGL(k_extend, dim3(1), dim3(BOOK), 0, (hipStream_t)stream, g);
-  if (int rc = done(who)) return rc;
-  copy_groups(*c, g.x, n, (hipStream_t)stream);
+  ExtendArgs g{*c, scratch_of(*c), seqs, counts, seq_out, pos_out, n, n_new, capacity, parts_of(*c), page_bytes(*c)};
+  hipLaunchKernelGGL(k_extend, dim3(std::min(64, copy_blocks(*c, n))), dim3(BOOK), 0, (hipStream_t)stream, g);
   return done(who);
 }
 
@@ -532,10 +541,8 @@ extern "C" int si_cache_fork(const si_cache_t* c, const int32_t* parents, const 
   if (int rc = check_moves(c, who)) return rc;
   if (int rc = check_list(parents, children, true, n, who)) return rc;
   if (n == 0) return SI_OK;
-  ForkArgs g{*c, scratch_of(*c), parents, children, n};
-  hipLaunchKernelGGL(k_fork, dim3(1), dim3(BOOK), 0, (hipStream_t)stream, g);
-  if (int rc = done(who)) return rc;
-  copy_groups(*c, g.x, n, (hipStream_t)stream);
+  ForkArgs g{*c, scratch_of(*c), parents, children, n, parts_of(*c), page_bytes(*c)};
+  hipLaunchKernelGGL(k_fork, dim3(copy_blocks(*c, n)), dim3(BOOK), 0, (hipStream_t)stream, g);
   return done(who);
 }
 
