@@ -246,9 +246,10 @@ template <int TYPE, int D, int TILES> struct Attend {
     // writes its rows.
     auto blocks_of = [&](int k) { return (int64_t)max(1, Span(g, k, t0, t1, B).nb); };
     const int mine = (n + THREADS - 1) / THREADS, k0 = min(n, (int)threadIdx.x * mine), k1 = min(n, k0 + mine);  // sequences that a thread counts
-    int64_t total = 0, before = 0, counted = 0;
+    int64_t total, before = 0, counted = 0;
+    Span sp(g, 0, t0, t1, B);
     if (n == 1) {
-      total = blocks_of(0);
+      total = max(1, sp.nb);
     } else {
       for (int k = k0; k < k1; ++k) counted += blocks_of(k);
       total = scan(counted, before, s);
@@ -259,7 +260,11 @@ template <int TYPE, int D, int TILES> struct Attend {
     auto slice_end = [&](int w) { return quotient((w + 1) * total, G); };
     auto slice_of = [&](int64_t block) { return (int)quotient((block + 1) * G - 1, total); };  // the one whose end is the first beyond the block
     int i = 0;
-    int64_t begin = slice_end(slice - 1), left = slice < G ? slice_end(slice) - begin : 0;
+    int64_t begin = 0, left = total;
+    if (g.slices > 1) {
+      begin = slice_end(slice - 1);
+      left = slice < G ? slice_end(slice) - begin : 0;
+    }
     if (n > 1) {
       if (before <= begin && begin < before + counted)
         for (int k = k0; k < k1; ++k) {
@@ -274,7 +279,7 @@ template <int TYPE, int D, int TILES> struct Attend {
     // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
     int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
     for (; left > 0; ++i) {
-      const Span sp(g, i, t0, t1, B);
+      if (n > 1) sp = Span(g, i, t0, t1, B);
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
       part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
