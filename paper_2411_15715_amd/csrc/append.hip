@@ -25,6 +25,7 @@ struct Args {
   int qk_columns;   // blocks of the q / k part along the units of a token
   int v_columns;    // blocks of the v part along its columns
   int v_blocks;     // and in all
+  int run;          // blocks of the q / k part that follow each other on one die
 };
 
 __device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
@@ -269,25 +270,36 @@ template <int TYPE> __device__ void v_part(const Args& g, int block) {
   }
 }
 
+// Blocks go to the 8 dies in turn.  A line of a K block holds 16 bytes of eight tokens: the runs of blocks that have 32 neighbouring tokens go to one die,
+// whose cache puts the pieces together (else all dies write pieces of the same lines)
+__device__ __forceinline__ int on_one_die(int b, int blocks, int run) {
+  const int all = blocks / (8 * run) * (8 * run);
+  if (b >= all) return b;  // (what is left over stays in order)
+  const int die = b % 8, i = b / 8;
+  return (i / run * 8 + die) * run + i % run;
+}
+
 template <int TYPE> __global__ __launch_bounds__(THREADS) void k_append(Args g) {
   // (v first: its blocks have the longer way from load to store)
   if ((int)blockIdx.x < g.v_blocks) v_part<TYPE>(g, blockIdx.x);
-  else qk_part<TYPE>(g, blockIdx.x - g.v_blocks);
+  else qk_part<TYPE>(g, on_one_die(blockIdx.x - g.v_blocks, gridDim.x - g.v_blocks, g.run));
 }
 
 bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 hipError_t launch_append(const si_cache_t& c, int layer, const si_append_t& a, hipStream_t stream) {
-  Args g{c, a, layer, 1, 1, 0, 0};
+  Args g{c, a, layer, 1, 1, 0, 0, 1};
   const int per_head = a.rot_dim % 16 == 0 ? c.head_dim / 16 : c.head_dim - a.rot_dim / 2, units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * per_head;
   // A block has up to four units a thread, of one token or of up to 4 where these have few (4099 tokens of 576 units: 51 us with the angles formed
-  // by two blocks of a token, 39 by one); with few tokens one unit a thread (what waits there is memory, not the threads)
-  const int want = THREADS * (a.n_tokens >= 256 ? 4 : 1);
+  // by two blocks of a token, 39 by one); with few tokens, or pairs
+  // taken one by one, one unit a thread (what waits there is memory, not the threads)
+  const int want = THREADS * (a.n_tokens >= 256 && a.rot_dim % 16 == 0 ? 4 : 1);
   if (units >= want) g.qk_columns = (units + want - 1) / want;
   else if (a.n_tokens >= 256) g.per_block = std::min(MAX_TOKENS, want / units);
   const int E = kv_vec(c.type);
   g.v_columns = (c.n_kv_heads * c.head_dim + THREADS - 1) / THREADS;
   g.v_blocks = (a.n_tokens + E - 1) / E * g.v_columns;
+  g.run = 32 / g.per_block * g.qk_columns;
   const int64_t blocks = (int64_t)((a.n_tokens + g.per_block - 1) / g.per_block) * g.qk_columns + g.v_blocks;
   if (c.type == SI_KV_BF16) hipLaunchKernelGGL(k_append<SI_KV_BF16>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
   else hipLaunchKernelGGL(k_append<SI_KV_E4M3>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
