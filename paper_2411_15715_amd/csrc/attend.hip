@@ -10,7 +10,7 @@ namespace si {
 namespace {
 
 struct Cut {
-  int tiles, groups, slices, part_rows, last_joins;
+  int tiles, groups, slices, whole, part_rows, last_joins;
   int64_t scratch, parted_at, part_at;
 };
 
@@ -27,15 +27,17 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   // As many blocks as there are compute units; twice that where a slice holds several sequences (the next one's first loads have nothing beside
   // them: 512 sequences of 64 positions 57 -> 38 us) or the waves of a block share their loads and wait for each other (40 rows over
   // 16 x 8000 positions 119 -> 106 us) and two blocks fit a unit.  Else it is one more round of sums to write and read (131071 positions 86
-  // against 88 us).  Joining costs as much as five cache blocks a wave (517 positions, 17 blocks over 4 waves: 9.4 us whole, 10.4 in two
-  // slices); beyond, no slice has fewer than two a wave.
+  // against 88 us).  No slice has fewer than two cache blocks a wave.
+  // Short sequences have a block each, without a search and without joining (8 of 517 positions, 17 cache blocks: 15.2 us in slices, 10.3
+  // whole; 15 of 525 .. 1051 e4m3, 30 rows 28.7 and 22.3); a longer one alone is better cut (1000 positions 9.4 us, whole 12.0).  Where there
+  // are many, longer ones even out too (128 of 1 .. 1000 positions 54 us in slices, 51 whole).
   const bool twice = c.head_dim <= 128 && (k.tiles > 1 || a.n * units > 256);
   const int most = twice ? 512 : 256, streams = ATTEND_WAVES / k.tiles;
-  const int64_t least = each <= 5 * streams ? each : 2 * streams;
-  k.slices = (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + least - 1) / least));
+  k.whole = each <= 20 || (each <= 40 && a.n * units >= 512);
+  k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + 2 * streams - 1) / (2 * streams)));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
-  k.last_joins = k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
-  if (k.slices > 1) {
+  k.last_joins = !k.whole && k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
+  if (!k.whole && k.slices > 1) {
     k.parted_at = ATTEND_COUNTERS * 4;
     k.part_at = k.parted_at + (a.n * units * 8 + 15) / 16 * 16;
     k.scratch = k.part_at + units * k.slices * 2 * k.part_rows * (c.head_dim + 2) * 4;
@@ -84,7 +86,7 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
   if (a->n == 0) return SI_OK;
-  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.slices, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
+  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.slices, k.whole, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
   g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
   if (k.scratch > 0) {
     char* p = static_cast<char*>(a->scratch);

@@ -34,6 +34,7 @@ struct AttendArgs {
   int groups;     // row groups: blocks that share a kv head
   int tiles;      // waves of a block that share a stream of cache blocks, each with 16 rows of its own: 1, 2 or 4
   int slices;     // G
+  int whole;      // a slice for each sequence instead (short ones: nothing to even out, nothing to join)
   int part_rows;  // rows of a unit that the scratch has room for: min(rows, 16 tiles)
   int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
   float scale2;   // scale * log2(e)
@@ -164,12 +165,13 @@ template <int TYPE, int D, int TILES> struct Attend {
   static constexpr int H = E / 8;                                             // operands of 8 elements in 16 bytes
   static constexpr int WAVES = ATTEND_WAVES, THREADS = ATTEND_THREADS;
   static constexpr int PAD = D + 4;                                           // (rows of 16 banks more: the four groups of lanes write side by side)
-  // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
-  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256 a wave has a SIMD for itself.
-  static constexpr int WAVES_PER_SIMD = D < 256 ? 2 : 1;
 
   static constexpr int STREAMS = WAVES / TILES, BLOCK_BYTES = 128 * D, STAGE = STREAMS * BLOCK_BYTES;
   static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;  // (two blocks a compute unit, where heads are no longer than 128)
+  // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
+  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256, or where LDS
+  // has no room for two blocks, a wave has a SIMD for itself.
+  static constexpr int WAVES_PER_SIMD = D < 256 && (!SHARED || S * STAGE <= 80 * 1024) ? 2 : 1;
   static constexpr int PIECES = STAGE / 1024 / WAVES;                  // loads of a stage by each wave
 
   struct Lds {
@@ -247,8 +249,9 @@ template <int TYPE, int D, int TILES> struct Attend {
     auto blocks_of = [&](int k) { return (int64_t)max(1, Span(g, k, t0, t1, B).nb); };
     const int mine = (n + THREADS - 1) / THREADS, k0 = min(n, (int)threadIdx.x * mine), k1 = min(n, k0 + mine);  // sequences that a thread counts
     int64_t total, before = 0, counted = 0;
-    Span sp(g, 0, t0, t1, B);
-    if (n == 1) {
+    int i = g.whole ? slice : 0;
+    Span sp(g, i, t0, t1, B);
+    if (n == 1 || g.whole) {
       total = max(1, sp.nb);
     } else {
       for (int k = k0; k < k1; ++k) counted += blocks_of(k);
@@ -259,13 +262,12 @@ template <int TYPE, int D, int TILES> struct Attend {
     auto quotient = [](int64_t x, int64_t y) { return (int64_t)((double)x / (double)y); };
     auto slice_end = [&](int w) { return quotient((w + 1) * total, G); };
     auto slice_of = [&](int64_t block) { return (int)quotient((block + 1) * G - 1, total); };  // the one whose end is the first beyond the block
-    int i = 0;
     int64_t begin = 0, left = total;
-    if (g.slices > 1) {
+    if (g.slices > 1 && !g.whole) {
       begin = slice_end(slice - 1);
       left = slice < G ? slice_end(slice) - begin : 0;
     }
-    if (n > 1) {
+    if (n > 1 && !g.whole) {
       if (before <= begin && begin < before + counted)
         for (int k = k0; k < k1; ++k) {
           const int64_t nb = blocks_of(k);
@@ -279,11 +281,11 @@ template <int TYPE, int D, int TILES> struct Attend {
     // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
     int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
     for (; left > 0; ++i) {
-      if (n > 1) sp = Span(g, i, t0, t1, B);
+      if (n > 1 && !g.whole) sp = Span(g, i, t0, t1, B);
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
       part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
-      if (g.slices > 1) {
+      if (g.slices > 1 && !g.whole) {
         const int64_t first_block = slice_end(slice) - left - off;
         const int first = where_to < 0 ? slice : slice_of(first_block), parts = where_to < 0 ? 1 : slice_of(first_block + nb - 1) - first + 1;
         if (where_to == 0) { un_seq[0] = i; un_first[0] = first; un_parts[0] = parts; }
@@ -657,7 +659,7 @@ template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t st
   if (g.tiles == 1) hipLaunchKernelGGL((k_attend<TYPE, D, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.tiles == 2) hipLaunchKernelGGL((k_attend<TYPE, D, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else hipLaunchKernelGGL((k_attend<TYPE, D, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  if (g.slices > 1 && !g.last_joins) {
+  if (g.slices > 1 && !g.whole && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_join<D>, dim3(grid.x, g.a.n, g.part_rows), dim3(256), 0, stream, g);
