@@ -10,17 +10,17 @@ namespace si {
 namespace {
 
 struct Cut {
-  int tiles, groups, slices, whole, part_rows, last_joins;
+  int block_rows, groups, slices, whole, part_rows, last_joins;
   int64_t scratch, parted_at, part_at;
 };
 
-// Waves of a block that share cache blocks, row groups, and the slices that a kv head's cache blocks are cut into.
+// Rows of a block, row groups, and the slices that a kv head's cache blocks are cut into.
 Cut cut(const si_cache_t& c, const si_attend_t& a) {
   Cut k{};
-  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), tiles = (rows + 15) / 16, B = kv_block(c.type);
-  for (k.tiles = 1; k.tiles < tiles && k.tiles < ATTEND_WAVES;) k.tiles *= 2;
-  k.groups = (tiles + k.tiles - 1) / k.tiles;
-  k.part_rows = std::min(rows, 16 * k.tiles);
+  const int rows = a.n_new * (a.n_heads / c.n_kv_heads), B = kv_block(c.type);
+  for (k.block_rows = 16; k.block_rows < rows && k.block_rows < 128;) k.block_rows *= 2;
+  k.groups = (rows + k.block_rows - 1) / k.block_rows;
+  k.part_rows = std::min(rows, k.block_rows);
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
   const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B), units = (int64_t)c.n_kv_heads * k.groups;
@@ -31,8 +31,8 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   // Short sequences have a block each, without a search and without joining (8 of 517 positions, 17 cache blocks: 15.2 us in slices, 10.3
   // whole; 15 of 525 .. 1051 e4m3, 30 rows 28.7 and 22.3); a longer one alone is better cut (1000 positions 9.4 us, whole 12.0).  Where there
   // are many, longer ones even out too (128 of 1 .. 1000 positions 54 us in slices, 51 whole).
-  const bool twice = c.head_dim <= 128 && (k.tiles > 1 || a.n * units > 256);
-  const int most = twice ? 512 : 256, streams = ATTEND_WAVES / k.tiles;
+  const bool twice = c.head_dim <= 128 && (k.block_rows > 16 || a.n * units > 256);
+  const int most = twice ? 512 : 256, streams = std::max(1, 64 / k.block_rows);
   k.whole = each <= 20 || (each <= 40 && a.n * units >= 512);
   k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + 2 * streams - 1) / (2 * streams)));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
@@ -86,7 +86,7 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
   if (a->n == 0) return SI_OK;
-  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.tiles, k.slices, k.whole, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
+  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.block_rows, k.slices, k.whole, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
   g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
   if (k.scratch > 0) {
     char* p = static_cast<char*>(a->scratch);

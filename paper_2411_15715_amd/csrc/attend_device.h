@@ -1,6 +1,6 @@
 // Attention of a few new tokens over the paged cache: the kernel (hipcc only; instantiated by attend_bf16.hip and attend_e4m3.hip).
 //
-// The rows of a block are the query heads that share a kv head, for all new tokens: up to 16 NT of them.  Per cache block of
+// The rows of a block are the query heads that share a kv head, for all new tokens: up to 128 of them.  Per cache block of
 // B tokens a wave forms S^T = K Q^T (matrix instructions with K as the left operand) and O^T += V^T P^T.  The cache holds K and V in the
 // operand order of these instructions, so a wave loads both from memory into the registers that multiply, 16 bytes a lane and
 // 1 KB in a run; and the tokens of a K block are placed so that the scores a lane receives are those of the
@@ -32,10 +32,10 @@ struct AttendArgs {
   int layer;
   int rows;       // rows of a unit in all: n_new * heads per kv head
   int groups;     // row groups: blocks that share a kv head
-  int tiles;      // waves of a block that share a stream of cache blocks, each with 16 rows of its own: 1, 2 or 4
+  int block_rows; // rows of a block: 16, 32, 64 or 128
   int slices;     // G
   int whole;      // a slice for each sequence instead (short ones: nothing to even out, nothing to join)
-  int part_rows;  // rows of a unit that the scratch has room for: min(rows, 16 tiles)
+  int part_rows;  // rows of a unit that the scratch has room for: min(rows, block_rows)
   int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
   float scale2;   // scale * log2(e)
   uint32_t* count;  // [ATTEND_COUNTERS], of (sequence, unit); 0 between calls
@@ -154,33 +154,39 @@ __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv
 // s_waitcnt vmcnt(n) alone, n < 64
 template <int N> __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 0xf) | (((N >> 4) & 3) << 14)); }
 
-// TILES waves of a block have 16 rows each and go through the same cache blocks; 4 / TILES streams of them take these in turn.  Alone (TILES == 1)
-// a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97).  Several read them from LDS, into
-// which the block loads each cache block once, without a detour through registers: S stages of a block for each stream.  (Each
+// TILES waves of a block have 16 NT rows each and go through the same cache blocks; 4 / TILES streams of them take these in turn.  Alone
+// (TILES == 1) a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97).  Several read them from LDS,
+// into which the block loads each cache block once, without a detour through registers: S stages of a block for each stream.  (Each
 // wave loading for itself, TILES requests for every line at the caches: 24 rows over 16 x 8000 positions 108 us, this way 97.)
-template <int TYPE, int D, int TILES> struct Attend {
-  static constexpr bool SHARED = TILES > 1;
+// From 65 rows on a wave has 32 (96 rows over 16 x 8000 positions in two blocks of 64: 196 us, in one of 128: 136), with fewer 16: two waves with the
+// same cache block hide each other's waits (20 rows of e4m3 over 29 windows of 9000 positions, 32 a wave and a ring for each wave: 113 us, 16: 91).
+template <int TYPE, int D, int NT, int TILES> struct Attend {
+  static constexpr int ROWS = 16 * NT, BLOCK_ROWS = ROWS * TILES;              // of a wave, of a block
+  static constexpr bool RING = TILES > 1;                                     // K and V come by way of LDS
   static constexpr int E = TYPE == SI_KV_E4M3 ? 16 : 8, B = 4 * E, J = E / 4;  // J score tiles of 16 tokens
   static constexpr int NL = D / 16;                                           // loads of 16 bytes of K, and of V, a lane and block
   static constexpr int H = E / 8;                                             // operands of 8 elements in 16 bytes
   static constexpr int WAVES = ATTEND_WAVES, THREADS = ATTEND_THREADS;
   static constexpr int PAD = D + 4;                                           // (rows of 16 banks more: the four groups of lanes write side by side)
 
+  // A stage of the ring holds a block for each stream, K and V.  (Two blocks a compute unit, where heads are no longer than 128; stages of K and of
+  // V in turn are twice the barriers: 20 rows of e4m3 over 29 windows of 9000 positions 99 us, this way 91.)
   static constexpr int STREAMS = WAVES / TILES, BLOCK_BYTES = 128 * D, STAGE = STREAMS * BLOCK_BYTES;
-  static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;  // (two blocks a compute unit, where heads are no longer than 128)
+  static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;
+  static constexpr int PIECES = STAGE / 1024 / WAVES;  // loads of a stage by each wave
   // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
   // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256, or where LDS
   // has no room for two blocks, a wave has a SIMD for itself.
-  static constexpr int WAVES_PER_SIMD = D < 256 && (!SHARED || S * STAGE <= 80 * 1024) ? 2 : 1;
-  static constexpr int PIECES = STAGE / 1024 / WAVES;                  // loads of a stage by each wave
+  static constexpr int SUMS = WAVES * ROWS * (PAD + 2) * 4, LDS_BYTES = RING && S * STAGE > SUMS ? S * STAGE : SUMS;
+  static constexpr int WAVES_PER_SIMD = D < 256 && LDS_BYTES <= 79 * 1024 ? 2 : 1;
 
-  struct Lds {
+  struct Shared {
     union {
       struct {
-        float o[WAVES][16][PAD];
-        float m[WAVES][16], l[WAVES][16];
+        float o[WAVES][ROWS][PAD];
+        float m[WAVES][ROWS], l[WAVES][ROWS];
       };
-      char ring[SHARED ? S * STAGE : 16];
+      char ring[RING ? S * STAGE : 16];
     };
     int64_t scan[WAVES];
     int64_t begin;  // of the block's slice, from the first block of its first sequence
@@ -218,10 +224,44 @@ template <int TYPE, int D, int TILES> struct Attend {
   static __device__ __forceinline__ void load_lds(const char* from, char* to) {
     __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from, (void __attribute__((address_space(3)))*)to, 16, 0, 2 /* nt */);
   }
+  // until no more than the `younger` stages asked for last are on their way
+  template <int N> static __device__ __forceinline__ void wait_stage(int younger) {
+    if constexpr (N == 0) wait_vmcnt<0>();
+    else if (younger >= N) wait_vmcnt<N * PIECES>();
+    else wait_stage<N - 1>(younger);
+  }
+  static __device__ __forceinline__ uint32_t lds_at(const char* p) { return (uint32_t)(uintptr_t)(const char __attribute__((address_space(3)))*)p; }
+  // N times 16 bytes of LDS, 256 apart, asked for together.  (Left to the compiler each is waited for
+  // by itself: 96 rows over 16 x 8000 positions 164 us, together 136.)
+  template <int N, int OFFSET> static __device__ __forceinline__ void read_lds(uint32_t at, u32x4* v) {
+    if constexpr (N == 4)
+      asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                   : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(at), "i"(OFFSET), "i"(OFFSET + 256), "i"(OFFSET + 512), "i"(OFFSET + 768) : "memory");
+    else
+      asm volatile("ds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                   : "=&v"(v[0]), "=&v"(v[1]) : "v"(at), "i"(OFFSET), "i"(OFFSET + 256) : "memory");
+  }
+  // the operands of K and of V from the I-th on, in turn to `use(i, operand)`
+  template <int I, class F> static __device__ __forceinline__ void each_k(uint32_t at, F use) {
+    constexpr int N = J;
+    u32x4 v[N];
+    read_lds<N, I / J * (4 * B * 16)>(at, v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) use(I + k, v[k]);
+    if constexpr (I + N < NL) each_k<I + N>(at, use);
+  }
+  template <int I, class F> static __device__ __forceinline__ void each_v(uint32_t at, F use) {
+    constexpr int N = NL - I >= 4 ? 4 : 2;
+    u32x4 v[N];
+    read_lds<N, I * 256>(at, v);
+#pragma unroll
+    for (int k = 0; k < N; ++k) use(I + k, v[k]);
+    if constexpr (I + N < NL) each_v<I + N>(at, use);
+  }
   static __device__ __forceinline__ bf16x8 part_of(const u32x4& v, int h) { return E == 8 ? operand(v) : operand8(v[2 * h], v[2 * h + 1]); }
 
   // sum over the block, and the sum of the threads before this one
-  static __device__ __forceinline__ int64_t scan(int64_t v, int64_t& before, Lds& s) {
+  static __device__ __forceinline__ int64_t scan(int64_t v, int64_t& before, Shared& s) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     int64_t x = v;
 #pragma unroll
@@ -241,8 +281,8 @@ template <int TYPE, int D, int TILES> struct Attend {
     return total;
   }
 
-  static __device__ void run(const AttendArgs& g, Lds& s) {
-    const int block_row0 = blockIdx.x % g.groups * (16 * TILES), row_end = min(g.rows, block_row0 + 16 * TILES);
+  static __device__ void run(const AttendArgs& g, Shared& s) {
+    const int block_row0 = blockIdx.x % g.groups * BLOCK_ROWS, row_end = min(g.rows, block_row0 + BLOCK_ROWS);
     const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
@@ -315,33 +355,41 @@ template <int TYPE, int D, int TILES> struct Attend {
   }
 
   // Blocks [b0, b1) of sequence seq_i; where_to: -1: they are all of it, 0 / 1: the unfinished sum at the slice's begin / end
-  static __device__ __forceinline__ void part(const AttendArgs& g, Lds& s, const Span& sp, int seq_i, int block_row0, int row_end, int b0, int b1, int where_to) {
+  static __device__ __forceinline__ void part(const AttendArgs& g, Shared& s, const Span& sp, int seq_i, int block_row0, int row_end, int b0, int b1, int where_to) {
     const si_cache_t& c = g.c;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), grp = lane / 16, col = lane % 16;
     const int kv = blockIdx.x / g.groups, per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
-    // the block has the rows [block_row0, row_end), this wave 16 of them from row0 on; STREAMS waves take the cache blocks in turn
-    const int stream = wave / TILES, row0 = block_row0 + wave % TILES * 16;
+    // the block has the rows [block_row0, row_end), this wave ROWS of them from row0 on; STREAMS waves take the cache blocks in turn
+    const int stream = wave / TILES, row0 = block_row0 + wave % TILES * ROWS;
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
-    // this lane's row of q, as the right operand; token of the row, or -1
-    const int row = row0 + col, tok = row < row_end ? row / per : -1;
-    u32x4 q[D / 32];
-    {
+    // this lane's rows of q, as right operands; token of a row, or -1
+    int tok[NT];
+    u32x4 q[NT][D / 32];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const int row = row0 + 16 * u + col;
+      tok[u] = row < row_end ? row / per : -1;
       const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + ((int64_t)seq_i * n_new + row / per) * g.a.q_stride + (int64_t)(kv * per + row % per) * D;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         // operand x of K covers, in this lane, elements 32 x + 8 grp of a head (bf16), or half x % 2 of the 16 from 64 (x / 2) + 16 grp on
         const int dim = E == 8 ? 32 * x + 8 * grp : 64 * (x / 2) + 16 * grp + 8 * (x % 2);
-        q[x] = tok >= 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(p + dim)) : u32x4{0, 0, 0, 0};
+        q[u][x] = tok[u] >= 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(p + dim)) : u32x4{0, 0, 0, 0};
       }
     }
     const float sc = g.scale2 * (TYPE == SI_KV_E4M3 && c.scale_k ? c.scale_k[kv] : 1.f);
     const float scale_v = TYPE == SI_KV_E4M3 && c.scale_v ? c.scale_v[kv] : 1.f;
 
-    f32x4 o[NL];
-    float m = -INFINITY, l = 0.f;
+    f32x4 o[NT][NL];
+    float m[NT], l[NT];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < NT; ++u) {
+      m[u] = -INFINITY;
+      l[u] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) o[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     // Where a block of the stream lies: entry of the table and place in the page.  The page's number comes by a scalar load, which the loads of K
     // and V in flight have nothing to do with (a vector load in their midst is waited for along with all of them); nothing in this
@@ -364,8 +412,8 @@ template <int TYPE, int D, int TILES> struct Attend {
     const char* k_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 0, kv) * BYTES;
     const char* v_base = static_cast<const char*>(c.pages) + kv_head_offset(c, g.layer, 1, kv) * BYTES;
     const int k_lane = grp * (B * 16) + col * 16, v_lane = grp * (D * 16) + col * 16;
-    const char *k_lds = nullptr, *v_lds = nullptr;  // SHARED: the block in work
-    u32x4 kf[SHARED ? 1 : NL], vf[SHARED ? 1 : NL];
+    const char *k_lds = nullptr, *v_lds = nullptr;  // RING: the block in work
+    u32x4 kf[RING ? 1 : NL], vf[RING ? 1 : NL];
     auto load_k = [&](int page, int at) {
       const char* p = k_base + (uint32_t)max(page, 0) * page_bytes + at * (64 * D);
 #pragma unroll
@@ -376,96 +424,117 @@ template <int TYPE, int D, int TILES> struct Attend {
 #pragma unroll
       for (int i = 0; i < NL; ++i) vf[i] = load16(p + v_lane + i * 256);
     };
-    auto k_of = [&](int i) {
-      if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(k_lds + k_lane + i / J * (4 * B * 16) + i % J * 256);
-      else return kf[i];
+    // operands of K and of V, in turn to `use(i, operand)`
+    auto k_to = [&](auto use) {
+      if constexpr (RING) {
+        each_k<0>(lds_at(k_lds) + k_lane, use);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) use(i, kf[i]);
+      }
     };
-    auto v_of = [&](int i) {
-      if constexpr (SHARED) return *reinterpret_cast<const u32x4*>(v_lds + v_lane + i * 256);
-      else return vf[i];
+    auto v_to = [&](auto use) {
+      if constexpr (RING) {
+        each_v<0>(lds_at(v_lds) + v_lane, use);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) use(i, vf[i]);
+      }
     };
 
     // scores of a block: tile j, element i of this lane is token grp * E + 4 j + i
-    f32x4 x[J];
+    f32x4 x[NT][J];
     auto scores = [&] {
 #pragma unroll
-      for (int j = 0; j < J; ++j) x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < NT; ++u)
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const u32x4 k = k_of(i);
+        for (int j = 0; j < J; ++j) x[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      k_to([&](int i, const u32x4& k) {
 #pragma unroll
-        for (int h = 0; h < H; ++h) x[i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(k, h), operand(q[i / J * H + h]), x[i % J], 0, 0, 0);
-      }
+        for (int h = 0; h < H; ++h) {
+          const bf16x8 k8 = part_of(k, h);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) x[u][i % J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, operand(q[u][i / J * H + h]), x[u][i % J], 0, 0, 0);
+        }
+      });
     };
     // weights of the block, and what has been summed brought to its maximum; EDGE: some rows may not see some of its tokens.
     // The weights are rounded to bf16, as operands are (2^-8 of each, the sum l takes them as they were: the error of out is that of a
     // mean of roundings, below its own rounding)
-    u32x4 p[H];
+    u32x4 p[NT][H];
     auto weights = [&](auto EDGE, int t0) {
-      float top = -INFINITY;
-      const int see_hi = tok >= 0 ? max(0, first + tok) : 0, see_lo = window ? max(0, first + tok - window) : 0;
+      int mine = t0 + grp * E;  // first token of this lane
+      if constexpr (EDGE) asm volatile("" : "+v"(mine));  // (or the tokens of each element are formed before the loop and held through it)
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+      for (int u = 0; u < NT; ++u) {
+        float top = -INFINITY;
+        const int see_hi = tok[u] >= 0 ? max(0, first + tok[u]) : 0, see_lo = window ? max(0, first + tok[u] - window) : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float v = x[j][i] * sc;
-          if constexpr (EDGE) {
-            const int pos = t0 + grp * E + 4 * j + i;
-            v = pos >= see_lo && pos < see_hi ? v : -INFINITY;
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v = x[u][j][i] * sc;
+            if constexpr (EDGE) {
+              const int pos = mine + 4 * j + i;
+              v = pos >= see_lo && pos < see_hi ? v : -INFINITY;
+            }
+            x[u][j][i] = v;
+            top = fmaxf(top, v);
           }
-          x[j][i] = v;
-          top = fmaxf(top, v);
-        }
-      const float m_new = fmaxf(m, max_of_row(top)), base = finite_base(m_new);
-      if (__any(m_new > m)) {
-        const float f = pow2(m - base);
-        l *= f;
+        const float m_new = fmaxf(m[u], max_of_row(top)), base = finite_base(m_new);
+        if (__any(m_new > m[u])) {
+          const float f = pow2(m[u] - base);
+          l[u] *= f;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) o[i] *= f;
-        m = m_new;
+          for (int i = 0; i < NL; ++i) o[u][i] *= f;
+          m[u] = m_new;
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int j = 2 * h + w / 2, i = 2 * (w % 2);
+            const float a = pow2(x[u][j][i] - base), e = pow2(x[u][j][i + 1] - base);
+            l[u] += a + e;
+            p[u][h][w] = bf16_pair(a, e);
+          }
       }
-#pragma unroll
-      for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int j = 2 * h + w / 2, i = 2 * (w % 2);
-          const float a = pow2(x[j][i] - base), e = pow2(x[j][i + 1] - base);
-          l += a + e;
-          p[h][w] = bf16_pair(a, e);
-        }
     };
     auto products = [&](auto EDGE, const u32x4& keep) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        u32x4 v = v_of(i);
+      v_to([&](int i, u32x4 v) {
         if constexpr (EDGE) v &= keep;
 #pragma unroll
-        for (int h = 0; h < H; ++h) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[h]), o[i], 0, 0, 0);
-      }
+        for (int h = 0; h < H; ++h) {
+          const bf16x8 v8 = part_of(v, h);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) o[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, operand(p[u][h]), o[u][i], 0, 0, 0);
+        }
+      });
     };
     // the same where some rows may not see some tokens.  What no row sees may be anything (weight 0 times infinity would be NaN); what
     // some of the tokens see and is not finite takes a product for each of them
     auto products_at_edge = [&](int t0) {
-      const u32x4 keep = token_mask(t0 + grp * E, lo, hi);
+      int mine = t0 + grp * E;
+      asm volatile("" : "+v"(mine));
+      const u32x4 keep = token_mask(mine, lo, hi);
       bool bad = false;
-      if (n_new > 1) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) bad |= not_finite(v_of(i) & keep);
-      }
+      if (n_new > 1) v_to([&](int, const u32x4& v) { bad |= not_finite(v & keep); });
       if (!__any(bad)) {
         products(std::true_type{}, keep);
         return;
       }
-      for (int j = row0 / per; j <= (min(row_end, row0 + 16) - 1) / per; ++j) {
-        const u32x4 mine = token_mask(t0 + grp * E, window ? max(0, first + j - window) : 0, max(0, first + j));
+      for (int j = row0 / per; j <= (min(row_end, row0 + ROWS) - 1) / per; ++j) {
+        const u32x4 seen = token_mask(mine, window ? max(0, first + j - window) : 0, max(0, first + j));
+        v_to([&](int i, u32x4 v) {
+          v &= seen;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          const u32x4 v = v_of(i) & mine;
-          f32x4 r = {0.f, 0.f, 0.f, 0.f};
+          for (int u = 0; u < NT; ++u) {
+            f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[h]), r, 0, 0, 0);
-          if (tok == j) o[i] += r;
-        }
+            for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[u][h]), r, 0, 0, 0);
+            if (tok[u] == j) o[u][i] += r;
+          }
+        });
       }
     };
     auto weigh = [&](int t0) {  // after the scores; the main path and that of the edges
@@ -479,7 +548,7 @@ template <int TYPE, int D, int TILES> struct Attend {
     };
 
     bool bad_page = false;
-    if constexpr (SHARED) {
+    if constexpr (RING) {
       const int turns = (b1 - b0 + STREAMS - 1) / STREAMS;
       uint32_t missing = 0;  // bit turn * STREAMS + stream, modulo 32: the block's page is not there
       Place front{b0 / per_page, b0 % per_page};
@@ -502,10 +571,7 @@ template <int TYPE, int D, int TILES> struct Attend {
       };
       for (int turn = 0; turn < min(S - 1, turns); ++turn) issue(turn);
       for (int turn = 0; turn < turns; ++turn) {
-        const int younger = min(S - 2, turns - 1 - turn);  // stages asked for after this one
-        if (younger >= 2) wait_vmcnt<2 * PIECES>();
-        else if (younger == 1) wait_vmcnt<PIECES>();
-        else wait_vmcnt<0>();
+        wait_stage<S - 2>(turns - 1 - turn);
         // everybody's loads of this stage have arrived, and what was read of the one before has been used
         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
         asm volatile("" ::: "memory");
@@ -558,17 +624,20 @@ template <int TYPE, int D, int TILES> struct Attend {
     if (bad_page && lane == 0) atomicOr(c.status, SI_CACHE_BAD_PAGE);
 
     // the streams of the block
-    l = sum_of_row(l);
-    if (grp == 0) { s.m[wave][col] = m; s.l[wave][col] = l; }
 #pragma unroll
-    for (int i = 0; i < NL; ++i) *reinterpret_cast<f32x4*>(&s.o[wave][col][16 * i + 4 * grp]) = o[i];
+    for (int u = 0; u < NT; ++u) {
+      l[u] = sum_of_row(l[u]);
+      if (grp == 0) { s.m[wave][16 * u + col] = m[u]; s.l[wave][16 * u + col] = l[u]; }
+#pragma unroll
+      for (int i = 0; i < NL; ++i) *reinterpret_cast<f32x4*>(&s.o[wave][16 * u + col][16 * i + 4 * grp]) = o[u][i];
+    }
     __syncthreads();
     const int items = (row_end - block_row0) * (D / 4);
     float* sums = g.part + (((int64_t)blockIdx.x * g.slices + blockIdx.y) * 2 + max(where_to, 0)) * (g.part_rows * (D + 2));
     for (int i = threadIdx.x; i < items; i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
       Sum sum;
-      for (int w = r / 16; w < WAVES; w += TILES) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % 16][dim]), s.m[w][r % 16], s.l[w][r % 16]);
+      for (int w = r / ROWS; w < WAVES; w += TILES) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % ROWS][dim]), s.m[w][r % ROWS], s.l[w][r % ROWS]);
       float* to = sums + r * (D + 2);
       if (where_to < 0) {
         write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
@@ -611,9 +680,10 @@ template <int TYPE, int D, int TILES> struct Attend {
   }
 };
 
-template <int TYPE, int D, int TILES> __global__ __launch_bounds__((Attend<TYPE, D, TILES>::THREADS), (Attend<TYPE, D, TILES>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
-  __shared__ typename Attend<TYPE, D, TILES>::Lds s;
-  Attend<TYPE, D, TILES>::run(g, s);
+template <int TYPE, int D, int NT, int TILES>
+__global__ __launch_bounds__((Attend<TYPE, D, NT, TILES>::THREADS), (Attend<TYPE, D, NT, TILES>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
+  __shared__ typename Attend<TYPE, D, NT, TILES>::Shared s;
+  Attend<TYPE, D, NT, TILES>::run(g, s);
 }
 
 // Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
@@ -621,7 +691,7 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   constexpr int LANES = D / 4, SHARES = 256 / LANES;
   __shared__ f32x4 s_o[SHARES][LANES];
   __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
-  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, row = blockIdx.x % g.groups * (16 * g.tiles) + blockIdx.z;
+  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, row = blockIdx.x % g.groups * g.block_rows + blockIdx.z;
   typedef const int32_t __attribute__((address_space(4))) constant_t;
   const constant_t* parted = (const constant_t*)(uintptr_t)(g.parted + (int64_t)seq_i * gridDim.x + blockIdx.x);
   const int first = parted[0], parts = parted[1];
@@ -656,9 +726,10 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
 template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
   // (heads first: blocks go to the dies in turn, and all heads of a slice have the same to do)
   const dim3 grid(g.c.n_kv_heads * g.groups, g.slices);
-  if (g.tiles == 1) hipLaunchKernelGGL((k_attend<TYPE, D, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if (g.tiles == 2) hipLaunchKernelGGL((k_attend<TYPE, D, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else hipLaunchKernelGGL((k_attend<TYPE, D, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   if (g.slices > 1 && !g.whole && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

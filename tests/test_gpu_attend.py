@@ -132,6 +132,21 @@ def test_long_sequences_split_over_blocks(kind, n_new):
     attend_case(kind, [6000, 700], n_new, 4, 4, 128, 128, window=3000)
 
 
+@pytest.mark.parametrize("kind", [BF, F8])
+@pytest.mark.parametrize("n_new,heads", [(9, 16), (13, 20), (17, 16)])
+def test_many_rows_over_long_sequences(kind, n_new, heads):
+    """72, 130 and 136 rows a kv head: one block, and more, of 128 rows; pieces of a sequence from several blocks."""
+    attend_case(kind, [3001], n_new, heads, 2, 128, 128)
+    attend_case(kind, [2100, 0, 7, 1500, 1], n_new, heads, 2, 64, 64, window=1100)
+
+
+@pytest.mark.parametrize("kind", [BF, F8])
+def test_many_sequences_of_all_lengths(kind):
+    lens = [(i * 379) % 1700 for i in range(41)]
+    attend_case(kind, lens, 1, 8, 2, 64, 64)
+    attend_case(kind, lens, 5, 8, 2, 128, 128)
+
+
 def test_many_new_tokens():
     attend_case(BF, [100, 37, 400], 50, 8, 2, 64, 32)
     attend_case(F8, [300, 64], 65, 4, 2, 128, 64, window=40)
