@@ -315,7 +315,7 @@ void si_layer_destroy(si_layer_t* layer);
 
 /*
  * A stack of layers run back to back: the MLP / MoE blocks of consecutive Transformer layers with the
- * residual connection around each (attention lies outside this library),
+ * residual connection around each (nothing between them; what stands there in a model: scheinfer_attention.h),
  *   x_0 = x,   x_{l+1} = bf16(x_l + Layer_l(x_l)),   h_out = x_{n-1} + Layer_{n-1}(x_{n-1})   (fp32, not rounded).
  * Each layer keeps its own slicing rates, e.g. the r_GG that si_assign_gpu_memory gave it (Section IV-A.4).
  * prefetch bit 0: the first CG pieces of layer l+1 are put on the host link as soon as the copies of layer l are

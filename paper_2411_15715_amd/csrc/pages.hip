@@ -1,7 +1,10 @@
 // Moves of the cache's pages.  Every decision (which page is free, who shares what) depends on all of the small tables, so a block makes it
 // alone, with prefix sums instead of counters.  Where pages are copied, all blocks of a launch make the same decisions, each copies its
 // share (into pages that are free: nobody minds, whatever comes after), and the block that finishes last, when nobody reads the tables any
-// more, writes them: one launch, and no block waits for another.
+// more, writes them: one launch, and no block waits for another.  (A launch that decides and one that copies: 33 sequences extended
+// 13.9 us a call, in one launch 11.7; 48 beams of 5 sources forked 113 and 108.)
+// Forking and compacting are bound by memory (beams: 445 MB, 4.3 TB/s; 2.0 GB of a pool packed in 366 us, 5.5 TB/s), extending by the
+// chain of a decision: lists, lengths, table, counts, two prefix sums, 9 us in the kernel for 33 sequences.
 #include "si_internal.h"
 #include "si_error.h"
 #include "kv_layout.h"
