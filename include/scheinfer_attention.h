@@ -173,8 +173,8 @@ typedef struct {
 } si_attend_t;
 int si_attend(const si_cache_t* cache, int32_t layer, const si_attend_t* desc, void* stream);
 
-/* Bytes of scratch that si_attend needs for these descriptors, or a negative SI_E* code (host only, no GPU needed; q, out, lse, scratch and
- * scratch_bytes are not looked at). */
+/* Bytes of scratch that si_attend needs for these descriptors, and for any with a smaller n or max_len; or a negative SI_E* code (host only, no
+ * GPU needed; q, out, lse, scratch and scratch_bytes are not looked at). */
 int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc);
 
 /* ------------------------------------------------------------------------------------------------ moves of pages

@@ -34,13 +34,16 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   const bool twice = c.head_dim <= 128 && (k.block_rows > 16 || a.n * units > 256);
   const int most = twice ? 512 : 256, streams = std::max(1, 64 / k.block_rows);
   k.whole = each <= 20 || (each <= 40 && a.n * units >= 512);
-  k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min<int64_t>(most / units, (a.n * each + 2 * streams - 1) / (2 * streams)));
+  const int64_t useful = (a.n * each + 2 * streams - 1) / (2 * streams);
+  k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min(most / units, useful));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
   k.last_joins = !k.whole && k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
-  if (!k.whole && k.slices > 1) {
+  // (room for as many slices as any call of no more or longer sequences takes)
+  const int64_t room = std::min((c.head_dim <= 128 ? 512 : 256) / units, useful);
+  if (room > 1) {
     k.parted_at = ATTEND_COUNTERS * 4;
     k.part_at = k.parted_at + (a.n * units * 8 + 15) / 16 * 16;
-    k.scratch = k.part_at + units * k.slices * 2 * k.part_rows * (c.head_dim + 2) * 4;
+    k.scratch = k.part_at + units * room * 2 * k.part_rows * (c.head_dim + 2) * 4;
   }
   return k;
 }

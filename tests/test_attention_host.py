@@ -175,6 +175,16 @@ def moves(c):
             "si_cache_compact": lambda a=BASE, n=2, k=BASE: si.si_cache_compact(c, c, BASE)}
 
 
+@pytest.mark.parametrize("head_dim", [64, 256])
+@pytest.mark.parametrize("n_new", [1, 5, 40])
+def test_scratch_of_a_larger_call_serves_smaller_ones(head_dim, n_new):
+    """More sequences, or longer ones, need no less."""
+    c = cache(n_pages=1 << 20, max_pages=1 << 14, n_seqs=4096, head_dim=head_dim)
+    sizes = np.array([[si.si_attend_scratch_bytes(c, attend(n=n, n_new=n_new, max_len=L, q_stride=1 << 20, out_stride=1 << 20)) for L in
+                       (0, 1, 31, 600, 640, 641, 1280, 1281, 5000, 200000)] for n in (0, 1, 2, 7, 60, 128, 129, 256, 1000, 4000)])
+    assert (np.diff(sizes, axis=0) >= 0).all() and (np.diff(sizes, axis=1) >= 0).all()
+
+
 @pytest.mark.parametrize("kw", BAD_CACHES + [dict(refs=None), dict(scratch=None), dict(scratch=BASE + 8)])
 def test_moves_refuse_bad_caches(kw):
     for name, f in moves(cache(**kw)).items():
