@@ -175,10 +175,9 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;
   static constexpr int PIECES = STAGE / 1024 / WAVES;  // loads of a stage by each wave
   // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
-  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 256, or where LDS
-  // has no room for two blocks, a wave has a SIMD for itself.
-  static constexpr int SUMS = WAVES * ROWS * (PAD + 2) * 4, LDS_BYTES = RING && S * STAGE > SUMS ? S * STAGE : SUMS;
-  static constexpr int WAVES_PER_SIMD = D < 256 && LDS_BYTES <= 79 * 1024 ? 2 : 1;
+  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 192 and 256 a wave has a SIMD for itself: two do not
+  // fit their registers (192: 64 x 4000 positions 139 us spilling, 121 alone; e4m3 84 and 68), nor two blocks a unit's LDS.
+  static constexpr int WAVES_PER_SIMD = D < 192 ? 2 : 1;
 
   struct Shared {
     union {
