@@ -11,19 +11,24 @@ namespace {
 
 struct Cut {
   int block_rows, groups, slices, whole, part_rows, last_joins;
-  int64_t scratch, parted_at, part_at;
+  int64_t scratch, part_at;
 };
 
 // Rows of a block, row groups, and the slices that a kv head's cache blocks are cut into.
 Cut cut(const si_cache_t& c, const si_attend_t& a) {
   Cut k{};
   const int rows = a.n_new * (a.n_heads / c.n_kv_heads), B = kv_block(c.type);
-  for (k.block_rows = 16; k.block_rows < rows && k.block_rows < 128;) k.block_rows *= 2;
-  k.groups = (rows + k.block_rows - 1) / k.block_rows;
-  k.part_rows = std::min(rows, k.block_rows);
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
-  const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B), units = (int64_t)c.n_kv_heads * k.groups;
+  const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B);
+  // Blocks of 128 rows read the cache once where two of 64 read it twice (96 rows over 16 x 8000 positions 192 -> 130 us, e4m3 138 -> 121), but
+  // short sequences are not bound by that (200 rows over 300 and 900 positions e4m3 31 us in blocks of 64, 40 of 128), and with longer
+  // heads 32 rows a wave do not fit the registers (heads of 256 227 and 271 us).
+  const int most_rows = c.head_dim <= 128 && each > 20 ? 128 : 64;
+  for (k.block_rows = 16; k.block_rows < rows && k.block_rows < most_rows;) k.block_rows *= 2;
+  k.groups = (rows + k.block_rows - 1) / k.block_rows;
+  k.part_rows = std::min(rows, k.block_rows);
+  const int64_t units = (int64_t)c.n_kv_heads * k.groups;
   // As many blocks as there are compute units; twice that where a slice holds several sequences (the next one's first loads have nothing beside
   // them: 512 sequences of 64 positions 57 -> 38 us) or the waves of a block share their loads and wait for each other (40 rows over
   // 16 x 8000 positions 119 -> 106 us) and two blocks fit a unit.  Else it is one more round of sums to write and read (131071 positions 86
@@ -38,12 +43,12 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min(most / units, useful));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
   k.last_joins = !k.whole && k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
-  // (room for as many slices as any call of no more or longer sequences takes)
-  const int64_t room = std::min((c.head_dim <= 128 ? 512 : 256) / units, useful);
-  if (room > 1) {
-    k.parted_at = ATTEND_COUNTERS * 4;
-    k.part_at = k.parted_at + (a.n * units * 8 + 15) / 16 * 16;
-    k.scratch = k.part_at + units * room * 2 * k.part_rows * (c.head_dim + 2) * 4;
+  // Room for as many slices as any call of no more or longer sequences takes, in blocks of up to 64 rows too
+  for (int block_rows = std::min(64, k.block_rows); block_rows <= k.block_rows; block_rows *= 2) {
+    const int64_t block_units = (int64_t)c.n_kv_heads * ((rows + block_rows - 1) / block_rows), room = std::min((c.head_dim <= 128 ? 512 : 256) / block_units, useful);
+    const int64_t part_at = ATTEND_COUNTERS * 4 + (a.n * block_units * 8 + 15) / 16 * 16;
+    if (room > 1) k.scratch = std::max(k.scratch, part_at + block_units * room * 2 * std::min(rows, block_rows) * (c.head_dim + 2) * 4);
+    if (block_rows == k.block_rows) k.part_at = part_at;
   }
   return k;
 }
@@ -94,7 +99,7 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   if (k.scratch > 0) {
     char* p = static_cast<char*>(a->scratch);
     g.count = reinterpret_cast<uint32_t*>(p);
-    g.parted = reinterpret_cast<int2*>(p + k.parted_at);
+    g.parted = reinterpret_cast<int2*>(p + ATTEND_COUNTERS * 4);
     g.part = reinterpret_cast<float*>(p + k.part_at);
   }
   const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);

@@ -158,7 +158,7 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn
 // (TILES == 1) a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97).  Several read them from LDS,
 // into which the block loads each cache block once, without a detour through registers: S stages of a block for each stream.  (Each
 // wave loading for itself, TILES requests for every line at the caches: 24 rows over 16 x 8000 positions 108 us, this way 97.)
-// From 65 rows on a wave has 32 (96 rows over 16 x 8000 positions in two blocks of 64: 196 us, in one of 128: 136), with fewer 16: two waves with the
+// In blocks of 128 rows a wave has 32, in smaller ones 16: two waves with the
 // same cache block hide each other's waits (20 rows of e4m3 over 29 windows of 9000 positions, 32 a wave and a ring for each wave: 113 us, 16: 91).
 template <int TYPE, int D, int NT, int TILES> struct Attend {
   static constexpr int ROWS = 16 * NT, BLOCK_ROWS = ROWS * TILES;              // of a wave, of a block
@@ -728,7 +728,7 @@ template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t st
   if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if constexpr (D <= 128) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   if (g.slices > 1 && !g.whole && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
