@@ -148,7 +148,7 @@ int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* d
  *   out = softmax over them of (scale q . K) applied to V,   lse = ln sum exp(scale q . K)
  * A token that sees nothing (its position is negative: lens < n_new) gets out 0 and lse -infinity.  What a token does not see has no part in
  * its output, whatever the pages hold there, NaN and infinities included.  Products are of bf16 operands (e4m3 codes widen to bf16
- * exactly), sums, maxima and weights fp32.
+ * exactly); sums and maxima are fp32, a weight is multiplied as the sum of two bf16 values, 2^-16 of it lost.
  * max_len sizes the launch: an upper bound of lens (a sequence beyond it is still computed, by fewer blocks than it deserves).
  * scratch: si_attend_scratch_bytes of these descriptors or more, 16-byte aligned, zero before its first use; every call leaves it fit for
  * any other call.  Two calls that may run at once need one each.  Results do not depend on the order in which blocks run.

@@ -21,10 +21,10 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
   const int64_t each = std::max<int64_t>(1, (seen + B - 1) / B);
-  // Blocks of 128 rows read the cache once where two of 64 read it twice (96 rows over 16 x 8000 positions 192 -> 130 us, e4m3 138 -> 121), but
-  // short sequences are not bound by that (200 rows over 300 and 900 positions e4m3 31 us in blocks of 64, 40 of 128), and with longer
-  // heads 32 rows a wave do not fit the registers (heads of 256 227 and 271 us).
-  const int most_rows = c.head_dim <= 128 && each > 20 ? 128 : 64;
+  // Blocks of 128 rows read the cache once where two of 64 read it twice (96 rows over 16 x 8000 positions 182 us in blocks of 64, 168 of 128; 640 over
+  // 16 x 4000 487 and 443), but short sequences are not bound by that, and with longer heads 32 rows a wave do not fit the registers (e4m3,
+  // heads of 128, which also converts its codes there: the first case 153 and 161 us, 160 rows over 16 x 4000 138 and 183).
+  const int most_rows = c.head_dim <= attend_wide_dim(c.type) && each > 20 ? 128 : 64;
   for (k.block_rows = 16; k.block_rows < rows && k.block_rows < most_rows;) k.block_rows *= 2;
   k.groups = (rows + k.block_rows - 1) / k.block_rows;
   k.part_rows = std::min(rows, k.block_rows);

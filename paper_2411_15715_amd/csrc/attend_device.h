@@ -25,6 +25,7 @@ namespace si {
 constexpr int ATTEND_WAVES = 4;         // of a block
 constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
 constexpr int ATTEND_COUNTERS = 16384;  // sequences times units (kv head, row group) whose parts the last block may join
+constexpr int attend_wide_dim(int type) { return type == SI_KV_E4M3 ? 64 : 128; }  // longest heads of which a wave may have 32 rows
 
 struct AttendArgs {
   si_cache_t c;
@@ -178,6 +179,10 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 192 and 256 a wave has a SIMD for itself: two do not
   // fit their registers (192: 64 x 4000 positions 139 us spilling, 121 alone; e4m3 84 and 68), nor two blocks a unit's LDS.
   static constexpr int WAVES_PER_SIMD = D < 192 ? 2 : 1;
+  // Heads of 256 of e4m3 without the ring: K and V of two blocks, sums and weights fill the 256 registers that vector instructions reach.  The next K is
+  // asked for after the products with V instead of before, and q and the sums are held where only matrix instructions reach them (64 x 4000
+  // positions 86 us; else registers are spilled in the loop, and a reload waits for all loads in flight: 223).
+  static constexpr bool LEAN = !RING && TYPE == SI_KV_E4M3 && D == 256;
 
   struct Shared {
     union {
@@ -191,6 +196,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     int64_t begin;  // of the block's slice, from the first block of its first sequence
     int first;      // that sequence
     uint32_t arrived[2];
+    int again;      // RING: some wave's sums are not finite
   };
 
   // words of 16 bytes of V of this lane (E tokens from t0 on) that lie in [lo, hi)
@@ -207,16 +213,17 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     }
     return w;
   }
-  static __device__ __forceinline__ bool not_finite(const u32x4& v) {
-    bool bad = false;
+  // what is not finite becomes 0
+  static __device__ __forceinline__ u32x4 finite_only(const u32x4& v) {
+    u32x4 r = v;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < E / 4; ++e) {
-        if constexpr (E == 8) bad |= (v[i] >> (16 * e) & 0x7f80u) == 0x7f80u;
-        else bad |= (v[i] >> (8 * e) & 0x7fu) == 0x7fu;
+        const uint32_t all = E == 8 ? 0xffffu << (16 * e) : 0xffu << (8 * e), top = E == 8 ? 0x7f80u << (16 * e) : 0x7fu << (8 * e);
+        if ((v[i] & top) == top) r[i] &= ~all;
       }
-    return bad;
+    return r;
   }
   static __device__ __forceinline__ u32x4 load16(const char* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
   // 1 KB from the lanes' addresses to LDS, on its way until waited for
@@ -282,6 +289,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
 
   static __device__ void run(const AttendArgs& g, Shared& s) {
     const int block_row0 = blockIdx.x % g.groups * BLOCK_ROWS, row_end = min(g.rows, block_row0 + BLOCK_ROWS);
+    if (RING && threadIdx.x == 0) s.again = 0;
     const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
@@ -377,18 +385,17 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
         q[u][x] = tok[u] >= 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(p + dim)) : u32x4{0, 0, 0, 0};
       }
     }
+    if constexpr (LEAN) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) asm volatile("" : "+a"(q[u][x]));
+    }
     const float sc = g.scale2 * (TYPE == SI_KV_E4M3 && c.scale_k ? c.scale_k[kv] : 1.f);
     const float scale_v = TYPE == SI_KV_E4M3 && c.scale_v ? c.scale_v[kv] : 1.f;
 
     f32x4 o[NT][NL];
     float m[NT], l[NT];
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-      m[u] = -INFINITY;
-      l[u] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) o[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
 
     // Where a block of the stream lies: entry of the table and place in the page.  The page's number comes by a scalar load, which the loads of K
     // and V in flight have nothing to do with (a vector load in their midst is waited for along with all of them); nothing in this
@@ -444,6 +451,12 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     // scores of a block: tile j, element i of this lane is token grp * E + 4 j + i
     f32x4 x[NT][J];
     auto scores = [&] {
+      if constexpr (LEAN) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+          for (int i = 0; i < NL; ++i) asm volatile("" : "+a"(o[u][i]));
+      }
 #pragma unroll
       for (int u = 0; u < NT; ++u)
 #pragma unroll
@@ -458,9 +471,9 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
       });
     };
     // weights of the block, and what has been summed brought to its maximum; EDGE: some rows may not see some of its tokens.
-    // The weights are rounded to bf16, as operands are (2^-8 of each, the sum l takes them as they were: the error of out is that of a
-    // mean of roundings, below its own rounding)
-    u32x4 p[NT][H];
+    // A weight is the sum of two operands, its rounding to bf16 and that of what the rounding left: 2^-16 of it is lost.  (One operand loses
+    // 2^-8 of it, an error relative to sum p |v|, which shows where values cancel.)
+    u32x4 p[NT][H], p_rest[NT][H];
     auto weights = [&](auto EDGE, int t0) {
       int mine = t0 + grp * E;  // first token of this lane
       if constexpr (EDGE) asm volatile("" : "+v"(mine));  // (or the tokens of each element are formed before the loop and held through it)
@@ -495,7 +508,10 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
             const int j = 2 * h + w / 2, i = 2 * (w % 2);
             const float a = pow2(x[u][j][i] - base), e = pow2(x[u][j][i + 1] - base);
             l[u] += a + e;
-            p[u][h][w] = bf16_pair(a, e);
+            uint32_t pair = bf16_pair(a, e);
+            asm("" : "+v"(pair));  // (or the first of the pair is rounded once more by itself)
+            p[u][h][w] = pair;
+            p_rest[u][h][w] = bf16_pair(a - __uint_as_float(pair << 16), e - __uint_as_float(pair & 0xffff0000u));
           }
       }
     };
@@ -506,35 +522,18 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
         for (int h = 0; h < H; ++h) {
           const bf16x8 v8 = part_of(v, h);
 #pragma unroll
-          for (int u = 0; u < NT; ++u) o[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, operand(p[u][h]), o[u][i], 0, 0, 0);
+          for (int u = 0; u < NT; ++u) {
+            o[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, operand(p_rest[u][h]), o[u][i], 0, 0, 0);
+            o[u][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, operand(p[u][h]), o[u][i], 0, 0, 0);
+          }
         }
       });
     };
-    // the same where some rows may not see some tokens.  What no row sees may be anything (weight 0 times infinity would be NaN); what
-    // some of the tokens see and is not finite takes a product for each of them
+    // the same where some rows may not see some tokens: what no row sees may be anything (weight 0 times infinity would be NaN)
     auto products_at_edge = [&](int t0) {
       int mine = t0 + grp * E;
       asm volatile("" : "+v"(mine));
-      const u32x4 keep = token_mask(mine, lo, hi);
-      bool bad = false;
-      if (n_new > 1) v_to([&](int, const u32x4& v) { bad |= not_finite(v & keep); });
-      if (!__any(bad)) {
-        products(std::true_type{}, keep);
-        return;
-      }
-      for (int j = row0 / per; j <= (min(row_end, row0 + ROWS) - 1) / per; ++j) {
-        const u32x4 seen = token_mask(mine, window ? max(0, first + j - window) : 0, max(0, first + j));
-        v_to([&](int i, u32x4 v) {
-          v &= seen;
-#pragma unroll
-          for (int u = 0; u < NT; ++u) {
-            f32x4 r = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int h = 0; h < H; ++h) r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[u][h]), r, 0, 0, 0);
-            if (tok[u] == j) o[u][i] += r;
-          }
-        });
-      }
+      products(std::true_type{}, token_mask(mine, lo, hi));
     };
     auto weigh = [&](int t0) {  // after the scores; the main path and that of the edges
       if (t0 < lo_all || t0 + B > hi_all) {
@@ -545,7 +544,54 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
         products(std::false_type{}, u32x4{});
       }
     };
+    // Blocks with values that are not finite: a product for each of the new tokens, with what it sees alone, and none of such a value with the
+    // rest of a weight (which is 0, or of the other sign: infinity times the weight has to stay infinity)
+    auto weigh_one_by_one = [&](int t0) {
+      weights(std::true_type{}, t0);
+      int mine = t0 + grp * E;
+      asm volatile("" : "+v"(mine));
+#pragma unroll 1
+      for (int j = row0 / per; j <= (min(row_end, row0 + ROWS) - 1) / per; ++j) {
+        const u32x4 seen = token_mask(mine, window ? max(0, first + j - window) : 0, max(0, first + j));
+        v_to([&](int i, u32x4 v) {
+          v &= seen;
+          const u32x4 v_finite = finite_only(v);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) {
+            f32x4 r = o[u][i];
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v_finite, h), operand(p_rest[u][h]), r, 0, 0, 0);
+              r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part_of(v, h), operand(p[u][h]), r, 0, 0, 0);
+            }
+            if (tok[u] == j) o[u][i] = r;
+          }
+        });
+      }
+    };
+    auto clear = [&] {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        m[u] = -INFINITY;
+        l[u] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) o[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    // (rows that the call has; what is not finite stays so through every later step, so the end is soon enough to look)
+    auto sums_not_finite = [&] {
+      float t = 0.f;
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+        if (tok[u] >= 0)
+#pragma unroll
+          for (int i = 0; i < NL; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t = fmaf(o[u][i][e], 0.f, t);
+      return (bool)__any(t != 0.f);
+    };
 
+    clear();
     bool bad_page = false;
     if constexpr (RING) {
       const int turns = (b1 - b0 + STREAMS - 1) / STREAMS;
@@ -589,7 +635,30 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
           }
         }
       }
-      if (turns > 0) __syncthreads();  // (the ring's memory is used anew)
+      if (turns > 0) {
+        if (sums_not_finite() && lane == 0) s.again = 1;
+        __syncthreads();  // (the ring's memory is used anew)
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(s.again), 0)) {  // once more, as below
+          clear();
+          front = Place{b0 / per_page, b0 % per_page};
+#pragma unroll 1
+          for (int turn = 0; turn < turns; ++turn) {
+            __syncthreads();
+            if (turn == 0 && threadIdx.x == 0) s.again = 0;
+            issue(turn);
+            wait_vmcnt<0>();
+            __syncthreads();
+            const int b = b0 + turn * STREAMS + stream;
+            if (b < b1 && row0 < row_end && !(missing >> ((turn * STREAMS + stream) % 32) & 1)) {
+              k_lds = s.ring + turn % S * STAGE + stream * BLOCK_BYTES;
+              v_lds = k_lds + 64 * D;
+              scores();
+              weigh_one_by_one(b * B);
+            }
+          }
+          __syncthreads();
+        }
+      }
     } else {
       // K of the next block is asked for when the scores of this one are formed, V when it has been multiplied: 8 to 16 KB of a wave are
       // always on their way (heads of 128).  The last block has no next: written out, so that the loop's loads stand under no condition.
@@ -604,8 +673,9 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
           const Place after = step(next, STREAMS);
           const int after_page = page_of(after);
           scores();
-          load_k(next_page, next.at);
+          if constexpr (!LEAN) load_k(next_page, next.at);
           if (page >= 0) weigh(b * B);  // (a block whose page is not there is passed over)
+          if constexpr (LEAN) load_k(next_page, next.at);
           load_v(next_page, next.at);
           bad_page |= page < 0;
           page = next_page;
@@ -617,6 +687,21 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
           scores();
           weights(std::true_type{}, b * B);
           products_at_edge(b * B);
+        }
+      }
+      // A value that is not finite spoils the sums of rows that do not see it, and its products with the rests of the weights those of rows that do:
+      // once more, with an eye on each value.  Rows that see finite values only come out as they would without the others.
+      if (__builtin_expect(sums_not_finite(), 0)) {
+        clear();
+#pragma unroll 1
+        for (b = b0 + stream; b < b1; b += STREAMS) {
+          const Place here{b / per_page, b % per_page};
+          const int page = page_of(here);
+          if (page < 0) continue;
+          load_k(page, here.at);
+          load_v(page, here.at);
+          scores();
+          weigh_one_by_one(b * B);
         }
       }
     }
@@ -728,7 +813,7 @@ template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t st
   if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if constexpr (D <= 128) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   if (g.slices > 1 && !g.whole && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
