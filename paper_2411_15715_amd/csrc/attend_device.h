@@ -87,9 +87,13 @@ __device__ __forceinline__ float sum_of_row(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// 2^x for x <= 0 or -infinity
+// 2^x for x <= 0, or an infinity
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float finite_base(float m) { return m == -INFINITY ? 0.f : m; }
+// What scores are taken less of: their maximum m, or the largest finite number where that is infinite (infinity less itself would be NaN; this way the
+// weights' sum is infinite, as it should be, and the output NaN), or 0 where every weight is 0
+__device__ __forceinline__ float finite_base(float m) { return m == -INFINITY ? 0.f : fminf(m, 3.402823466e38f); }
+// factor of what was summed with maximum m where it is now m_new: 1 where they are alike, infinite ones too
+__device__ __forceinline__ float rescale(float m, float m_new, float base) { return m == m_new ? 1.f : pow2(m - base); }
 
 // Values that other blocks (on other dies, with caches of their own) read within the launch: device-scope accesses go to memory
 __device__ __forceinline__ void put2(float* p, float a, float b) {
@@ -136,7 +140,7 @@ struct Sum {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   __device__ __forceinline__ void add(const f32x4& o2, float m2, float l2) {
-    const float m_new = fmaxf(m, m2), base = finite_base(m_new), f = pow2(m - base), h = pow2(m2 - base);
+    const float m_new = fmaxf(m, m2), base = finite_base(m_new), f = rescale(m, m_new, base), h = rescale(m2, m_new, base);
     m = m_new;
     l = l * f + l2 * h;
     o = o * f + o2 * h;
@@ -495,7 +499,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
           }
         const float m_new = fmaxf(m[u], max_of_row(top)), base = finite_base(m_new);
         if (__any(m_new > m[u])) {
-          const float f = pow2(m[u] - base);
+          const float f = rescale(m[u], m_new, base);
           l[u] *= f;
 #pragma unroll
           for (int i = 0; i < NL; ++i) o[u][i] *= f;

@@ -111,3 +111,27 @@ def test_values_that_overflow_the_sum():
     q = torch.zeros((1, 64), dtype=torch.bfloat16, device="cuda")
     out, _ = call(c, q, [64], 1, 1)
     assert np.isposinf(out[0, 0, 0, 9]) and np.isfinite(np.delete(out[0, 0, 0], 9)).all()
+
+
+@pytest.mark.parametrize("per,n_new,L", [(4, 1, 300), (4, 1, 9000), (6, 4, 700), (6, 5, 9000), (16, 5, 2500)])
+def test_scores_of_plus_infinity(per, n_new, L):
+    """A key of +infinity against positive queries: ln sum exp is +infinity, the output inf / inf; against negative ones the weight is 0.  The other sequence
+    and the tokens before keep their bits, and NaN beside +infinity is NaN."""
+    c = filled(BF, [L, 90], 128, 2, 64, seed=4)
+    q = (torch.randn((2 * n_new, 2 * per * 64), generator=torch.Generator().manual_seed(3)) * 0.3).to(torch.bfloat16).cuda()
+    q.view(2, n_new, 2, per, 64)[0, :, 0, :, 7] = torch.tensor([1.0, -1.0] * (per // 2), dtype=torch.bfloat16)
+    clean_out, clean_lse = call(c, q, [L, 90], n_new, 2 * per)
+    pages = c.pages.clone()
+    for at, seen in ((L // 2, 0), (L - 1, n_new - 1)):
+        set_value(c, 0, at, 7, 0x7f80, which=0)
+        out, lse = call(c, q, [L, 90], n_new, 2 * per)
+        rows = lse[0, seen:, :per]
+        assert np.isposinf(rows[:, ::2]).all() and np.isfinite(rows[:, 1::2]).all()
+        assert np.isnan(out[0, seen:, :per:2]).all() and np.isfinite(out[0, seen:, 1:per:2]).all()
+        for a, b in ((out, clean_out), (lse, clean_lse)):
+            assert np.array_equal(a[1], b[1]) and np.array_equal(a[0, :, per:], b[0, :, per:]) and np.array_equal(a[0, :seen], b[0, :seen])
+        c.pages.copy_(pages)
+    set_value(c, 0, L // 2, 7, 0x7f80, which=0)
+    set_value(c, 0, 3, 7, 0x7fc0, which=0)
+    out, lse = call(c, q, [L, 90], n_new, 2 * per)
+    assert np.isnan(lse[0, :, :per]).all() and np.isnan(out[0, :, :per]).all() and np.isfinite(out[1]).all()
