@@ -106,7 +106,7 @@ typedef struct {
   int32_t head_dim;       /* bf16: 64, 96, 128, 192 or 256; e4m3: 64, 128, 192 or 256 */
   int32_t type;           /* SI_KV_* */
   int32_t n_seqs, max_pages;
-} si_cache_t;
+} si_cache_t; /* limits: page_tokens and n_layers up to 65536, n_kv_heads up to 1024, max_pages * page_tokens up to 0x7fff0000 */
 
 /* Element offsets inside a page, from its first: K and V of element `dim` of the token at position t_in_page (host, no GPU needed).
  * Errors: SI_EINVAL (bad descriptor, an index outside it). */
@@ -156,7 +156,8 @@ int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* d
  * Left out with a bit in *status: a sequence outside the table (as if its length were 0), a length that is negative or
  * beyond the table (cut to it), a page outside the pool (its tokens are not seen).
  * Errors: SI_EINVAL (NULL or misaligned pointer: 2 bytes for q and out, 4 for lse and seqs; n_heads not a multiple of n_kv_heads or above 4096;
- * a stride smaller than its row; n_new < 1 or above 65536; window or max_len negative; scale not finite; scratch_bytes too small; layer outside the
+ * a stride smaller than its row; n negative, above 65535, or above n_seqs without seqs; n_new < 1 or above 65536; n * n_kv_heads *
+ * ceil(n_new * n_heads / n_kv_heads / 64) of 2^24 or more; window or max_len negative; scale not finite; scratch_bytes too small; layer outside the
  * cache; bad cache descriptor), SI_EHIP.  n == 0 is a no-op.
  */
 typedef struct {

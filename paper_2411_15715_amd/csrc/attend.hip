@@ -9,6 +9,8 @@
 namespace si {
 namespace {
 
+constexpr int64_t ATTEND_BLOCKS = 1 << 24;  // (a launch has fewer than 2^32 threads)
+
 struct Cut {
   int block_rows, groups, slices, whole, part_rows, last_joins;
   int64_t scratch, part_at;
@@ -38,7 +40,8 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   // are many, longer ones even out too (128 of 1 .. 1000 positions 54 us in slices, 51 whole).
   const bool twice = c.head_dim <= 128 && (k.block_rows > 16 || a.n * units > 256);
   const int most = twice ? 512 : 256, streams = std::max(1, 64 / k.block_rows);
-  k.whole = each <= 20 || (each <= 40 && a.n * units >= 512);
+  // So have so many sequences that a launch could not hold a joining block for each of their rows.
+  k.whole = each <= 20 || (each <= 40 && a.n * units >= 512) || (most / units > 1 && a.n * units * k.part_rows >= ATTEND_BLOCKS);
   const int64_t useful = (a.n * each + 2 * streams - 1) / (2 * streams);
   k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min(most / units, useful));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
@@ -64,9 +67,9 @@ int check_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
     return set_error(SI_EINVAL, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, a->n_heads, c->n_kv_heads);
   if (a->window < 0 || a->max_len < 0) return set_error(SI_EINVAL, "%s: window %d or max_len %d is negative", who, a->window, a->max_len);
   if (!std::isfinite(a->scale)) return set_error(SI_EINVAL, "%s: scale is not finite", who);
-  const Cut k = cut(*c, *a);
-  // (a launch has fewer than 2^32 threads: of the joining kernel, a block for each row)
-  if ((int64_t)c->n_kv_heads * k.groups * std::max<int64_t>(k.slices, (int64_t)a->n * k.part_rows) >= ((int64_t)1 << 24))
+  // (at most so many blocks, in cut() of up to 128 rows, have a slice for each sequence)
+  const int64_t groups = ((int64_t)a->n_new * (a->n_heads / c->n_kv_heads) + 63) / 64;
+  if (std::max(1, a->n) * c->n_kv_heads * groups >= ATTEND_BLOCKS)
     return set_error(SI_EINVAL, "%s: n * n_new * n_heads is too large for one call (%d, %d, %d)", who, a->n, a->n_new, a->n_heads);
   return SI_OK;
 }
