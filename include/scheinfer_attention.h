@@ -125,7 +125,7 @@ int si_kv_offsets(const si_cache_t* cache, int32_t layer, int32_t kv_head, int32
  * projection.  q == NULL: keys and values only.
  * Errors: SI_EINVAL (NULL or misaligned pointer: 2 bytes for rows, 4 for the others; rot_dim odd, negative or beyond head_dim; rot_dim without
  * inv_freq; n_heads not a multiple of n_kv_heads or above 4096; layer outside the cache; bad cache descriptor; more than 2^22 tokens, or more
- * than 2^33 elements of k, in one call), SI_EHIP.  n_tokens == 0 is a no-op.
+ * than 2^33 elements of k, or about 2^38 of q and k (2^35 where rot_dim is no multiple of 16), in one call), SI_EHIP.  n_tokens == 0 is a no-op.
  */
 typedef struct {
   const void* q;         /* bf16 [n_tokens][n_heads][head_dim], or NULL */

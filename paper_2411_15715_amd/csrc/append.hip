@@ -297,8 +297,10 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_append(Args g) 
 
 bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-hipError_t launch_append(const si_cache_t& c, int layer, const si_append_t& a, hipStream_t stream) {
-  Args g{c, a, layer, 1, 1, 0, 0, 1};
+// How a call is cut into blocks; returns their number.
+int64_t cut(Args& g) {
+  const si_cache_t& c = g.c;
+  const si_append_t& a = g.a;
   const int per_head = units_of_head(a.rot_dim, c.head_dim), units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * per_head;
   // A block has up to four units a thread, of one token or of up to 4 where these have few (4099 tokens of 576 units: 51 us with the angles formed
   // by two blocks of a token, 39 by one); with few tokens one unit a thread (what waits there is memory, not the threads)
@@ -309,8 +311,11 @@ hipError_t launch_append(const si_cache_t& c, int layer, const si_append_t& a, h
   g.v_columns = (c.n_kv_heads * c.head_dim + THREADS - 1) / THREADS;
   g.v_blocks = (a.n_tokens + E - 1) / E * g.v_columns;
   g.run = 32 / g.per_block * g.qk_columns;
-  const int64_t blocks = (int64_t)((a.n_tokens + g.per_block - 1) / g.per_block) * g.qk_columns + g.v_blocks;
-  if (c.type == SI_KV_BF16) hipLaunchKernelGGL(k_append<SI_KV_BF16>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
+  return (int64_t)((a.n_tokens + g.per_block - 1) / g.per_block) * g.qk_columns + g.v_blocks;
+}
+
+hipError_t launch_append(const Args& g, int64_t blocks, hipStream_t stream) {
+  if (g.c.type == SI_KV_BF16) hipLaunchKernelGGL(k_append<SI_KV_BF16>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
   else hipLaunchKernelGGL(k_append<SI_KV_E4M3>, dim3((unsigned)blocks), dim3(THREADS), 0, stream, g);
   return hipGetLastError();
 }
@@ -373,9 +378,12 @@ extern "C" int si_cache_append(const si_cache_t* c, int32_t layer, const si_appe
   if (bad(a->k_stride, row_kv) || bad(a->v_stride, row_kv) || (a->q && (bad(a->q_stride, row_q) || bad(a->q_out_stride, row_q))))
     return set_error(SI_EINVAL, "%s: a stride is smaller than its row", who);
   if (a->n_tokens == 0) return SI_OK;
-  // (a launch has fewer than 2^32 threads)
   if (a->n_tokens > (1 << 22) || (int64_t)a->n_tokens * row_kv > ((int64_t)1 << 33)) return set_error(SI_EINVAL, "%s: too many tokens in one call (%d)", who, a->n_tokens);
-  const hipError_t e = launch_append(*c, layer, *a, (hipStream_t)stream);
+  Args g{*c, *a, layer, 1, 1, 0, 0, 1};
+  const int64_t blocks = cut(g);
+  if (blocks >= (1 << 24))  // (a launch has fewer than 2^32 threads)
+    return set_error(SI_EINVAL, "%s: too many tokens and heads in one call (%d, %d)", who, a->n_tokens, a->n_heads);
+  const hipError_t e = launch_append(g, blocks, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "append launch failed: %s", hipGetErrorString(e));
   return SI_OK;
 }

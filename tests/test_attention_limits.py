@@ -21,3 +21,10 @@ def test_prompts_and_batches_are_not_too_large(n, n_new, n_heads, max_len):
                                 dict(n=32768, n_new=8, n_heads=4096, max_len=5)])
 def test_more_blocks_than_a_launch_holds(kw):
     assert "too large" in refused(si.si_attend_scratch_bytes, big_cache(), attend(**kw))
+
+
+@pytest.mark.parametrize("kw", [dict(n_tokens=2_000_000, n_heads=64, rot_dim=254), dict(n_tokens=1 << 22, n_heads=1024, rot_dim=256), dict(n_tokens=1 << 21, n_heads=4096, rot_dim=0)])
+def test_tokens_and_heads_for_more_blocks_than_a_launch_holds(kw):
+    row = kw["n_heads"] * 256
+    c = big_cache(n_kv_heads=1, head_dim=256)
+    assert "too many tokens and heads" in refused(si.si_cache_append, c, 0, append(q_stride=row, q_out_stride=row, k_stride=256, v_stride=256, **kw))
