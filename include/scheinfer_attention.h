@@ -193,7 +193,8 @@ int64_t si_cache_scratch_bytes(const si_cache_t* cache);
 
 /*
  * Cuts sequence seqs[i] to its first keep[i] tokens (keep NULL: to nothing, i.e. frees it): rejected drafts, ended sequences.  Pages
- * that no other sequence shares become free.  A sequence number outside the table or a length above the present one is left out.
+ * that no other sequence shares become free.  A sequence number outside the table or a length above the present one is left out (of a
+ * sequence named twice: the length that the entries before have left it).
  */
 int si_cache_trim(const si_cache_t* cache, const int32_t* seqs, int32_t n, const int32_t* keep, void* stream);
 

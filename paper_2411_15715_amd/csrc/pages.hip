@@ -215,20 +215,34 @@ __device__ bool last_block(BookLds& s, Head* head) {
   return s.arrived == gridDim.x - 1;
 }
 
-__global__ __launch_bounds__(WAVE) void k_trim(si_cache_t c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ keep) {
-  const int seq = seqs[blockIdx.x], lane = threadIdx.x, to = keep ? keep[blockIdx.x] : 0;
-  if (seq < 0 || seq >= c.n_seqs || to < 0) {
-    if (lane == 0) atomicOr(c.status, to < 0 ? SI_CACHE_BAD_LEN : SI_CACHE_BAD_SEQ);
+// A wave for each entry of the list; that of a sequence's first entry takes all of its entries, in list order, so that no two waves write to
+// a sequence and what is reported does not depend on which comes first.  Each entry that is not left out makes the sequence shorter: the pages
+// are dropped together, after the last.
+__global__ __launch_bounds__(WAVE) void k_trim(si_cache_t c, const int32_t* __restrict__ seqs, int n, const int32_t* __restrict__ keep) {
+  const int e = blockIdx.x, seq = seqs[e], lane = threadIdx.x;
+  if (seq < 0 || seq >= c.n_seqs) {
+    if (lane == 0) atomicOr(c.status, keep && keep[e] < 0 ? SI_CACHE_BAD_LEN : SI_CACHE_BAD_SEQ);
     return;
   }
-  // (an exchange, so that a sequence named twice loses its pages once)
-  int old = lane == 0 ? atomicMin(c.lens + seq, to) : 0;
-  old = __builtin_amdgcn_readfirstlane(old);
-  int why = old < to ? SI_CACHE_BAD_LEN : 0;
+  const int old = c.lens[seq];
+  bool earlier = false;
+  for (int i = lane; i < e; i += WAVE) earlier |= seqs[i] == seq;
+  if (__any(earlier)) return;
+  int len = old, why = 0;
+  for (int i0 = e; i0 < n; i0 += WAVE) {
+    const int i = i0 + lane;
+    const bool mine = i < n && seqs[i] == seq;
+    const int to = mine && keep ? keep[i] : 0;
+    for (uint64_t m = __ballot(mine); m; m &= m - 1) {
+      const int k = __builtin_amdgcn_readlane(to, __ffsll((unsigned long long)m) - 1);
+      if (k < 0 || k > len) why |= SI_CACHE_BAD_LEN;
+      else len = k;
+    }
+  }
   const int most = c.max_pages * c.page_tokens;
-  if (old > most) { old = most; why = SI_CACHE_BAD_LEN; }
+  if (old > most) why |= SI_CACHE_BAD_LEN;
   int32_t* row = c.table + (int64_t)seq * c.max_pages;
-  for (int j = ceil_div(min(to, most), c.page_tokens) + lane; j < ceil_div(max(old, 0), c.page_tokens); j += WAVE) {
+  for (int j = ceil_div(min(max(len, 0), most), c.page_tokens) + lane; j < ceil_div(min(max(old, 0), most), c.page_tokens); j += WAVE) {
     const int page = row[j];
     row[j] = -1;
     if (page < 0 || page >= c.n_pages) {
@@ -238,6 +252,7 @@ __global__ __launch_bounds__(WAVE) void k_trim(si_cache_t c, const int32_t* __re
       why |= SI_CACHE_BAD_PAGE;
     }
   }
+  if (lane == 0 && len != old) c.lens[seq] = len;
   if (why) atomicOr(c.status, why);
 }
 
@@ -521,7 +536,7 @@ extern "C" int si_cache_trim(const si_cache_t* c, const int32_t* seqs, int32_t n
   if (int rc = check_moves(c, who)) return rc;
   if (int rc = check_list(seqs, keep, false, n, who)) return rc;
   if (n == 0) return SI_OK;
-  hipLaunchKernelGGL(k_trim, dim3(n), dim3(WAVE), 0, (hipStream_t)stream, *c, seqs, keep);
+  hipLaunchKernelGGL(k_trim, dim3(n), dim3(WAVE), 0, (hipStream_t)stream, *c, seqs, n, keep);
   return done(who);
 }
 
