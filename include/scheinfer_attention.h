@@ -202,8 +202,9 @@ int si_cache_trim(const si_cache_t* cache, const int32_t* seqs, int32_t n, const
  * Adds counts[i] tokens (counts NULL: n_new) to sequence seqs[i] and gives them pages.  A partly filled last page that other
  * sequences share is replaced by a copy first (the last of its sharers keeps it).  The new tokens, in list order and ascending
  * positions, are written to seq_out / pos_out, -1 from there to `capacity`: the arrays that si_cache_append takes (both NULL: not wanted).
- * Nothing is done, seq_out is all -1, and *status has a bit, where a sequence is outside the table or named twice, a length is bad or grows
- * beyond the table's row, more than `capacity` tokens are added, or pages run out (looked at in this order).
+ * Nothing is done, seq_out is all -1, and *status has bits, where a sequence is outside the table or named twice, a length is bad or grows
+ * beyond the table's row, a partly filled last page is outside the pool or has no count, more than `capacity` tokens are added, or pages run out (the
+ * last two are looked at where the others are in order).
  */
 int si_cache_extend(const si_cache_t* cache, const int32_t* seqs, int32_t n, const int32_t* counts, int32_t n_new, int32_t* seq_out, int32_t* pos_out,
                     int32_t capacity, void* stream);
@@ -211,6 +212,8 @@ int si_cache_extend(const si_cache_t* cache, const int32_t* seqs, int32_t n, con
 /*
  * Makes sequence children[i], which has to be empty, a copy of parents[i]: full pages are shared, a partly filled last one is copied (a parent's
  * once read, however many children it has).  A sequence may be the parent of several, but not a parent and a child in one call.
+ * Nothing is done, and *status has a bit, where that is not so or a sequence is outside the table, a length is bad, a page of a parent is outside
+ * the pool or has no count, or pages run out (looked at in this order).
  */
 int si_cache_fork(const si_cache_t* cache, const int32_t* parents, const int32_t* children, int32_t n, void* stream);
 

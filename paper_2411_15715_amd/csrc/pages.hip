@@ -285,8 +285,10 @@ __global__ __launch_bounds__(BOOK) void k_extend(ExtendArgs g) {
         need = ceil_div(len + m, page) - ceil_div(len, page);
         if (m > 0 && len % page > 0) {
           const int last = c.table[(int64_t)seq * c.max_pages + len / page];
-          if (last < 0 || last >= c.n_pages) why = SI_CACHE_BAD_PAGE;
-          else if ((shared = c.refs[last] - 1) > 0) src = last;
+          // (a page with a count of 0 counts as free, and would be given away)
+          const int count = last < 0 || last >= c.n_pages ? 0 : c.refs[last];
+          if (count <= 0) why = SI_CACHE_BAD_PAGE;
+          else if ((shared = count - 1) > 0) src = last;
         }
       }
     }
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(BOOK) void k_fork(ForkArgs g) {
     named = s.put[n];
     for (int f = e; f < named; f += BOOK) {
       const int i = entry_of(s.put, n, f), p = c.table[(int64_t)s.first[i] * c.max_pages + f - s.put[i]];
-      if (p < 0 || p >= c.n_pages) bad_page = 1;
+      if (p < 0 || p >= c.n_pages || c.refs[p] <= 0) bad_page = 1;
     }
     bad_page = __syncthreads_or(bad_page);
     if (bad_page) why = SI_CACHE_BAD_PAGE;
