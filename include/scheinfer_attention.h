@@ -13,6 +13,7 @@
  * Conventions: those of scheinfer.h (codes, si_last_error, bf16 as bit patterns, stream as void*), and
  *  - every pointer inside the descriptors is a DEVICE address, aligned to its element; the descriptors themselves are HOST and are
  *    read during the call only;
+ *  - a call with no rows, tokens, sequences or list entries is a no-op, and the addresses of what is empty may then be NULL;
  *  - no call allocates, copies to or from the host, or waits: every call can be recorded into a HIP graph, and acts on the
  *    descriptors' addresses and on the device's tables as they are when it runs.  Work runs on the current HIP device, which has to be
  *    the one that owns the memory and the stream;

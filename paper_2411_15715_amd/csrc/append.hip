@@ -366,6 +366,7 @@ extern "C" int si_cache_append(const si_cache_t* c, int32_t layer, const si_appe
   if (int rc = check_layer(c, layer, who)) return rc;
   if (!a) return set_error(SI_EINVAL, "%s: descriptor is NULL", who);
   if (a->n_tokens < 0) return set_error(SI_EINVAL, "%s: n_tokens %d", who, a->n_tokens);
+  if (a->n_tokens == 0) return SI_OK;  // (an empty tensor's address may be NULL)
   if (!a->k || !a->v || !a->seq || !a->pos || (a->q && !a->q_out)) return set_error(SI_EINVAL, "%s: k, v, seq, pos or q_out is NULL", who);
   if (a->q && (a->n_heads < 1 || a->n_heads > 4096 || a->n_heads % c->n_kv_heads != 0))
     return set_error(SI_EINVAL, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, a->n_heads, c->n_kv_heads);
@@ -377,7 +378,6 @@ extern "C" int si_cache_append(const si_cache_t* c, int32_t layer, const si_appe
   auto bad = [&](int64_t stride, int64_t row) { return stride < row && !(a->n_tokens <= 1 && stride == 0); };
   if (bad(a->k_stride, row_kv) || bad(a->v_stride, row_kv) || (a->q && (bad(a->q_stride, row_q) || bad(a->q_out_stride, row_q))))
     return set_error(SI_EINVAL, "%s: a stride is smaller than its row", who);
-  if (a->n_tokens == 0) return SI_OK;
   if (a->n_tokens > (1 << 22) || (int64_t)a->n_tokens * row_kv > ((int64_t)1 << 33)) return set_error(SI_EINVAL, "%s: too many tokens in one call (%d)", who, a->n_tokens);
   Args g{*c, *a, layer, 1, 1, 0, 0, 1};
   const int64_t blocks = cut(g);

@@ -88,6 +88,7 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   const char* who = "si_attend";
   if (int rc = check_shape(c, a, who)) return rc;
   if (int rc = check_layer(c, layer, who)) return rc;
+  if (a->n == 0) return SI_OK;  // (an empty tensor's address may be NULL)
   if (!a->q || !a->out) return set_error(SI_EINVAL, "%s: q or out is NULL", who);
   if (misaligned(a->q, 2) || misaligned(a->out, 2) || misaligned(a->lse, 4) || misaligned(a->seqs, 4)) return set_error(SI_EINVAL, "%s: a pointer is not aligned to its element", who);
   if (!a->seqs && a->n > c->n_seqs) return set_error(SI_EINVAL, "%s: n %d of %d sequences", who, a->n, c->n_seqs);
@@ -96,7 +97,6 @@ extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* 
   const Cut k = cut(*c, *a);
   if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
-  if (a->n == 0) return SI_OK;
   AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.block_rows, k.slices, k.whole, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
   g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
   if (k.scratch > 0) {

@@ -322,12 +322,13 @@ bool misaligned(const void* p, int type) { return (reinterpret_cast<uintptr_t>(p
 extern "C" int si_norm(const si_norm_t* a, void* stream) {
   using namespace si;
   if (!a) return set_error(SI_EINVAL, "si_norm: descriptor is NULL");
-  if (!a->r && !a->y) return set_error(SI_EINVAL, "si_norm: neither r nor y");
-  if (!a->r_out && !a->out) return set_error(SI_EINVAL, "si_norm: neither r_out nor out");
   if (a->rows < 0 || a->d < 1 || a->d > SI_NORM_MAX_D) return set_error(SI_EINVAL, "si_norm: bad rows=%d or d=%d (1 .. %d)", a->rows, a->d, SI_NORM_MAX_D);
   if (!std::isfinite(a->eps) || a->eps < 0.f) return set_error(SI_EINVAL, "si_norm: eps has to be finite and not negative");
   for (int k : {a->post, a->pre})
     if (k != SI_NORM_NONE && k != SI_NORM_RMS && k != SI_NORM_MEAN) return set_error(SI_EINVAL, "si_norm: unknown norm %d", k);
+  if (a->rows == 0) return SI_OK;  // (an empty tensor's address may be NULL)
+  if (!a->r && !a->y) return set_error(SI_EINVAL, "si_norm: neither r nor y");
+  if (!a->r_out && !a->out) return set_error(SI_EINVAL, "si_norm: neither r_out nor out");
   if (a->post != SI_NORM_NONE && !a->y) return set_error(SI_EINVAL, "si_norm: post normalises y, which is NULL");
   const struct { const char* name; const void* p; int type; int64_t stride; bool output; } ops[] = {
       {"r", a->r, a->r_type, a->r_stride, false}, {"y", a->y, a->y_type, a->y_stride, false}, {"gate", a->gate, a->gate_type, a->gate_stride, false},
@@ -339,7 +340,6 @@ extern "C" int si_norm(const si_norm_t* a, void* stream) {
     if (misaligned(o.p, o.type)) return set_error(SI_EINVAL, "si_norm: %s is not aligned to its type", o.name);
     if (o.stride < (o.output ? a->d : 0)) return set_error(SI_EINVAL, "si_norm: stride %lld of %s", (long long)o.stride, o.name);
   }
-  if (a->rows == 0) return SI_OK;
   const hipError_t e = launch_norm(*a, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "norm launch failed: %s", hipGetErrorString(e));
   return SI_OK;
