@@ -98,8 +98,8 @@ typedef struct {
   int32_t* lens;          /* [n_seqs] */
   int32_t* refs;          /* [n_pages]; may be NULL for si_cache_append and si_attend */
   int32_t* status;        /* [1] */
-  void* scratch;          /* si_cache_scratch_bytes bytes, 16-byte aligned, zero before the first call that uses it and left so by every
-                             call: the page calls only */
+  void* scratch;          /* si_cache_scratch_bytes bytes, 16-byte aligned, zero before its first use; every call leaves it fit for the next:
+                             the page calls only */
   int32_t n_pages;        /* >= 1 */
   int32_t page_tokens;    /* a multiple of B: 32 (bf16) or 64 (e4m3) */
   int32_t n_layers;
@@ -121,7 +121,8 @@ int si_kv_offsets(const si_cache_t* cache, int32_t layer, int32_t kv_head, int32
  * fp32, rounded once; e4m3: x / scale of the head, cut to +-448, rounded to nearest even (NaN stays NaN).
  * Nothing else of the cache changes: si_cache_extend has given the tokens their pages and counted them.
  * A token with seq -1 is left out (q_out is 0), so that a recorded graph may have more tokens than a step needs.  So is, with
- * a bit in *status, one whose sequence, position or page is not there.  A place that two tokens of a call name gets one of them.
+ * a bit in *status, one whose sequence, position or page is not there.  Each element
+ * of a place that two tokens of a call name is that of one of them, and neighbours need not be of the same (si_cache_extend names no place twice).
  * Strides are in elements between tokens, at least the row they stride (or 0 where there is one token); q, k and v may be slices of one
  * projection.  q == NULL: keys and values only.
  * Errors: SI_EINVAL (NULL or misaligned pointer: 2 bytes for rows, 4 for the others; rot_dim odd, negative or beyond head_dim; rot_dim without
@@ -223,7 +224,7 @@ int si_cache_fork(const si_cache_t* cache, const int32_t* parents, const int32_t
  * `to` is a cache of the same shape but for n_pages (>= m), whose pages, table, lens and refs are written (its status and scratch are not used), or
  * the same cache: then it is packed in place.  Anything between (some arrays shared, pools that overlap) is allowed for whole arrays
  * only: each of to's four is either the cache's own or memory of its own.  n_used, DEVICE [1] or NULL, receives m.  Where m exceeds to's
- * n_pages, nothing else is written.
+ * n_pages, nothing else is written.  (Pools of up to 2^24 pieces of 64 KB, a page counted in whole pieces: SI_EINVAL beyond.)
  */
 int si_cache_compact(const si_cache_t* cache, const si_cache_t* to, int32_t* n_used, void* stream);
 
