@@ -180,9 +180,11 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;
   static constexpr int PIECES = STAGE / 1024 / WAVES;  // loads of a stage by each wave
   // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
-  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 192 and 256 a wave has a SIMD for itself: two do not
-  // fit their registers (192: 64 x 4000 positions 139 us spilling, 121 alone; e4m3 84 and 68), nor two blocks a unit's LDS.
-  static constexpr int WAVES_PER_SIMD = D < 192 ? 2 : 1;
+  // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 192 and 256 a wave of up to 16 rows a block has a SIMD for itself: K
+  // and V on their way do not fit half the registers (192: 64 x 4000 positions 132 us spilling, 122 alone; e4m3 300 and 67).  Blocks of 64
+  // rows have them in the ring (40 rows over 16 x 8000 positions, 192: 90 us in two, 107 alone, e4m3 77 and 85; 256: 111 and 130, 91 and 102);
+  // of those of 32 a unit's LDS holds one.
+  static constexpr int WAVES_PER_SIMD = D < 192 || TILES == 4 ? 2 : 1;
   // Heads of 256 of e4m3 without the ring: K and V of two blocks, sums and weights fill the 256 registers that vector instructions reach.  The next K is
   // asked for after the products with V instead of before, and q and the sums are held where only matrix instructions reach them (64 x 4000
   // positions 86 us; else registers are spilled in the loop, and a reload waits for all loads in flight: 223).
