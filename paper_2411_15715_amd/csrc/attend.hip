@@ -35,17 +35,22 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   // them: 512 sequences of 64 positions 57 -> 38 us) or the waves of a block share their loads and wait for each other (40 rows over
   // 16 x 8000 positions 119 -> 106 us) and two blocks fit a unit.  Else it is one more round of sums to write and read (131071 positions 86
   // against 88 us).  No slice has fewer than two cache blocks a wave.
-  // Short sequences have a block each, without a search and without joining (8 of 517 positions, 17 cache blocks: 15.2 us in slices, 10.3
-  // whole; 15 of 525 .. 1051 e4m3, 30 rows 28.7 and 22.3); a longer one alone is better cut (1000 positions 9.4 us, whole 12.0).  Where there
-  // are many, longer ones even out too (128 of 1 .. 1000 positions 54 us in slices, 51 whole).
   const bool twice = c.head_dim <= 128 && (k.block_rows > 16 || a.n * units > 256);
   const int most = twice ? 512 : 256, streams = std::max(1, 64 / k.block_rows);
+  // Short sequences have a block each, without a search and without joining.  How short goes by the turns that a wave then takes and by the
+  // number of these blocks: few leave most of the chip idle, many even out by themselves.  8 kv heads, us in slices and whole:
+  //   up to 16 rows      1 x 640 (5 turns) 9.0, 8.5;  1 x 900 (8) 9.1, 10.5;  8 x 768 (6) 12.3, 12.3;  8 x 1536 (12) 16.3, 19.9;  32 x 1 .. 2560 (20) 35.7, 35.7;
+  //                      64 x 1 .. 3584 (28) 80.8, 89.1
+  //   more, whose sums   1 x 300 (20 rows, 5 turns) 13.1, 11.7;  1 x 300 (48 rows, 10) 13.3, 16.5;  4 x 1 .. 512 (20 rows, 8) 22.4, 15.2;  8 x 768 (20 rows, 12) 18.5, 19.8;  8 x 1 .. 512 (48 rows, 16) 21.1, 22.0;
+  //   are longer         16 x 1 .. 1792 (20 rows, 28) 36.1, 35.8;  32 x 1280 (48 rows, 40) 52.5, 46.0;  64 x 1 .. 640 (48 rows, 20) 59.4, 33.7
+  const int64_t turns = (each + streams - 1) / streams, blocks = a.n * units;
+  k.whole = turns <= (k.block_rows > 16 ? std::min<int64_t>(5 + blocks / 8, 40) : std::clamp<int64_t>(blocks / 8, 5, 20));
   // So have so many sequences that a launch could not hold a joining block for each of their rows.
-  k.whole = each <= 20 || (each <= 40 && a.n * units >= 512) || (most / units > 1 && a.n * units * k.part_rows >= ATTEND_BLOCKS);
+  if (most / units > 1 && blocks * k.part_rows >= ATTEND_BLOCKS) k.whole = 1;
   const int64_t useful = (a.n * each + 2 * streams - 1) / (2 * streams);
   k.slices = k.whole ? std::max(1, a.n) : (int)std::max<int64_t>(1, std::min(most / units, useful));
   const int64_t join_bytes = (k.slices / std::max(1, a.n) + 1) * k.part_rows * (c.head_dim + 2) * 4ll;
-  k.last_joins = !k.whole && k.slices > 1 && join_bytes <= 64 * 1024 && a.n * units <= ATTEND_COUNTERS;
+  k.last_joins = !k.whole && k.slices > 1 && join_bytes <= 64 * 1024 && blocks <= ATTEND_COUNTERS;
   // Room for as many slices as any call of no more or longer sequences takes, in blocks of up to 64 rows too
   for (int block_rows = std::min(64, k.block_rows); block_rows <= k.block_rows; block_rows *= 2) {
     const int64_t block_units = (int64_t)c.n_kv_heads * ((rows + block_rows - 1) / block_rows), room = std::min((c.head_dim <= 128 ? 512 : 256) / block_units, useful);
