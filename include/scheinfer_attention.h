@@ -148,6 +148,7 @@ int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* d
  *   p <= lens - n_new + j,  and with window > 0 also  p > lens - n_new + j - window,
  * and for every head h, with kv head h / (n_heads / n_kv_heads):
  *   out = softmax over them of (scale q . K) applied to V,   lse = ln sum exp(scale q . K)
+ * Made for a few new tokens over a long cache; whole prompts are taken too.
  * A token that sees nothing (its position is negative: lens < n_new) gets out 0 and lse -infinity, and so does a row all of whose scores are
  * -infinity; a row with a score of +infinity gets out NaN and lse +infinity.  What a token does not see has no part in
  * its output, whatever the pages hold there, NaN and infinities included.  Products are of bf16 operands (e4m3 codes widen to bf16

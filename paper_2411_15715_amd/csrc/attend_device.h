@@ -2,17 +2,21 @@
 //
 // The rows of a block are the query heads that share a kv head, for all new tokens: up to 128 of them.  Per cache block of
 // B tokens a wave forms S^T = K Q^T (matrix instructions with K as the left operand) and O^T += V^T P^T.  The cache holds K and V in the
-// operand order of these instructions, so a wave loads both from memory into the registers that multiply, 16 bytes a lane and
-// 1 KB in a run; and the tokens of a K block are placed so that the scores a lane receives are those of the
-// tokens whose weights it has to hold for the second product: nothing passes through LDS or between lanes but the maximum of a row.
-// Running maximum m and sum l (base 2) per row; the waves of a block and the parts of a sequence are joined by
+// operand order of these instructions, so that 16 bytes a lane and 1 KB in a run are an operand as they come: of up to 16 rows a block from memory
+// straight into the registers that multiply, of more by way of a ring in LDS, which the waves share.  The tokens of a K block are placed so that
+// the scores a lane receives are those of the tokens whose weights it has to hold for the second product: no score or weight passes
+// through LDS or between lanes, only the maximum of a row does.  Running maximum m and sum l (base 2) per row; the waves of a block and the parts of a
+// sequence are joined by
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m)
 // in the order of the parts, so that the result does not depend on who does it.
+// Bound by memory with up to 32 rows of bf16 (131071 positions 85.6 us, 6.3 TB/s; 64 sequences of 1 .. 8000 173 us, 6.2) and one row of e4m3 (32 x 8000 positions
+// 87 us, 6.0); with more rows by the waits for LDS and for each other, vector and matrix instructions of two waves a SIMD (96 rows over 16 x 8000 164 us, half
+// of the waves' time waiting).
 //
 // Who does what: the cache blocks of all sequences, one after the other, are cut into G equal slices, and each block of a kv head takes one:
 // the end of a sequence, some whole ones, the beginning of another, or a piece from the middle of a long one.  Every compute unit has the
-// same to read, however the lengths are spread, and a block leaves at most two unfinished sums.  (A block for each sequence, or for each
-// equal part of the longest: 64 sequences of 1 .. 8000 positions 192 and 178 us, 156 where all have 4000.)
+// same to read, however the lengths are spread, and a block leaves at most two unfinished sums.  (64 sequences of 1 .. 8000 positions, measured
+// when the choice was made: a block for each sequence 192 us, for each equal part of the longest 178, slices 173.)
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -160,11 +164,11 @@ __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv
 template <int N> __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 0xf) | (((N >> 4) & 3) << 14)); }
 
 // TILES waves of a block have 16 NT rows each and go through the same cache blocks; 4 / TILES streams of them take these in turn.  Alone
-// (TILES == 1) a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97).  Several read them from LDS,
+// (TILES == 1) a wave loads K and V into its registers, past the caches (131071 positions 86 us, without the hint 97 .. 101).  Several read them from LDS,
 // into which the block loads each cache block once, without a detour through registers: S stages of a block for each stream.  (Each
 // wave loading for itself, TILES requests for every line at the caches: 24 rows over 16 x 8000 positions 108 us, this way 97.)
-// In blocks of 128 rows a wave has 32, in smaller ones 16: two waves with the
-// same cache block hide each other's waits (20 rows of e4m3 over 29 windows of 9000 positions, 32 a wave and a ring for each wave: 113 us, 16: 91).
+// In blocks of 128 rows a wave has 32, in smaller ones 16: two waves with the same cache block hide each other's waits (before the weights had two
+// operands, 20 rows of e4m3 over 29 windows of 9000 positions, 32 a wave and a ring for each wave: 113 us, 16: 91).
 template <int TYPE, int D, int NT, int TILES> struct Attend {
   static constexpr int ROWS = 16 * NT, BLOCK_ROWS = ROWS * TILES;              // of a wave, of a block
   static constexpr bool RING = TILES > 1;                                     // K and V come by way of LDS
@@ -174,14 +178,14 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   static constexpr int WAVES = ATTEND_WAVES, THREADS = ATTEND_THREADS;
   static constexpr int PAD = D + 4;                                           // (rows of 16 banks more: the four groups of lanes write side by side)
 
-  // A stage of the ring holds a block for each stream, K and V.  (Two blocks a compute unit, where heads are no longer than 128; stages of K and of
+  // A stage of the ring holds a block for each stream, K and V.  (Two blocks a compute unit, but for 32 rows with heads of 192 and 256; stages of K and of
   // V in turn are twice the barriers: 20 rows of e4m3 over 29 windows of 9000 positions 99 us, this way 91.)
   static constexpr int STREAMS = WAVES / TILES, BLOCK_BYTES = 128 * D, STAGE = STREAMS * BLOCK_BYTES;
   static constexpr int S = STAGE > 27000 ? 2 : STAGE > 20000 ? 3 : 4;
   static constexpr int PIECES = STAGE / 1024 / WAVES;  // loads of a stage by each wave
   // Two waves share a SIMD, with 256 registers each; said to the compiler, it also keeps the accumulators out of the registers that only
   // matrix instructions reach (copies to and fro were a fifth of the loop).  With heads of 192 and 256 a wave of up to 16 rows a block has a SIMD for itself: K
-  // and V on their way do not fit half the registers (192: 64 x 4000 positions 132 us spilling, 122 alone; e4m3 300 and 67).  Blocks of 64
+  // and V on their way do not fit half the registers (192: 64 x 4000 positions 132 us spilling, 121 alone; e4m3 300 and 65).  Blocks of 64
   // rows have them in the ring (40 rows over 16 x 8000 positions, 192: 90 us in two, 107 alone, e4m3 77 and 85; 256: 111 and 130, 91 and 102);
   // of those of 32 a unit's LDS holds one.
   static constexpr int WAVES_PER_SIMD = D < 192 || TILES == 4 ? 2 : 1;
@@ -243,8 +247,8 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     else wait_stage<N - 1>(younger);
   }
   static __device__ __forceinline__ uint32_t lds_at(const char* p) { return (uint32_t)(uintptr_t)(const char __attribute__((address_space(3)))*)p; }
-  // N times 16 bytes of LDS, 256 apart, asked for together.  (Left to the compiler each is waited for
-  // by itself: 96 rows over 16 x 8000 positions 164 us, together 136.)
+  // N times 16 bytes of LDS, 256 apart, asked for together.  (Left to the compiler: 40 rows with heads of 192 over 16 x 8000 positions 93 us, this way 90;
+  // heads of 64 and 128 alike.)
   template <int N, int OFFSET> static __device__ __forceinline__ void read_lds(uint32_t at, u32x4* v) {
     if constexpr (N == 4)
       asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"

@@ -305,8 +305,9 @@ hipError_t launch_norm(const si_norm_t& a, hipStream_t stream) {
   if (slots <= 32) return launch<32, 1, 256>(a, {256, 8}, stream);
   if (slots <= 64) return launch<64, 1, 256>(a, {256, 4}, stream);
   auto shape = [&](int n) { return Shape{(slots + WAVE * n - 1) / (WAVE * n) * WAVE, 1}; };
-  // One slot a thread: 4096 x 6144 in 45.1 us, with two 46.6 (more threads hold fewer registers each, and more rows are in flight).  Beyond 12
-  // waves a row's barriers leave too little beside it: 3000 x 8192 with N1 59.4 us with one slot, 45.1 with two (plain: 46.3, 45.5).
+  // One slot a thread: more threads hold fewer registers each, and more rows are in flight.  Beyond 12 waves a row's barriers leave too little
+  // beside it.  25 M elements, bf16 r and fp32 y, us with one slot and with two:
+  //   2048 columns 44.5, 45.5 (with N1 45.9, 50.5);  6144 44.7, 46.4 (50.5, 58.5);  6656 47.8, 46.9 (68.9, 58.4);  8192 46.5, 45.9 (63.9, 55.8)
   if (slots <= 768) return launch<0, 1, 768>(a, shape(1), stream);
   if (slots <= 1024) return launch<0, 2, 512>(a, shape(2), stream);
   if (slots <= 2048) return launch<0, 4, 512>(a, shape(4), stream);
