@@ -45,7 +45,7 @@ extern "C" {
  * N2 reads r' as formed, not as rounded to r_out's type.  Sums, means and r' are fp32; every output is rounded once.
  * Strides are in elements, between the rows of an operand; an input's stride may be 0 (one row for all of them, e.g. a gate that
  * belongs to the layer), an output's at least d.  r_out and out may be r, y or gate themselves (same address, type and
- * stride); other overlaps are not allowed.
+ * stride; another type or stride there is refused); other overlaps are not allowed.
  * Errors: SI_EINVAL (NULL descriptor, neither r nor y, neither output, unknown type or kind, rows < 0, d outside 1 .. SI_NORM_MAX_D, a stride
  * as above, an address not aligned to its type, eps negative or not finite, post without y).  rows == 0 is a no-op.
  */
@@ -133,7 +133,7 @@ typedef struct {
   const void* q;         /* bf16 [n_tokens][n_heads][head_dim], or NULL */
   const void* k;         /* bf16 [n_tokens][n_kv_heads][head_dim] */
   const void* v;
-  void* q_out;           /* bf16 [n_tokens][n_heads][head_dim]; may be q */
+  void* q_out;           /* bf16 [n_tokens][n_heads][head_dim]; may be q, with its stride */
   const int32_t* seq;    /* [n_tokens] */
   const int32_t* pos;
   const float* inv_freq; /* [rot_dim / 2], NULL where rot_dim == 0 */

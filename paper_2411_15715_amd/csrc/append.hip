@@ -378,6 +378,7 @@ extern "C" int si_cache_append(const si_cache_t* c, int32_t layer, const si_appe
   auto bad = [&](int64_t stride, int64_t row) { return stride < row && !(a->n_tokens <= 1 && stride == 0); };
   if (bad(a->k_stride, row_kv) || bad(a->v_stride, row_kv) || (a->q && (bad(a->q_stride, row_q) || bad(a->q_out_stride, row_q))))
     return set_error(SI_EINVAL, "%s: a stride is smaller than its row", who);
+  if (a->q && a->q_out == a->q && a->q_out_stride != a->q_stride && a->n_tokens > 1) return set_error(SI_EINVAL, "%s: q_out is q, with another stride", who);
   if (a->n_tokens > (1 << 22) || (int64_t)a->n_tokens * row_kv > ((int64_t)1 << 33)) return set_error(SI_EINVAL, "%s: too many tokens in one call (%d)", who, a->n_tokens);
   Args g{*c, *a, layer, 1, 1, 0, 0, 1};
   const int64_t blocks = cut(g);

@@ -340,6 +340,10 @@ extern "C" int si_norm(const si_norm_t* a, void* stream) {
     if (!type_ok(o.type)) return set_error(SI_EINVAL, "si_norm: unknown type %d of %s", o.type, o.name);
     if (misaligned(o.p, o.type)) return set_error(SI_EINVAL, "si_norm: %s is not aligned to its type", o.name);
     if (o.stride < (o.output ? a->d : 0)) return set_error(SI_EINVAL, "si_norm: stride %lld of %s", (long long)o.stride, o.name);
+    // (an output in an input's place: with another type or stride, elements that other threads have still to read would be written)
+    for (const auto& in : ops)
+      if (o.output && !in.output && in.p == o.p && (in.type != o.type || (in.stride != o.stride && a->rows > 1)))
+        return set_error(SI_EINVAL, "si_norm: %s is at the address of %s, with another type or stride", o.name, in.name);
   }
   const hipError_t e = launch_norm(*a, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "norm launch failed: %s", hipGetErrorString(e));
