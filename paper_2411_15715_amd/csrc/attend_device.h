@@ -357,7 +357,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
       if (threadIdx.x < 2) {
-        const int seq_i = un_seq[threadIdx.x];
+        const int seq_i = threadIdx.x == 0 ? un_seq[0] : un_seq[1];  // (an index that the compiler knows: no private memory)
         s.arrived[threadIdx.x] = seq_i < 0 ? 0 : __hip_atomic_fetch_add(g.count + seq_i * gridDim.x + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
