@@ -590,15 +590,15 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     };
     // (rows that the call has; what is not finite stays so through every later step, so the end is soon enough to look)
     auto sums_not_finite = [&] {
-      float t = 0.f;
+      f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < NT; ++u)
         if (tok[u] >= 0)
 #pragma unroll
           for (int i = 0; i < NL; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t = fmaf(o[u][i][e], 0.f, t);
-      return (bool)__any(t != 0.f);
+            for (int e = 0; e < 4; ++e) t[e] = fmaf(o[u][i][e], 0.f, t[e]);
+      return (bool)__any(t[0] + t[1] + t[2] + t[3] != 0.f);
     };
 
     clear();
