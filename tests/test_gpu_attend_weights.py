@@ -135,3 +135,23 @@ def test_scores_of_plus_infinity(per, n_new, L):
     set_value(c, 0, 3, 7, 0x7fc0, which=0)
     out, lse = call(c, q, [L, 90], n_new, 2 * per)
     assert np.isnan(lse[0, :, :per]).all() and np.isnan(out[0, :, :per]).all() and np.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("kind,d", [(BF, 96), (BF, 128), (BF, 192), (BF, 256), (F8, 128), (F8, 192), (F8, 256)])
+@pytest.mark.parametrize("per,n_new", [(4, 1), (5, 4), (9, 6), (16, 6)])
+def test_values_that_are_not_finite_in_heads_of_other_sizes(kind, d, per, n_new):
+    """One that all rows see, one that only the last token sees."""
+    lens = [1500, 90]
+    c = filled(kind, lens, 128, 2, d, seed=d)
+    q = (torch.randn((2 * n_new, 2 * per * d), generator=torch.Generator().manual_seed(d)) * 0.3).to(torch.bfloat16).cuda()
+    clean_out, clean_lse = call(c, q, lens, n_new, 2 * per)
+    nan = 0x7f if kind == F8 else 0x7fc0
+    set_value(c, 0, 700, d - 1, nan if kind == F8 else 0x7f80, head=0)
+    set_value(c, 0, lens[0] - 1, 3, nan, head=1)
+    out, lse = call(c, q, lens, n_new, 2 * per)
+    first = out[0, :, :per, d - 1]
+    assert np.isnan(first).all() if kind == F8 else np.isposinf(first).all()
+    assert np.isnan(out[0, n_new - 1, per:, 3]).all()
+    out[0, :, :per, d - 1] = clean_out[0, :, :per, d - 1]
+    out[0, n_new - 1, per:, 3] = clean_out[0, n_new - 1, per:, 3]
+    assert np.array_equal(out, clean_out) and np.array_equal(lse, clean_lse)
