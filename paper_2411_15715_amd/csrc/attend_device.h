@@ -109,6 +109,14 @@ __device__ __forceinline__ float2 get2(const float* p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
+// Which kv head and row group a block has (blockIdx.x): the last rows, which see most, first, and the heads side by side, on the dies in turn (a prompt of
+// 4096 tokens, 32 heads on 8: last rows last, head by head 456 us, this way 276; 8 of 700 138 and 123)
+struct Unit { int kv, group; };
+__device__ __forceinline__ Unit unit_of(const AttendArgs& g) {
+  const int group = blockIdx.x / g.c.n_kv_heads;
+  return Unit{(int)blockIdx.x - group * g.c.n_kv_heads, g.groups - 1 - group};
+}
+
 // What the new tokens t0 .. t1 of a sequence see, in positions and in blocks of B
 struct Span {
   int seq, len, window, first;  // first: where the sight of token 0 ends
@@ -298,7 +306,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   }
 
   static __device__ void run(const AttendArgs& g, Shared& s) {
-    const int block_row0 = blockIdx.x % g.groups * BLOCK_ROWS, row_end = min(g.rows, block_row0 + BLOCK_ROWS);
+    const int block_row0 = unit_of(g).group * BLOCK_ROWS, row_end = min(g.rows, block_row0 + BLOCK_ROWS);
     if (RING && threadIdx.x == 0) s.again = 0;
     const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
@@ -375,7 +383,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   static __device__ __forceinline__ void part(const AttendArgs& g, Shared& s, const Span& sp, int seq_i, int block_row0, int row_end, int b0, int b1, int where_to) {
     const si_cache_t& c = g.c;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), grp = lane / 16, col = lane % 16;
-    const int kv = blockIdx.x / g.groups, per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
+    const int kv = unit_of(g).kv, per = g.a.n_heads / c.n_kv_heads, n_new = g.a.n_new;
     // the block has the rows [block_row0, row_end), this wave ROWS of them from row0 on; STREAMS waves take the cache blocks in turn
     const int stream = wave / TILES, row0 = block_row0 + wave % TILES * ROWS;
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
@@ -749,7 +757,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   }
 
   static __device__ __forceinline__ void join(const AttendArgs& g, int seq_i, int first, int parts, int block_row0, int row_end) {
-    const int kv = blockIdx.x / g.groups, part_floats = g.part_rows * (D + 2);
+    const int kv = unit_of(g).kv, part_floats = g.part_rows * (D + 2);
     const float* sums = g.part + ((int64_t)blockIdx.x * g.slices + first) * 2 * part_floats;
     for (int i = threadIdx.x; i < (row_end - block_row0) * (D / 4); i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
@@ -785,7 +793,7 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   constexpr int LANES = D / 4, SHARES = 256 / LANES;
   __shared__ f32x4 s_o[SHARES][LANES];
   __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
-  const int kv = blockIdx.x / g.groups, seq_i = blockIdx.y, row = blockIdx.x % g.groups * g.block_rows + blockIdx.z;
+  const int kv = unit_of(g).kv, seq_i = blockIdx.y, row = unit_of(g).group * g.block_rows + blockIdx.z;
   typedef const int32_t __attribute__((address_space(4))) constant_t;
   const constant_t* parted = (const constant_t*)(uintptr_t)(g.parted + (int64_t)seq_i * gridDim.x + blockIdx.x);
   const int first = parted[0], parts = parted[1];
