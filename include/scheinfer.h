@@ -265,6 +265,47 @@ int si_route(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_
 int si_route_noalloc(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_routing_out_t* out,
                      void* stream);
 
+/*
+ * Token assignment by scores instead of raw logits.  For the logits x of a token, with b = bias (NULL: 0):
+ *   SI_SCORE_SOFTMAX  s_e = e^(x_e - max x) / sum e^(x - max x), over all E experts      SI_SCORE_SIGMOID  s_e = 1 / (1 + e^(-x_e))
+ *   chosen: the k experts with the largest s_e + b_e (ties: the lower one), in this order
+ *   n_groups > 1: the experts are n_groups runs of E / n_groups neighbours; only those of the top_groups groups with the largest sum of
+ *     their group_best largest s + b (ties: the lower group) can be chosen
+ *   weights: w = scale s (without b), with renorm scale s / (sum of the k chosen s)      (scale 0: 1)
+ * Scores, sums and comparisons are in 64 bits, weights are rounded once.  A logit of -infinity has score 0, and so has every expert of a
+ * token whose logits all are; logits of +infinity share the softmax.  Weights of chosen scores that sum to 0 are 0.  A score that is NaN (of a
+ * NaN, with the softmax of its whole token) is chosen after all others, and its weight is NaN.  k different experts are chosen whatever the logits are.
+ * The rest of the assignment is that of si_route.
+ */
+#define SI_SCORE_SOFTMAX 0
+#define SI_SCORE_SIGMOID 1
+typedef struct {
+  const float* bias;   /* DEVICE f32 [E], or NULL */
+  int32_t score;       /* SI_SCORE_* */
+  int32_t n_groups;    /* 0 or 1: no groups, and the next two are not looked at */
+  int32_t top_groups;
+  int32_t group_best;
+  int32_t renorm;
+  float scale;
+} si_score_t;
+
+/*
+ * The assignment alone, as si_route; out->idx and out->w are needed (their memory is the call's only working memory: nothing is allocated,
+ * any call can be recorded into a HIP graph), the others may be NULL.  Runs on the current HIP device.
+ * Errors: SI_EINVAL (NULL or misaligned pointer, T outside 0 .. 2^24 or T * k of 2^31 or more, E outside 1 .. 256, k outside 1 .. E, unknown
+ * score, scale not finite, n_groups negative or no divisor of E, top_groups or group_best outside their groups, fewer than k experts in top_groups
+ * groups), SI_EHIP.  T == 0 is a no-op.
+ */
+int si_route_scored(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_score_t* score, const si_routing_out_t* out,
+                    void* stream);
+
+/*
+ * Makes later forward calls of the layer, inside a stack too, assign their tokens by these scores (NULL: by raw logits again, the state after
+ * creation).  The descriptor is copied; bias stays the caller's memory and is read by every forward.  Errors: SI_EINVAL as above, SI_ESTATE (a
+ * layer of one expert).
+ */
+int si_layer_set_scores(si_layer_t* layer, const si_score_t* score);
+
 /* Timings and byte counts of the last forward call; synchronises the layer's events. */
 int si_layer_stats(si_layer_t* layer, si_stats_t* out);
 

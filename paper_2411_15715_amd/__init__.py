@@ -22,6 +22,7 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_layer_stats", "si_layer_set_profiling", "si_repack_chunks", "si_cc_compute", "si_layer_destroy", "si_last_error", "si_version",
            "si_stack_create", "si_stack_forward", "si_stack_destroy",
            "si_layer_create_q4", "si_repack_chunks_q4", "si_cc_compute_q4", "si_layer_create_placed", "si_place_experts", "si_layer_resplit",
+           "si_route_scored", "si_layer_set_scores",
            # scheinfer_solver.h
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
@@ -29,6 +30,7 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_norm", "si_kv_offsets", "si_cache_append", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
            "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
+SI_SCORE_SOFTMAX, SI_SCORE_SIGMOID = 0, 1
 SI_F32, SI_BF16 = 0, 1
 SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
 SI_NORM_MAX_D = 32768
@@ -52,6 +54,11 @@ class si_q4_weights_t(ctypes.Structure):
 class si_routing_out_t(ctypes.Structure):
     _fields_ = [("idx", ctypes.c_void_p), ("w", ctypes.c_void_p), ("count", ctypes.c_void_p),
                 ("off", ctypes.c_void_p), ("perm", ctypes.c_void_p), ("inv", ctypes.c_void_p)]
+
+
+class si_score_t(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("score", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_best", ctypes.c_int32), ("renorm", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class si_stats_t(ctypes.Structure):
@@ -162,6 +169,10 @@ def lib():
         L.si_route.argtypes = [vp, i32, i32, i32, ctypes.POINTER(si_routing_out_t), vp]
         L.si_route_noalloc.restype = ctypes.c_int
         L.si_route_noalloc.argtypes = [vp, i32, i32, i32, ctypes.POINTER(si_routing_out_t), vp]
+        L.si_route_scored.restype = ctypes.c_int
+        L.si_route_scored.argtypes = [vp, i32, i32, i32, ctypes.POINTER(si_score_t), ctypes.POINTER(si_routing_out_t), vp]
+        L.si_layer_set_scores.restype = ctypes.c_int
+        L.si_layer_set_scores.argtypes = [vp, ctypes.POINTER(si_score_t)]
         L.si_layer_stats.restype = ctypes.c_int
         L.si_layer_stats.argtypes = [vp, ctypes.POINTER(si_stats_t)]
         L.si_layer_set_profiling.restype = ctypes.c_int
@@ -366,6 +377,16 @@ def si_route(logits_ptr, T, E, k, routing_out, stream=0):
 def si_route_noalloc(logits_ptr, T, E, k, routing_out, stream=0):
     """si_route without any device allocation (fixed scratch; T * k <= SI_ROUTE_NOALLOC_MAX_PAIRS)."""
     _check(lib().si_route_noalloc(logits_ptr, T, E, k, _routing(routing_out), stream))
+
+
+def si_route_scored(logits_ptr, T, E, k, score, routing_out, stream=0):
+    """Token assignment by scores; score: si_score_t, routing_out: dict name -> address (idx and w needed)."""
+    _check(lib().si_route_scored(logits_ptr, T, E, k, ctypes.byref(score), _routing(routing_out), stream))
+
+
+def si_layer_set_scores(layer, score):
+    """Later forwards of the layer choose experts by score (si_score_t; None: by raw logits again)."""
+    _check(lib().si_layer_set_scores(layer, ctypes.byref(score) if score is not None else None))
 
 
 def si_layer_set_profiling(layer, on):

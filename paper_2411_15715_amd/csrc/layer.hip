@@ -257,6 +257,8 @@ struct si_layer {
   CcPool* pool = nullptr;
   // stats
   int profiling = 0;
+  bool scored = false;  // tokens are assigned by `score`
+  si_score_t score{};
   int in_staged = 0;  // the launches being enqueued read a staged piece
   std::vector<hipEvent_t> ev_pool;
   size_t ev_used = 0;
@@ -842,6 +844,17 @@ int si_layer_set_profiling(si_layer_t* L, int32_t on) {
   return SI_OK;
 }
 
+int si_layer_set_scores(si_layer_t* L, const si_score_t* score) {
+  if (!L) return fail(SI_EINVAL, "layer is NULL");
+  if (score) {
+    if (L->E == 1) return fail(SI_ESTATE, "si_layer_set_scores: a layer of one expert chooses none");
+    if (int rc = si::check_score(score, L->E, L->k, "si_layer_set_scores")) return rc;
+    L->score = *score;
+  }
+  L->scored = score != nullptr;
+  return SI_OK;
+}
+
 int si_route(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_routing_out_t* out, void* stream) {
   if (!logits_dev || !out) return fail(SI_EINVAL, "logits_dev or out is NULL");
   if (T < 0 || E < 1 || E > MAX_EXPERTS || k < 1 || k > E) return fail(SI_EINVAL, "bad T=%d E=%d k=%d", T, E, k);
@@ -1034,11 +1047,12 @@ int si_layer_forward(si_layer_t* L, const void* x_dev, const float* logits_dev, 
   const bool dense = E == 1 && !L->has_shared, asked = u.idx || u.w || u.count || u.off || u.perm || u.inv;
   L->plan.dense_T = dense ? T : 0;
   L->plan.dense_x1 = n_x1;
-  bool fuse_route = path == SI_DECODE && resident_only && !dense && T <= FUSED_ROUTE_MAX_T && T * k <= FUSED_ROUTE_MAX_PAIRS;
+  // (Scores have an assignment kernel of their own.)
+  bool fuse_route = path == SI_DECODE && resident_only && !dense && !L->scored && T <= FUSED_ROUTE_MAX_T && T * k <= FUSED_ROUTE_MAX_PAIRS;
   FusedRoute fr{E > 1 ? logits_dev : nullptr, T, E, k, L->has_shared, n_x1, u};
   if (!fuse_route && (!dense || asked)) {
     SegScope sc(L, stream, 0);
-    hipError_t e = launch_route(E > 1 ? logits_dev : nullptr, T, E, k, L->has_shared, n_g, L->plan, u, stream);
+    hipError_t e = launch_route(E > 1 ? logits_dev : nullptr, T, E, k, L->has_shared, n_g, L->plan, u, stream, L->scored ? &L->score : nullptr);
     if (e != hipSuccess) return fail(SI_EHIP, "route launch failed: %s", hipGetErrorString(e));
   }
   // ---- hand-off to the host: the rows of X1 and the assignment go to the CPU for the CC part (Section III-B),

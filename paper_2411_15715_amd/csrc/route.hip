@@ -4,9 +4,12 @@
 // Everything that decides an index is integer or an exact fp32 comparison, so the result does not
 // depend on scheduling.
 #include "si_internal.h"
+#include "si_error.h"
 #include "route_device.h"
+#include "route_scored.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace si {
 
@@ -22,12 +25,30 @@ __device__ __forceinline__ void put_choice(const Plan& p, const RouteOut& u, siz
   if (u.w) u.w[q] = w;
 }
 
+// How a wave chooses the experts of token t: by the raw logits, or by scores (route_scored.h).
+struct ByLogits {
+  struct Lds {};
+  const float* logits;
+  template <class F> __device__ __forceinline__ void choose(int t, int E, int k, int lane, Lds&, F put) const {
+    topk_token(logits + (size_t)t * E, E, k, lane, put);
+  }
+};
+struct ByScores {
+  using Lds = ScoreLds;
+  const float* logits;
+  si_score_t score;
+  template <class F> __device__ __forceinline__ void choose(int t, int E, int k, int lane, Lds& s, F put) const {
+    scored_token(logits + (size_t)t * E, E, k, score, lane, s, put);
+  }
+};
+
 // One wave per token.
-__global__ __launch_bounds__(256) void k_topk(const float* __restrict__ logits, int T, int E, int k, Plan p, RouteOut u) {
+template <class By> __global__ __launch_bounds__(256) void k_topk(By by, int T, int E, int k, Plan p, RouteOut u) {
+  __shared__ typename By::Lds s_by[4];
   const int wv = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
   const int t = blockIdx.x * 4 + wv;
   if (t >= T) return;
-  topk_token(logits + (size_t)t * E, E, k, lane, [&](int s, int e, float w) { put_choice(p, u, (size_t)t * k + s, e, w); });
+  by.choose(t, E, k, lane, s_by[wv], [&](int s, int e, float w) { put_choice(p, u, (size_t)t * k + s, e, w); });
 }
 
 struct AssignLds {
@@ -215,13 +236,14 @@ __global__ __launch_bounds__(256) void k_dense_assign(int T, int n_x1, Plan p, R
 // a reload of the choices, is 4.3 us.  Launches, with the faster selection: 4 tokens, top-8 of 64 experts 11.4 -> 5.2 us; 24 tokens,
 // top-2 of 8 9.1 -> 5.5 (45 tokens, top-3 of 60, in the general kernel: 20.0 -> 9.2).
 constexpr int FEW_PAIRS = WAVE;
-__global__ __launch_bounds__(ROUTE_THREADS) void k_route_few(const float* __restrict__ logits, int T, int E, int k, int has_shared,
-                                                             int n_x1, Plan p, RouteOut u) {
+template <class By>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_route_few(By by, int T, int E, int k, int has_shared, int n_x1, Plan p, RouteOut u) {
   __shared__ int32_t s_idx[FEW_PAIRS];
+  __shared__ typename By::Lds s_by[ROUTE_WAVES];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
   const int n_pairs = T * k, EX = E + (has_shared ? 1 : 0);
   for (int t = wv; t < T; t += blockDim.x / WAVE)
-    topk_token(logits + (size_t)t * E, E, k, lane, [&](int s, int e, float w) {
+    by.choose(t, E, k, lane, s_by[wv], [&](int s, int e, float w) {
       s_idx[t * k + s] = e;
       put_choice(p, u, (size_t)t * k + s, e, w);
     });
@@ -287,13 +309,14 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_few(const float* __rest
 
 // Up to 64 tokens: selection and assignment in one launch.  Wave v of the block takes
 // tokens v, v + 16, ...; the assignment then runs on the whole block.
-__global__ __launch_bounds__(ROUTE_THREADS) void k_route_small(const float* __restrict__ logits, int T, int E, int k,
-                                                               int has_shared, int n_x1, Plan p, RouteOut u) {
+template <class By>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_route_small(By by, int T, int E, int k, int has_shared, int n_x1, Plan p, RouteOut u) {
   __shared__ AssignLds s;
+  __shared__ typename By::Lds s_by[ROUTE_WAVES];
   const int wv = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-  if (logits) {
+  if (by.logits) {
     for (int t = wv; t < T; t += ROUTE_WAVES)
-      topk_token(logits + (size_t)t * E, E, k, lane, [&](int i, int e, float w) { put_choice(p, u, (size_t)t * k + i, e, w); });
+      by.choose(t, E, k, lane, s_by[wv], [&](int i, int e, float w) { put_choice(p, u, (size_t)t * k + i, e, w); });
   } else {
     for (int t = threadIdx.x; t < T; t += ROUTE_THREADS) {
       p.idx[t] = 0; p.w[t] = 1.f;
@@ -326,23 +349,18 @@ hipError_t launch_handoff(const Plan& plan, const uint16_t* x, size_t x_bytes, i
   return hipGetLastError();
 }
 
-hipError_t launch_route(const float* logits, int T, int E, int k, int has_shared, int n_g,
-                        const Plan& plan, const RouteOut& user, hipStream_t stream) {
-  if (T <= 0) return hipSuccess;
-  const int n_x1 = T - n_g;
-  if (!logits && E == 1 && !has_shared) {
-    hipLaunchKernelGGL(k_dense_assign, dim3((T + 255) / 256), dim3(256), 0, stream, T, n_x1, plan, user);
+namespace {
+
+template <class By> hipError_t launch_by(const By& by, int T, int E, int k, int has_shared, int n_x1, const Plan& plan, const RouteOut& user, hipStream_t stream) {
+  if (by.logits && T * k <= FEW_PAIRS) {
+    hipLaunchKernelGGL(k_route_few<By>, dim3(1), dim3(WAVE * std::min(T, ROUTE_WAVES)), 0, stream, by, T, E, k, has_shared, n_x1, plan, user);
     return hipGetLastError();
   }
-  if (logits && T * k <= FEW_PAIRS) {
-    hipLaunchKernelGGL(k_route_few, dim3(1), dim3(WAVE * std::min(T, ROUTE_WAVES)), 0, stream, logits, T, E, k, has_shared, n_x1, plan, user);
+  if (T <= 64 || !by.logits) {
+    hipLaunchKernelGGL(k_route_small<By>, dim3(1), dim3(ROUTE_THREADS), 0, stream, by, T, E, k, has_shared, n_x1, plan, user);
     return hipGetLastError();
   }
-  if (T <= 64 || !logits) {
-    hipLaunchKernelGGL(k_route_small, dim3(1), dim3(ROUTE_THREADS), 0, stream, logits, T, E, k, has_shared, n_x1, plan, user);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(k_topk, dim3((T + 3) / 4), dim3(256), 0, stream, logits, T, E, k, plan, user);
+  hipLaunchKernelGGL(k_topk<By>, dim3((T + 3) / 4), dim3(256), 0, stream, by, T, E, k, plan, user);
   // at most 64 blocks: each counts all pairs
   const int n_pairs = T * k, per_block = (n_pairs + 63) / 64;
   const int span = (per_block + ROUTE_THREADS - 1) / ROUTE_THREADS * ROUTE_THREADS;
@@ -350,4 +368,53 @@ hipError_t launch_route(const float* logits, int T, int E, int k, int has_shared
   return hipGetLastError();
 }
 
+}  // namespace
+
+hipError_t launch_route(const float* logits, int T, int E, int k, int has_shared, int n_g, const Plan& plan, const RouteOut& user, hipStream_t stream,
+                        const si_score_t* score) {
+  if (T <= 0) return hipSuccess;
+  const int n_x1 = T - n_g;
+  if (!logits && E == 1 && !has_shared) {
+    hipLaunchKernelGGL(k_dense_assign, dim3((T + 255) / 256), dim3(256), 0, stream, T, n_x1, plan, user);
+    return hipGetLastError();
+  }
+  return score && logits ? launch_by(ByScores{logits, *score}, T, E, k, has_shared, n_x1, plan, user, stream)
+                         : launch_by(ByLogits{logits}, T, E, k, has_shared, n_x1, plan, user, stream);
+}
+
+int check_score(const si_score_t* s, int E, int k, const char* who) {
+  if (!s) return set_error(SI_EINVAL, "%s: the score's descriptor is NULL", who);
+  if (s->score != SI_SCORE_SOFTMAX && s->score != SI_SCORE_SIGMOID) return set_error(SI_EINVAL, "%s: unknown score %d", who, s->score);
+  if ((reinterpret_cast<uintptr_t>(s->bias) & 3) != 0) return set_error(SI_EINVAL, "%s: bias is not aligned to 4 bytes", who);
+  if (!std::isfinite(s->scale)) return set_error(SI_EINVAL, "%s: scale is not finite", who);
+  if (s->n_groups < 0) return set_error(SI_EINVAL, "%s: n_groups %d", who, s->n_groups);
+  if (s->n_groups > 1) {
+    if (E % s->n_groups != 0) return set_error(SI_EINVAL, "%s: %d experts in %d groups", who, E, s->n_groups);
+    const int of_group = E / s->n_groups;
+    if (s->top_groups < 1 || s->top_groups > s->n_groups || s->group_best < 1 || s->group_best > of_group)
+      return set_error(SI_EINVAL, "%s: top_groups %d of %d, group_best %d of %d", who, s->top_groups, s->n_groups, s->group_best, of_group);
+    if (k > s->top_groups * of_group) return set_error(SI_EINVAL, "%s: %d experts of %d groups of %d", who, k, s->top_groups, of_group);
+  }
+  return SI_OK;
+}
+
 }  // namespace si
+
+extern "C" int si_route_scored(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_score_t* score, const si_routing_out_t* out, void* stream) {
+  using namespace si;
+  const char* who = "si_route_scored";
+  if (T < 0 || T > (1 << 24) || E < 1 || E > MAX_EXPERTS || k < 1 || k > E || (int64_t)T * k >= ((int64_t)1 << 31))
+    return set_error(SI_EINVAL, "%s: bad T=%d E=%d k=%d", who, T, E, k);
+  if (int rc = check_score(score, E, k, who)) return rc;
+  if (!out) return set_error(SI_EINVAL, "%s: out is NULL", who);
+  if (T == 0) return SI_OK;  // (an empty tensor's address may be NULL)
+  if (!logits_dev || !out->idx || !out->w) return set_error(SI_EINVAL, "%s: logits_dev, idx or w is NULL", who);
+  for (const void* p : {(const void*)logits_dev, (const void*)out->idx, (const void*)out->w, (const void*)out->count, (const void*)out->off, (const void*)out->perm, (const void*)out->inv})
+    if ((reinterpret_cast<uintptr_t>(p) & 3) != 0) return set_error(SI_EINVAL, "%s: a pointer is not aligned to its element", who);
+  Plan p{};
+  p.idx = out->idx;
+  p.w = out->w;
+  const hipError_t e = launch_route(logits_dev, T, E, k, 0, 0, p, RouteOut{nullptr, nullptr, out->count, out->off, out->perm, out->inv}, (hipStream_t)stream, score);
+  if (e != hipSuccess) return set_error(SI_EHIP, "route launch failed: %s", hipGetErrorString(e));
+  return SI_OK;
+}

@@ -74,7 +74,9 @@ struct RouteOut {
 
 // route.hip
 hipError_t launch_route(const float* logits, int T, int E, int k, int has_shared, int n_g,
-                        const Plan& plan, const RouteOut& user, hipStream_t stream);
+                        const Plan& plan, const RouteOut& user, hipStream_t stream, const si_score_t* score = nullptr);
+// SI_OK, or an error that names `who`
+int check_score(const si_score_t* score, int E, int k, const char* who);
 
 // Hand-off to the host (layer.hip): the first x_bytes of x, the first n_pairs idx / w and the EX counts and X1 counts of
 // the plan into pinned host memory (hcount: count, then count1).
