@@ -12,7 +12,8 @@
 namespace si {
 
 struct ScoreLds {  // of a wave
-  double c[MAX_EXPERTS];      // then, of the groups, their worth
+  double s[MAX_EXPERTS];
+  uint64_t c[MAX_EXPERTS];    // keys of s + b; then, of the groups, their worth
   uint32_t open[MAX_EXPERTS];
 };
 
@@ -22,10 +23,13 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// order-preserving map to an unsigned integer; NaN: 0, below -infinity
+// order-preserving map to an unsigned integer and back; NaN: 0, below -infinity
 __device__ __forceinline__ uint64_t score_key(double v) {
   const uint64_t u = (uint64_t)__double_as_longlong(v);
   return v != v ? 0 : u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double score_of(uint64_t key) {
+  return __longlong_as_double((long long)(key == 0 ? ~0ull : key >> 63 ? key & ~(1ull << 63) : ~key));
 }
 
 // LDS of a wave: its accesses are in order, only the compiler has to keep it
@@ -34,16 +38,89 @@ __device__ __forceinline__ void wave_lds() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Which groups are open: lds.open[g].  lds.c holds the experts' keys.
+__device__ __forceinline__ void open_groups(int E, const si_score_t& rule, int lane, ScoreLds& lds) {
+  const int n = rule.n_groups, of_group = E / n;
+  uint64_t worth[MAX_EXPERTS / 64];
+  if (rule.group_best <= 2) {
+    // P neighbouring lanes look at a group and keep its two largest keys.  (One lane a group, of 8 with 32 experts each, for 8192 tokens: the launch
+    // 38.9 us, this way and with the rounds below 16.)
+    int P = 1;
+    while (2 * P * n <= 64 && 2 * P <= of_group) P *= 2;
+#pragma unroll
+    for (int i = 0; i < MAX_EXPERTS / 64; ++i) {
+      const int g = (lane + 64 * i) / P;  // (i > 0: P is 1, or there is none)
+      worth[i] = 0;
+      if (64 * i >= n * P) continue;
+      uint64_t a = 0, b = 0;
+      if (g < n)
+        for (int e = lane % P; e < of_group; e += P) {
+          const uint64_t c = lds.c[g * of_group + e];
+          b = max(b, min(a, c));
+          a = max(a, c);
+        }
+      for (int d = 1; d < P; d *= 2) {
+        const uint64_t a2 = __shfl_xor(a, d), b2 = __shfl_xor(b, d);
+        b = max(max(b, b2), min(a, a2));
+        a = max(a, a2);
+      }
+      worth[i] = rule.group_best == 1 ? a : score_key(score_of(a) + score_of(b));
+    }
+    wave_lds();
+#pragma unroll
+    for (int i = 0; i < MAX_EXPERTS / 64; ++i) {
+      const int g = (lane + 64 * i) / P;
+      if (g < n && lane % P == 0 && 64 * i < n * P) lds.c[g] = worth[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MAX_EXPERTS / 64; ++i) {
+      const int g = lane + 64 * i;
+      worth[i] = 0;
+      if (g >= n) continue;
+      // the largest, then the largest after it in the order of (key, place), and so on
+      const uint64_t* c = lds.c + g * of_group;
+      double sum = 0.0;
+      uint64_t last = ~0ull;
+      int last_at = -1;
+      for (int r = 0; r < rule.group_best; ++r) {
+        uint64_t best = 0;
+        int at = of_group;
+        for (int e = 0; e < of_group; ++e) {
+          const bool left = c[e] < last || (c[e] == last && e > last_at);
+          if (left && (at == of_group || c[e] > best)) { best = c[e]; at = e; }
+        }
+        sum += score_of(best);
+        last = best;
+        last_at = at;
+      }
+      worth[i] = score_key(sum);
+    }
+    wave_lds();
+#pragma unroll
+    for (int i = 0; i < MAX_EXPERTS / 64; ++i)
+      if (lane + 64 * i < n) lds.c[lane + 64 * i] = worth[i];
+  }
+  wave_lds();
+  for (int g = lane; g < n; g += 64) {
+    const uint64_t mine = lds.c[g];
+    int before = 0;
+    for (int h = 0; h < n; ++h) before += lds.c[h] > mine || (lds.c[h] == mine && h < g);
+    lds.open[g] = before < rule.top_groups;
+  }
+  wave_lds();
+}
+
 // N experts a lane: lane + 64 i
 template <int N, class F> __device__ __forceinline__ void scored_rounds(const float* __restrict__ l, int E, int k, const si_score_t& rule, int lane, ScoreLds& lds, F put) {
   float x[N];
   double s[N];
   uint64_t key[N];
-  bool in[N];
+  int ex[N];  // the expert of a key, or MAX_EXPERTS: none
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    in[i] = lane + 64 * i < E;
-    x[i] = in[i] ? l[lane + 64 * i] : -INFINITY;
+    ex[i] = lane + 64 * i < E ? lane + 64 * i : MAX_EXPERTS;
+    x[i] = lane + 64 * i < E ? l[lane + 64 * i] : -INFINITY;
   }
   if (rule.score == SI_SCORE_SOFTMAX) {
     uint32_t m = 0;
@@ -66,100 +143,76 @@ template <int N, class F> __device__ __forceinline__ void scored_rounds(const fl
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = 1.0 / (1.0 + exp(-(double)x[i]));
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    key[i] = 0;
+    if (ex[i] == MAX_EXPERTS) continue;
+    key[i] = score_key(s[i] + (rule.bias ? (double)rule.bias[lane + 64 * i] : 0.0));
+    lds.s[lane + 64 * i] = s[i];
+    if (rule.n_groups > 1) lds.c[lane + 64 * i] = key[i];
+  }
+  wave_lds();
   if (rule.n_groups > 1) {
+    open_groups(E, rule, lane, lds);
     const int of_group = E / rule.n_groups;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (in[i]) lds.c[lane + 64 * i] = s[i] + (rule.bias ? (double)rule.bias[lane + 64 * i] : 0.0);
-    wave_lds();
-    uint64_t worth[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int g = lane + 64 * i;
-      worth[i] = 0;
-      if (g >= rule.n_groups) continue;
-      const double* c = lds.c + g * of_group;
-      // the largest, then the largest after it in the order of (value, place), and so on
-      double sum = 0.0;
-      uint64_t last = ~0ull;
-      int last_at = -1;
-      for (int r = 0; r < rule.group_best; ++r) {
-        uint64_t best = 0;
-        int at = of_group;
-        for (int e = 0; e < of_group; ++e) {
-          const uint64_t ke = score_key(c[e]);
-          const bool left = ke < last || (ke == last && e > last_at);
-          if (left && (at == of_group || ke > best)) { best = ke; at = e; }
-        }
-        sum += c[at];
-        last = best;
-        last_at = at;
-      }
-      worth[i] = score_key(sum);
-    }
-    wave_lds();
-    uint64_t* all = reinterpret_cast<uint64_t*>(lds.c);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (lane + 64 * i < rule.n_groups) all[lane + 64 * i] = worth[i];
-    wave_lds();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int g = lane + 64 * i;
-      if (g >= rule.n_groups) continue;
-      int before = 0;
-      for (int h = 0; h < rule.n_groups; ++h) before += all[h] > worth[i] || (all[h] == worth[i] && h < g);
-      lds.open[g] = before < rule.top_groups;
-    }
-    wave_lds();
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (in[i]) in[i] = lds.open[(lane + 64 * i) / of_group] != 0;
+      if (ex[i] < MAX_EXPERTS && !lds.open[ex[i] / of_group]) { key[i] = 0; ex[i] = MAX_EXPERTS; }
   }
-  unsigned long long open[N];  // lanes whose i-th expert may be chosen yet
+  // The keys of a lane in order, (larger key, then lower expert) first, so that a round looks at one of them
+  auto before = [](uint64_t k0, int e0, uint64_t k1, int e1) { return k0 > k1 || (k0 == k1 && e0 < e1); };
+  auto order = [&](int i, int j) {
+    if (before(key[j], ex[j], key[i], ex[i])) {
+      const uint64_t t = key[i]; key[i] = key[j]; key[j] = t;
+      const int e = ex[i]; ex[i] = ex[j]; ex[j] = e;
+    }
+  };
+  if constexpr (N == 2) order(0, 1);
+  if constexpr (N == 4) { order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2); }
+  // k rounds: the largest key of the wave, by its upper half where only one lane has that, then the lowest expert that has it
+  int sel[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    key[i] = in[i] ? score_key(s[i] + (rule.bias ? (double)rule.bias[lane + 64 * i] : 0.0)) : 0;
-    open[i] = __ballot(in[i]);
-  }
-  // k rounds: the largest key of the wave, its upper half first, then the lowest expert that has it
-  double sel_s[N];
-  int sel_e[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) { sel_s[i] = 0.0; sel_e[i] = 0; }
-  double sum = 0.0;
+  for (int i = 0; i < N; ++i) sel[i] = 0;
   for (int r = 0; r < k; ++r) {
-    uint64_t m = key[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) m = max(m, key[i]);
-    const uint32_t hi = wave_max((uint32_t)(m >> 32)), lo = wave_max((uint32_t)(m >> 32) == hi ? (uint32_t)m : 0u);
-    m = (uint64_t)hi << 32 | lo;
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const unsigned long long c = __ballot(key[i] == m) & open[i];
-      if (!found && c) {
-        const int w = __builtin_ctzll(c);
-        const uint64_t bits = (uint64_t)__double_as_longlong(s[i]);
-        const double v = __longlong_as_double((long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bits >> 32), w) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)bits, w)));
-        sum += v;
-#pragma unroll
-        for (int g = 0; g < N; ++g)
-          if (lane + 64 * g == r) { sel_s[g] = v; sel_e[g] = w + 64 * i; }
-        if (lane == w) key[i] = 0;
-        open[i] &= ~(1ull << w);
-        found = true;
-      }
+    const uint32_t hi = (uint32_t)(key[0] >> 32), top = wave_max(hi);
+    unsigned long long who = __ballot(hi == top);
+    if (who & (who - 1)) {
+      const uint32_t lo = (uint32_t)key[0], low = wave_max(hi == top ? lo : 0u);
+      const bool equal = hi == top && lo == low;
+      const uint32_t e = equal ? MAX_EXPERTS - (uint32_t)ex[0] : 0u, first = wave_max(e);  // (of no expert: 0)
+      who = __ballot(equal && e == first);
     }
+    const int w = __builtin_ctzll(who), e = __builtin_amdgcn_readlane(ex[0], w);
+#pragma unroll
+    for (int g = 0; g < N; ++g)
+      if (lane + 64 * g == r) sel[g] = e;
+    if (lane == w) {
+#pragma unroll
+      for (int i = 0; i + 1 < N; ++i) { key[i] = key[i + 1]; ex[i] = ex[i + 1]; }
+      key[N - 1] = 0;
+      ex[N - 1] = MAX_EXPERTS;
+    }
+  }
+  double v[N], sum = 0.0;
+#pragma unroll
+  for (int g = 0; g < N; ++g) {
+    v[g] = lane + 64 * g < k ? lds.s[sel[g]] : 0.0;
+    sum += v[g];
   }
   const double scale = rule.scale == 0.f ? 1.0 : (double)rule.scale;
+  if (rule.renorm) {
+    sum = wave_sum(sum);
+#pragma unroll
+    for (int g = 0; g < N; ++g) v[g] = sum == 0.0 ? 0.0 : v[g] / sum;
+  }
 #pragma unroll
   for (int g = 0; g < N; ++g)
-    if (lane + 64 * g < k) put(lane + 64 * g, sel_e[g], (float)(rule.renorm ? (sum == 0.0 ? 0.0 : sel_s[g] / sum * scale) : sel_s[g] * scale));
+    if (lane + 64 * g < k) put(lane + 64 * g, sel[g], (float)(v[g] * scale));
 }
 
 template <class F> __device__ __forceinline__ void scored_token(const float* __restrict__ l, int E, int k, const si_score_t& rule, int lane, ScoreLds& lds, F put) {
   if (E <= 64) scored_rounds<1>(l, E, k, rule, lane, lds, put);
+  else if (E <= 128) scored_rounds<2>(l, E, k, rule, lane, lds, put);
   else scored_rounds<4>(l, E, k, rule, lane, lds, put);
 }
 
