@@ -143,6 +143,26 @@ typedef struct {
 int si_cache_append(const si_cache_t* cache, int32_t layer, const si_append_t* desc, void* stream);
 
 /*
+ * The same with a norm of every head of q and k before its rotation:
+ *   q_out[i] = R(p) N_q(q[i]),   K of (s, p) = R(p) N_k(k[i]),   V of (s, p) = v[i]
+ * N over the head_dim elements of a head, SI_NORM_RMS or SI_NORM_MEAN as of si_norm; one weight and bias for all heads of q (of k), or with
+ * per_head one for each.  SI_NORM_NONE: the call is si_cache_append.  In fp32 from the values as given, with no rounding between norm and rotation.
+ * Errors: those of si_cache_append, and SI_EINVAL for a NULL norm, unknown kind or type, a weight or bias that is not aligned to its type, eps
+ * negative or not finite.
+ */
+typedef struct {
+  const void* w_q;     /* [head_dim], or [n_heads][head_dim] with per_head, of w_type; NULL: 1 */
+  const void* b_q;     /* the same; NULL: 0 */
+  const void* w_k;     /* [head_dim], or [n_kv_heads][head_dim] */
+  const void* b_k;
+  int32_t w_type;      /* SI_F32 | SI_BF16 */
+  int32_t kind;        /* SI_NORM_* */
+  int32_t per_head;
+  float eps;
+} si_head_norm_t;
+int si_cache_append_normed(const si_cache_t* cache, int32_t layer, const si_append_t* desc, const si_head_norm_t* norm, void* stream);
+
+/*
  * Attention of the last n_new tokens of n sequences over the cache (they are in it: si_cache_append came before).  Row i * n_new + j of q
  * and out is token j of sequence seqs[i], at position lens - n_new + j; it sees the positions p with
  *   p <= lens - n_new + j,  and with window > 0 also  p > lens - n_new + j - window,

@@ -27,7 +27,7 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
-           "si_norm", "si_kv_offsets", "si_cache_append", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
+           "si_norm", "si_kv_offsets", "si_cache_append", "si_cache_append_normed", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
            "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
 SI_SCORE_SOFTMAX, SI_SCORE_SIGMOID = 0, 1
@@ -132,6 +132,10 @@ class si_append_t(ctypes.Structure):
     _fields_ = _fields("q k v q_out seq pos inv_freq", "q_stride k_stride v_stride q_out_stride", "n_tokens n_heads rot_dim rot_pairs")
 
 
+class si_head_norm_t(ctypes.Structure):
+    _fields_ = _fields("w_q b_q w_k b_k", "", "w_type kind per_head", "eps")
+
+
 class si_attend_t(ctypes.Structure):
     _fields_ = _fields("q out lse seqs scratch", "scratch_bytes q_stride out_stride", "n n_new n_heads window max_len", "scale")
 
@@ -231,6 +235,8 @@ def lib():
         L.si_kv_offsets.argtypes = [pc, i32, i32, i32, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]
         L.si_cache_append.restype = ctypes.c_int
         L.si_cache_append.argtypes = [pc, i32, ctypes.POINTER(si_append_t), vp]
+        L.si_cache_append_normed.restype = ctypes.c_int
+        L.si_cache_append_normed.argtypes = [pc, i32, ctypes.POINTER(si_append_t), ctypes.POINTER(si_head_norm_t), vp]
         L.si_attend.restype = ctypes.c_int
         L.si_attend.argtypes = [pc, i32, ctypes.POINTER(si_attend_t), vp]
         L.si_attend_scratch_bytes.restype = i64
@@ -569,6 +575,11 @@ def si_kv_offsets(cache, layer, kv_head, t_in_page, dim):
 def si_cache_append(cache, layer, desc, stream=0):
     """Rotates q and k of new tokens and writes k and v into their pages; cache: si_cache_t, desc: si_append_t."""
     _check(lib().si_cache_append(ctypes.byref(cache), layer, ctypes.byref(desc), stream))
+
+
+def si_cache_append_normed(cache, layer, desc, norm, stream=0):
+    """si_cache_append with a norm of each head of q and k before its rotation; norm: si_head_norm_t."""
+    _check(lib().si_cache_append_normed(ctypes.byref(cache), layer, ctypes.byref(desc), ctypes.byref(norm), stream))
 
 
 def si_attend_scratch_bytes(cache, desc) -> int:

@@ -35,5 +35,6 @@ inline SI_HD int kv_page_of(const si_cache_t& c, int seq, int pos, int& why) {
 // append.hip: SI_OK, or an error that names `who`
 int check_cache(const si_cache_t* c, const char* who);
 int check_layer(const si_cache_t* c, int layer, const char* who);
+int check_append(const si_cache_t* c, int layer, const si_append_t* a, const char* who, bool* nothing);
 
 }  // namespace si
