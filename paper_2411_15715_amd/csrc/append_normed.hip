@@ -3,6 +3,8 @@
 // L lanes have a head, 16 of its elements each (12 of 16 lanes with heads of 192, 6 of 8 with 96): the two vectors of 8 that turn into
 // each other, so that statistics, weights and rotation meet in registers and nothing is read twice.  Sums are over the 16 elements of a lane, then
 // over neighbouring lanes; the second moment of a norm about the mean is taken about the mean.  v goes its way as without the norm.
+// Bound by memory, as the append without a norm: 4099 tokens of 64 + 8 heads of 128 (160 MB) into e4m3 39.0 us, 4.1 TB/s (without norm 37.6); in
+// between, by the waves that fit: with 150 registers, the weights of q and k among them, 66 us, with 64 forced 46.  8 tokens: 4.7 us in the kernel.
 #include "si_error.h"
 #include "append_device.h"
 
@@ -31,32 +33,35 @@ template <int L> __device__ __forceinline__ float sum_of(float v) {
   return v;
 }
 
-// 8 weights as loaded
-struct Weights { u32x4 v[2]; };
-__device__ __forceinline__ Weights load_weights(const void* w, int type, int at) {
-  Weights r;
-  if (type == SI_BF16) {
-    r.v[0] = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(w) + at);
-    r.v[1] = u32x4{0, 0, 0, 0};
-  } else {
-    r.v[0] = *reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(w) + at);
-    r.v[1] = *reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(w) + at + 4);
-  }
-  return r;
+__device__ __forceinline__ float weight_at(const void* w, int type, int at) {
+  return type == SI_BF16 ? widen(static_cast<const uint16_t*>(w)[at]) : static_cast<const float*>(w)[at];
 }
-__device__ __forceinline__ void widen_weights(const Weights& w, int type, float (&f)[8]) {
+__device__ __forceinline__ void weights_at(const void* w, int type, int at, float (&f)[8]) {
   if (type == SI_BF16) {
-    widen8(w.v[0], f);
+    const u32x4 v = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(w) + at);
+    widen8(v, f);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w.v[i / 4][i % 4]);
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 v = *reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(w) + at + 4 * h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[4 * h + i] = __uint_as_float(v[i]);
+    }
   }
 }
+// The lanes of a head (of one wave) exchange by way of LDS, whose accesses are in order: only the compiler has to keep it
+__device__ __forceinline__ void wave_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
 
-template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int block) {
+// GENERAL: each head has weights of its own, or the halves of the rotated part do not begin at a vector of 8, so that the other element of a
+// pair is in another lane.  Else the weights that all heads share lie in LDS, in fp32, and a lane has both elements of its pairs.
+template <int TYPE, int L, bool GENERAL> __device__ void normed_part(const NormedArgs& na, int block) {
   __shared__ float2 s_turn[MAX_TOKENS][MAX_ANGLES];
   __shared__ Token s_token[MAX_TOKENS];
-  __shared__ float s_x[THREADS / L][16 * L];  // heads whose halves of a rotated part do not begin at a vector
+  __shared__ float s_x[GENERAL ? THREADS / L : 1][GENERAL ? 16 * L : 1];
+  __shared__ __align__(16) float s_w[2][GENERAL ? 4 : 16 * L], s_b[2][GENERAL ? 4 : 16 * L];  // of q, of k
   constexpr int E = TYPE == SI_KV_E4M3 ? 16 : 8;
   const Args& g = na.g;
   const si_append_t& a = g.a;
@@ -65,7 +70,7 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
   const int t0 = block / g.qk_columns * g.per_block, n = min(g.per_block, a.n_tokens - t0), column = block % g.qk_columns;
   const int n_heads = a.q ? a.n_heads : 0, heads = n_heads + g.c.n_kv_heads;
   const int span = (heads + g.qk_columns - 1) / g.qk_columns, h0 = column * span, width = max(0, min(heads, h0 + span) - h0), all = width * n * L;
-  const bool here = 16 * j < d, by_halves = !a.rot_pairs && rot % 16 == 0, shifted = !a.rot_pairs && rot % 16 != 0;
+  const bool here = 16 * j < d, by_halves = !GENERAL && !a.rot_pairs;
   // first elements of this lane's two vectors
   const int d0 = by_halves && j < rot / 16 ? 8 * j : 16 * j, d1 = by_halves && j < rot / 16 ? 8 * j + half : 16 * j + 8;
 
@@ -90,6 +95,13 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
   };
   Unit next;
   if (tid < all) next = fetch(tid);
+  if constexpr (!GENERAL)
+    for (int i = tid; i < 2 * d; i += THREADS) {
+      const int which = i >= d, at = i - which * d;
+      const void *w = which ? nm.w_k : nm.w_q, *b = which ? nm.b_k : nm.b_q;
+      s_w[which][at] = w ? weight_at(w, nm.w_type, at) : 1.f;
+      s_b[which][at] = b ? weight_at(b, nm.w_type, at) : 0.f;
+    }
   for (int i = tid; i < n * half; i += THREADS) s_turn[i / half][i % half] = turn(a.pos[t0 + i / half], a.inv_freq[i % half]);
   if (tid < n) {
     const int seq = a.seq[t0 + tid], pos = a.pos[t0 + tid];
@@ -130,25 +142,54 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += x[i] * x[i] + y[i] * y[i];
     const float rs = rsqrtf(sum_of<L>(here ? sum : 0.f) * per_d + nm.eps);
-    const void *w = is_q ? nm.w_q : nm.w_k, *b = is_q ? nm.b_q : nm.b_k;
-    const int w_at = nm.per_head ? head * d : 0;
+    if (here) {
+      if constexpr (GENERAL) {
+        const void *w = is_q ? nm.w_q : nm.w_k, *b = is_q ? nm.b_q : nm.b_k;
+        const int first = nm.per_head ? head * d : 0;
+        auto take = [&](int at, float (&v)[8]) {
+          float t[8];
+          if (w) {
+            weights_at(w, nm.w_type, first + at, t);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { x[i] *= rs; y[i] *= rs; }
-    if (here && w) {
-      float wx[8], wy[8];
-      widen_weights(load_weights(w, nm.w_type, w_at + d0), nm.w_type, wx);
-      widen_weights(load_weights(w, nm.w_type, w_at + d1), nm.w_type, wy);
+            for (int i = 0; i < 8; ++i) v[i] *= t[i];
+          }
+          if (b) {
+            weights_at(b, nm.w_type, first + at, t);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { x[i] *= wx[i]; y[i] *= wy[i]; }
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+          }
+        };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x[i] *= rs; y[i] *= rs; }
+        take(d0, x);
+        take(d1, y);
+      } else {
+        const float *w = s_w[!is_q], *b = s_b[!is_q];
+        const bool biased = (is_q ? nm.b_q : nm.b_k) != nullptr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x[i] = x[i] * rs * w[d0 + i]; y[i] = y[i] * rs * w[d1 + i]; }
+        if (biased)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) { x[i] += b[d0 + i]; y[i] += b[d1 + i]; }
+      }
     }
-    if (here && b) {
-      float bx[8], by[8];
-      widen_weights(load_weights(b, nm.w_type, w_at + d0), nm.w_type, bx);
-      widen_weights(load_weights(b, nm.w_type, w_at + d1), nm.w_type, by);
+    if constexpr (GENERAL) {
+      float* row = s_x[tid / L];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { x[i] += bx[i]; y[i] += by[i]; }
-    }
-    if (by_halves) {
+      for (int i = 0; i < 8; ++i) { row[d0 + i] = x[i]; row[d1 + i] = y[i]; }
+      wave_lds();
+      for (int u = j; u < half; u += L) {
+        const float2 cs = s_turn[k.t][u];
+        const int i0 = a.rot_pairs ? 2 * u : u, i1 = a.rot_pairs ? 2 * u + 1 : u + half;
+        const float p = row[i0], q = row[i1];
+        row[i0] = p * cs.x - q * cs.y;
+        row[i1] = q * cs.x + p * cs.y;
+      }
+      wave_lds();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { x[i] = row[d0 + i]; y[i] = row[d1 + i]; }
+      wave_lds();
+    } else if (by_halves) {
       if (j < rot / 16) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -158,7 +199,7 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
           y[i] = q * cs.x + p * cs.y;
         }
       }
-    } else if (a.rot_pairs) {
+    } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float& p = i < 4 ? x[(2 * i) % 8] : y[(2 * i) % 8];
@@ -170,24 +211,6 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
           q = q0 * cs.x + p0 * cs.y;
         }
       }
-    } else if (shifted) {
-      // the other element of a pair is in another lane: by way of LDS, which the lanes of a head (of one wave) share
-      float* row = s_x[tid / L];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { row[d0 + i] = x[i]; row[d1 + i] = y[i]; }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-      __builtin_amdgcn_wave_barrier();
-      auto turned = [&](int dim, float own) {
-        if (dim >= rot) return own;
-        const bool second = dim >= half;
-        const float other = row[second ? dim - half : dim + half];
-        const float2 cs = s_turn[k.t][second ? dim - half : dim];
-        return second ? own * cs.x + other * cs.y : own * cs.x - other * cs.y;
-      };
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { x[i] = turned(d0 + i, x[i]); y[i] = turned(d1 + i, y[i]); }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-      __builtin_amdgcn_wave_barrier();
     }
     if (!here) continue;
     if (is_q) {
@@ -202,19 +225,26 @@ template <int TYPE, int L> __device__ void normed_part(const NormedArgs& na, int
   }
 }
 
-template <int TYPE, int L> __global__ __launch_bounds__(THREADS) void k_append_normed(NormedArgs na) {
+template <int TYPE, int L, bool GENERAL> __global__ __launch_bounds__(THREADS) void k_append_normed(NormedArgs na) {
   const Args& g = na.g;
   if ((int)blockIdx.x < g.v_blocks) v_part<TYPE>(g, blockIdx.x);
-  else normed_part<TYPE, L>(na, on_one_die(blockIdx.x - g.v_blocks, gridDim.x - g.v_blocks, g.run));
+  else {
+    const int block = on_one_die(blockIdx.x - g.v_blocks, gridDim.x - g.v_blocks, g.run);
+    normed_part<TYPE, L, GENERAL>(na, block);
+  }
 }
 
-// How a call is cut into blocks (as without the norm: up to four heads' shares a thread, one with few tokens); returns their number.
+// How a call is cut into blocks; returns their number.
 int64_t cut(Args& g, int lanes) {
   const si_cache_t& c = g.c;
   const si_append_t& a = g.a;
-  const int units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * lanes, want = THREADS * (a.n_tokens >= 256 ? 4 : 1);
+  const int units = ((a.q ? a.n_heads : 0) + c.n_kv_heads) * lanes;
+  // A block has the heads of up to 4 tokens, whose angles and weights are formed once, as long as there are some 1000 blocks: 4099 tokens of 576 lanes in
+  // blocks of 1, 2, 4 tokens 40.7, 40.2, 39.0 us (e4m3), by three blocks a token 54.8; 1931 of 256 lanes 14.2, 13.4, 15.6.  With few tokens a
+  // lane has one head (what waits there is memory).
+  const int want = THREADS * (a.n_tokens >= 256 ? 9 : 1);
   if (units >= want) g.qk_columns = (units + want - 1) / want;
-  else if (a.n_tokens >= 256) g.per_block = std::min(MAX_TOKENS, want / units);
+  else if (a.n_tokens >= 256) g.per_block = std::clamp(a.n_tokens / 960, 1, std::min(MAX_TOKENS, want / units));
   const int E = kv_vec(c.type);
   g.v_columns = (c.n_kv_heads * c.head_dim + THREADS - 1) / THREADS;
   g.v_blocks = (a.n_tokens + E - 1) / E * g.v_columns;
@@ -222,11 +252,11 @@ int64_t cut(Args& g, int lanes) {
   return (int64_t)((a.n_tokens + g.per_block - 1) / g.per_block) * g.qk_columns + g.v_blocks;
 }
 
-template <int TYPE> hipError_t launch(const NormedArgs& na, int lanes, int64_t blocks, hipStream_t stream) {
+template <int TYPE, bool GENERAL> hipError_t launch(const NormedArgs& na, int lanes, int64_t blocks, hipStream_t stream) {
   const dim3 grid((unsigned)blocks);
-  if (lanes == 4) hipLaunchKernelGGL((k_append_normed<TYPE, 4>), grid, dim3(THREADS), 0, stream, na);
-  else if (lanes == 8) hipLaunchKernelGGL((k_append_normed<TYPE, 8>), grid, dim3(THREADS), 0, stream, na);
-  else hipLaunchKernelGGL((k_append_normed<TYPE, 16>), grid, dim3(THREADS), 0, stream, na);
+  if (lanes == 4) hipLaunchKernelGGL((k_append_normed<TYPE, 4, GENERAL>), grid, dim3(THREADS), 0, stream, na);
+  else if (lanes == 8) hipLaunchKernelGGL((k_append_normed<TYPE, 8, GENERAL>), grid, dim3(THREADS), 0, stream, na);
+  else hipLaunchKernelGGL((k_append_normed<TYPE, 16, GENERAL>), grid, dim3(THREADS), 0, stream, na);
   return hipGetLastError();
 }
 
@@ -254,7 +284,9 @@ extern "C" int si_cache_append_normed(const si_cache_t* c, int32_t layer, const 
   const int64_t blocks = cut(na.g, lanes);
   if (blocks >= (1 << 24))  // (a launch has fewer than 2^32 threads)
     return set_error(SI_EINVAL, "%s: too many tokens and heads in one call (%d, %d)", who, a->n_tokens, a->n_heads);
-  const hipError_t e = (c->type == SI_KV_BF16 ? launch<SI_KV_BF16> : launch<SI_KV_E4M3>)(na, lanes, blocks, (hipStream_t)stream);
+  const bool general = n->per_head || (!a->rot_pairs && a->rot_dim % 16 != 0);
+  const auto f = c->type == SI_KV_BF16 ? (general ? launch<SI_KV_BF16, true> : launch<SI_KV_BF16, false>) : (general ? launch<SI_KV_E4M3, true> : launch<SI_KV_E4M3, false>);
+  const hipError_t e = f(na, lanes, blocks, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "append launch failed: %s", hipGetErrorString(e));
   return SI_OK;
 }
