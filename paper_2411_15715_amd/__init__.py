@@ -28,7 +28,9 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
            "si_norm", "si_kv_offsets", "si_cache_append", "si_cache_append_normed", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
-           "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact"]
+           "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact",
+           # scheinfer_sample.h
+           "si_sample", "si_sample_scratch_bytes"]
 SI_MAX_EDGE_POINTS, SI_PROFILE_MAX_SIZES = 24, 12
 SI_SCORE_SOFTMAX, SI_SCORE_SIGMOID = 0, 1
 SI_F32, SI_BF16 = 0, 1
@@ -36,6 +38,7 @@ SI_NORM_NONE, SI_NORM_RMS, SI_NORM_MEAN = 0, 1, 2
 SI_NORM_MAX_D = 32768
 SI_KV_BF16, SI_KV_E4M3 = 0, 1
 SI_CACHE_MAX_LIST = 1024
+SI_SAMPLE_MAX_VOCAB, SI_SAMPLE_MAX_ROWS = 1 << 20, 1 << 16
 SI_CACHE_BAD_SEQ, SI_CACHE_BAD_LEN, SI_CACHE_BAD_PAGE, SI_CACHE_NO_PAGES, SI_CACHE_NO_ROOM = 1, 2, 4, 8, 16
 
 
@@ -138,6 +141,10 @@ class si_head_norm_t(ctypes.Structure):
 
 class si_attend_t(ctypes.Structure):
     _fields_ = _fields("q out lse seqs scratch", "scratch_bytes q_stride out_stride", "n n_new n_heads window max_len", "scale")
+
+
+class si_sample_t(ctypes.Structure):
+    _fields_ = _fields("logits temperature top_k top_p min_p u token prob kept scratch", "scratch_bytes stride", "rows vocab type")
 
 
 SI_K_NAMES = ["route", "decode_gateup", "decode_down", "decode_combine", "prefill_gateup", "prefill_down",
@@ -251,6 +258,10 @@ def lib():
         L.si_cache_fork.argtypes = [pc, vp, vp, i32, vp]
         L.si_cache_compact.restype = ctypes.c_int
         L.si_cache_compact.argtypes = [pc, pc, vp, vp]
+        L.si_sample.restype = ctypes.c_int
+        L.si_sample.argtypes = [ctypes.POINTER(si_sample_t), vp]
+        L.si_sample_scratch_bytes.restype = i64
+        L.si_sample_scratch_bytes.argtypes = [ctypes.POINTER(si_sample_t)]
         _lib = L
     return _lib
 
@@ -618,3 +629,15 @@ def si_cache_fork(cache, parents, children, n, stream=0):
 def si_cache_compact(cache, to, n_used=None, stream=0):
     """Packs the pages in use into the pool of `to` (or in place, to = cache)."""
     _check(lib().si_cache_compact(ctypes.byref(cache), ctypes.byref(to), n_used, stream))
+
+
+# ---------------------------------------------------------------- scheinfer_sample.h
+def si_sample(desc, stream=0):
+    """One token for each row of logits, by temperature, top_k, top_p, min_p and a random number a row; desc: si_sample_t."""
+    _check(lib().si_sample(ctypes.byref(desc), stream))
+
+
+def si_sample_scratch_bytes(desc) -> int:
+    n = lib().si_sample_scratch_bytes(ctypes.byref(desc))
+    _check(min(n, SI_OK))
+    return n

@@ -1,0 +1,702 @@
+// The next token of a row of logits (scheinfer_sample.h has the formulas), in one launch.
+//
+// A block takes a chunk of a row and leaves its maximum, where the row needs it the sum of e^((l - max) / T) in 64 bits, and for top_k the maxima of
+// runs of 32 elements; the block of a row that finishes last does the rest, from the caches.  What can be left is cut down before anything is put in
+// order: with n runs or more the top k lie at or above the k-th largest of the runs' maxima, and a token of less than (1 - top_p) S / vocab cannot be
+// needed for a share of top_p.  Few tokens beyond that bound are sorted in LDS.  Many are counted and summed in LDS by the leading bits of an
+// order-preserving key, the bin with the border again, until what it holds can be sorted.  Weights are integers (2^62 / vocab or more for the
+// largest), so that sums in any order are the same.
+#include "si_internal.h"
+#include "si_error.h"
+#include "scheinfer_attention.h"
+#include "scheinfer_sample.h"
+#include "route_device.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace si {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+
+constexpr int THREADS = 1024, WAVES = THREADS / 64;
+constexpr int EACH = 8;                    // neighbouring elements of a thread
+constexpr int CHUNK = THREADS * EACH;
+constexpr int MAX_CHUNKS = SI_SAMPLE_MAX_VOCAB / CHUNK;
+constexpr int RUNS = THREADS / 4;          // of a chunk, 4 threads each
+constexpr int BINS = 2048, LIST = 2048;    // two a thread
+
+struct Args {
+  si_sample_t a;
+  int chunks;
+  int shift;       // a weight of 1 is 2^shift
+  uint32_t* count; // [rows] chunks done; 0 between calls
+  double* sum;     // [rows][chunks]
+  float* top;      // [rows][chunks]
+  uint32_t* n;     // [rows][chunks] elements above -infinity
+  float* runs;     // [rows][chunks * RUNS]
+};
+
+struct Shared {
+  union {
+    struct { uint64_t w[BINS]; uint32_t n[BINS]; } hist;
+    uint64_t list[LIST];
+  };
+  uint64_t part[MAX_CHUNKS * WAVES];  // sums of runs of 512 elements
+  uint64_t wave_a[WAVES], wave_b[WAVES];
+  double pow2[256];                   // 2^(i / 256)
+  double wave_d[WAVES];
+  float wave_f[WAVES];
+  uint64_t found[4];
+  uint32_t counter, last;
+};
+
+// what other blocks read within the launch goes past the caches of this die
+template <class T> __device__ __forceinline__ void put(T* p, T v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+__device__ __forceinline__ float a_little_below(double v) {
+  const float f = (float)v;
+  return f - fabsf(f) * 1e-6f - 1e-30f;
+}
+__device__ __forceinline__ uint64_t composite(uint32_t hi, uint32_t lo) { return (uint64_t)hi << 32 | lo; }
+
+// Elements of a thread one after the other: eight series at once do not fit the registers of 16 waves
+__device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
+
+// sum over the block; before: of the threads before this one
+__device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t& before, uint64_t (&waves)[WAVES]) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint64_t x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint64_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  before = x - v;
+  x = waves[lane % WAVES];
+  const uint64_t own = x;
+#pragma unroll
+  for (int d = 1; d < WAVES; d *= 2) {
+    const uint64_t y = __shfl_up(x, d, WAVES);
+    if (lane % WAVES >= d) x += y;
+  }
+  before += __shfl(x - own, wave);
+  return __shfl(x, WAVES - 1);
+}
+__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ double block_sum(double v, Shared& s) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) s.wave_d[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = s.wave_d[threadIdx.x % WAVES];
+#pragma unroll
+  for (int d = WAVES / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ float block_max(float v, Shared& s) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) s.wave_f[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = s.wave_f[threadIdx.x % WAVES];
+#pragma unroll
+  for (int d = WAVES / 2; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+template <int TYPE> struct Row {
+  const Args& g;
+  Shared& s;
+  const char* logits;
+  int vocab, row, tid;
+  float top;        // the row's largest (in the first pass the chunk's)
+  double rate;      // 256 log2(e) / T
+
+  // 2^shift e^((l - top) / T) = 2^(shift + n / 256) 2^(f / 256) with n the integer next to 256 log2(e) (l - top) / T and |f| <= 1/2: a table of 256 and four
+  // terms of the series, some 2^-52 of the value off.  What is as large as the largest has 2^shift, infinite or not; -infinity has 0 at any temperature.
+  __device__ __forceinline__ double weight(float l, int shift) const {
+    const double y = fmax(((double)l - (double)top) * rate, -3e5), r = rint(y), z = (y - r) * 0.0027076061740622863;
+    const int n = (int)r;
+    const double e = ldexp(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0), (n >> 8) + shift);
+    return l == top ? ldexp(1.0, shift) : l == -INFINITY ? 0.0 : e;
+  }
+
+  // EACH elements from `at` on, NaN and what is beyond the row as -infinity
+  struct Raw { u32x4 v[TYPE == SI_BF16 ? 1 : 2]; };
+  __device__ __forceinline__ void load(int at, float (&l)[EACH]) const {
+    if (at + EACH <= vocab) {
+      if constexpr (TYPE == SI_BF16) {
+        const u32x4 v = *reinterpret_cast<const u32x4_a2*>(logits + (int64_t)at * 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { l[2 * i] = __uint_as_float(v[i] << 16); l[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+      } else {
+        const u32x4 v = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4), w = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4 + 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { l[i] = __uint_as_float(v[i]); l[4 + i] = __uint_as_float(w[i]); }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        l[i] = -INFINITY;
+        if (at + i < vocab) {
+          if constexpr (TYPE == SI_BF16) l[i] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(logits)[at + i] << 16);
+          else l[i] = reinterpret_cast<const float*>(logits)[at + i];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+  }
+  __device__ __forceinline__ uint64_t whole(float l) const {
+    const double v = weight(l, g.shift);
+    const uint32_t hi = (uint32_t)(v * 0x1p-32);
+    return composite(hi, (uint32_t)fma(-0x1p32, (double)hi, v));
+  }
+
+  // f(first element, its EACH elements) for all of the row
+  template <class F> __device__ __forceinline__ void each(F f) const {
+    for (int r = 0; r < g.chunks; ++r) {
+      float l[EACH];
+      const int at = r * CHUNK + tid * EACH;
+      load(at, l);
+      f(at, l);
+    }
+  }
+
+  // What a token adds where the row is gone through in ascending index
+  enum { SAME, NUMBER, WEIGHT };  // 1 with this key; of what is left, 1 or its weight
+  struct Left {
+    uint32_t key, index;  // the last that is left
+    double least;         // and what a weight has to reach (0: nothing)
+  };
+  __device__ __forceinline__ uint64_t adds(int what, const Left& left, float l, int i) const {
+    const uint32_t key = route_key(l);
+    if (l == -INFINITY) return 0;
+    if (what == SAME) return key == left.key;
+    if (key < left.key || (key == left.key && (uint32_t)i > left.index)) return 0;
+    if (left.least > 0.0 && weight(l, 0) < left.least) return 0;
+    return what == NUMBER ? 1 : whole(l);
+  }
+  // Their sums over runs of 512 tokens of the rounds [r0, r1), into s.part; returns the sum of all
+  __device__ __forceinline__ uint64_t add_up(int r0, int r1, int what, const Left& left) const {
+    __syncthreads();
+    for (int r = r0; r < r1; ++r) {
+      float l[EACH];
+      const int at = r * CHUNK + tid * EACH;
+      load(at, l);
+      uint64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
+      sum = wave_total(sum);
+      if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = sum;
+    }
+    __syncthreads();
+    const int parts = (r1 - r0) * WAVES;
+    uint64_t before;
+    return scan((2 * tid < parts ? s.part[2 * tid] : 0) + (2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0), before, s.wave_a);
+  }
+  // The first token at which the sum is above `target` (below the sum of all), after add_up with the same
+  __device__ __forceinline__ int locate(int r0, int r1, int what, const Left& left, uint64_t target) const {
+    const int parts = (r1 - r0) * WAVES, lane = tid % 64;
+    const uint64_t p0 = 2 * tid < parts ? s.part[2 * tid] : 0, p1 = 2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0;
+    uint64_t before;
+    scan(p0 + p1, before, s.wave_a);
+    if (before <= target && target < before + p0 + p1) {
+      const bool second = target >= before + p0;
+      s.found[0] = 2 * tid + second;
+      s.found[1] = target - before - (second ? p0 : 0);
+    }
+    __syncthreads();
+    const int run = (int)s.found[0];
+    uint64_t rest = s.found[1];
+    if (tid < 64) {
+      float l[EACH];
+      const int at = r0 * CHUNK + run * 64 * EACH + lane * EACH;
+      load(at, l);
+      uint64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
+      uint64_t x = sum;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+      }
+      x -= sum;
+      if (x <= rest && rest < x + sum) {
+        int token = -1;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          x += adds(what, left, l[i], at + i);
+          if (token < 0 && x > rest) token = at + i;
+          one_by_one();
+        }
+        s.found[2] = token;
+      }
+    }
+    __syncthreads();
+    return (int)s.found[2];
+  }
+  __device__ __forceinline__ float logit(int i) const {
+    float v;
+    if constexpr (TYPE == SI_BF16) v = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(logits)[i] << 16);
+    else v = reinterpret_cast<const float*>(logits)[i];
+    return v;
+  }
+
+  // the list's first n entries in descending order (n <= LIST); every thread's part is in LDS before and after
+  __device__ __forceinline__ int sort(int n) const {
+    int size = 64;
+    while (size < n) size *= 2;
+    __syncthreads();
+    for (int i = n + tid; i < size; i += THREADS) s.list[i] = 0;
+    for (int k = 2; k <= size; k *= 2)
+      for (int j = k / 2; j > 0; j /= 2) {
+        __syncthreads();
+        if (2 * tid < size) {
+          const int i = 2 * tid - tid % j, o = i + j;  // (of 2 j neighbours, those of the first half)
+          const uint64_t a = s.list[i], b = s.list[o];
+          const bool down = (i & k) == 0;
+          if ((a < b) == down) { s.list[i] = b; s.list[o] = a; }
+        }
+      }
+    __syncthreads();
+    return size;
+  }
+
+  // elements with a key in [lo, hi] into the list, as (key, ~index); returns their number, which may be above LIST
+  __device__ __forceinline__ int collect(uint32_t lo, uint32_t hi) const {
+    __syncthreads();
+    if (tid == 0) s.counter = 0;
+    __syncthreads();
+    each([&](int at, const float (&l)[EACH]) {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const uint32_t key = route_key(l[i]);
+        const bool in = key >= lo && key <= hi && l[i] > -INFINITY;
+        if (in) {
+          const uint32_t to = atomicAdd(&s.counter, 1u);
+          if (to < LIST) s.list[to] = composite(key, ~(uint32_t)(at + i));
+        }
+      }
+    });
+    __syncthreads();
+    return (int)s.counter;
+  }
+
+  struct Border { uint32_t key, index; uint64_t n, w; };  // the last token left, and how many they are with it and their sum
+
+  // Border of the first token at which the number (by_n) or the sum of those up to it reaches `need`, among keys of [lo, hi]: those above hi do not exist
+  __device__ __forceinline__ Border border(uint32_t lo, uint32_t hi, bool by_n, uint64_t need) const {
+    uint64_t n_above = 0, w_above = 0;
+    uint32_t inside;
+    for (;;) {
+      const uint32_t width = hi - lo;
+      const int drop = max(0, 32 - __clz((int)width) - 11);  // (at most BINS bins of 2^drop keys)
+      __syncthreads();
+      for (int i = tid; i < BINS; i += THREADS) { s.hist.w[i] = 0; s.hist.n[i] = 0; }
+      __syncthreads();
+      each([&](int, const float (&l)[EACH]) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          const uint32_t key = route_key(l[i]);
+          if (key >= lo && key <= hi && l[i] > -INFINITY) {
+            const uint32_t b = (hi - key) >> drop;
+            atomicAdd(&s.hist.n[b], 1u);
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist.w[b]), (unsigned long long)whole(l[i]));
+          }
+          one_by_one();
+        }
+      });
+      if (tid == 0) s.found[0] = ~0ull;
+      __syncthreads();
+      const uint64_t n0 = s.hist.n[2 * tid], n1 = s.hist.n[2 * tid + 1], w0 = s.hist.w[2 * tid], w1 = s.hist.w[2 * tid + 1];
+      uint64_t n_before, w_before;
+      const uint64_t n_all = scan(n0 + n1, n_before, s.wave_a), w_all = scan(w0 + w1, w_before, s.wave_b);
+      n_before += n_above;
+      w_before += w_above;
+      const uint64_t goal = by_n ? min(need, n_above + n_all) : min(need, w_above + w_all);
+      const uint64_t x0 = by_n ? n_before : w_before, d0 = by_n ? n0 : w0, d1 = by_n ? n1 : w1;
+      if (x0 < goal && goal <= x0 + d0 + d1) {
+        const bool second = goal > x0 + d0;
+        s.found[0] = 2 * tid + second;
+        s.found[1] = n_before + (second ? n0 : 0);
+        s.found[2] = w_before + (second ? w0 : 0);
+        s.found[3] = second ? n1 : n0;
+      }
+      __syncthreads();
+      const uint32_t bin = (uint32_t)s.found[0];
+      n_above = s.found[1];
+      w_above = s.found[2];
+      inside = (uint32_t)s.found[3];
+      need = goal;
+      hi -= bin << drop;
+      lo = max(lo, hi - ((1u << drop) - 1));
+      if (inside <= LIST || drop == 0) break;
+    }
+    Border r;
+    if (inside <= LIST) {
+      const int n = collect(lo, hi);
+      sort(n);
+      uint64_t e[2], w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        e[i] = 2 * tid + i < n ? s.list[2 * tid + i] : 0;
+        w[i] = 2 * tid + i < n ? whole(value_of((uint32_t)(e[i] >> 32))) : 0;
+      }
+      uint64_t before;
+      scan(w[0] + w[1], before, s.wave_a);
+      before += w_above;
+      // (the bin holds the border: one of its entries reaches the goal)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint64_t at = n_above + 2 * tid + i + 1;
+        const bool here = 2 * tid + i < n && (by_n ? at == need : before < need && need <= before + w[i]);
+        if (here) {
+          s.found[0] = e[i];
+          s.found[1] = at;
+          s.found[2] = before + w[i];
+        }
+        before += w[i];
+      }
+      __syncthreads();
+      r = Border{(uint32_t)(s.found[0] >> 32), ~(uint32_t)s.found[0], s.found[1], s.found[2]};
+    } else {  // more tokens of one logit than the list holds: as many as are needed, from the lowest index
+      const uint64_t each_w = whole(value_of(lo));
+      const uint64_t k = by_n ? need - n_above : (need - w_above + each_w - 1) / each_w;
+      const Left same{lo, 0, 0.0};
+      add_up(0, g.chunks, SAME, same);
+      const int at = locate(0, g.chunks, SAME, same, k - 1);
+      r = Border{lo, (uint32_t)at, n_above + k, w_above + k * each_w};
+    }
+    __syncthreads();
+    return r;
+  }
+
+  __device__ __forceinline__ void write(int token, double prob, int kept) const {
+    if (tid != 0) return;
+    g.a.token[row] = token;
+    if (g.a.prob) g.a.prob[row] = (float)prob;
+    if (g.a.kept) g.a.kept[row] = kept;
+  }
+};
+
+template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) {
+  __shared__ Shared s;
+  const int row = blockIdx.x / g.chunks, chunk = blockIdx.x % g.chunks, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const si_sample_t& a = g.a;
+  constexpr int BYTES = TYPE == SI_BF16 ? 2 : 4;
+  const float t = a.temperature ? a.temperature[row] : 1.f;
+  const bool greedy = !(t > 0.f);
+  const int k = a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.vocab ? a.top_k[row] : 0;
+  const float p_given = a.top_p ? a.top_p[row] : 1.f, m_given = a.min_p ? a.min_p[row] : 0.f;
+  const bool by_p = p_given < 1.f, by_m = m_given > 0.f;
+  const double p = fmaxf(p_given, 0.f), least = fminf(m_given, 1.f);
+  const bool summed = !greedy && k == 0 && (by_p || !by_m);
+  Row<TYPE> R{g, s, static_cast<const char*>(a.logits) + (int64_t)row * a.stride * BYTES, a.vocab, row, tid, 0.f, greedy ? 0.0 : 369.3299304675746 / (double)t};
+  if (tid < 256) s.pow2[tid] = exp2(tid / 256.0);
+
+  {
+    float l[EACH];
+    R.load(chunk * CHUNK + tid * EACH, l);
+    float top = l[0];
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      top = fmaxf(top, l[i]);
+      n += __popcll(__ballot(l[i] > -INFINITY));
+    }
+    if (k > 0) {
+      float run = fmaxf(top, __shfl_xor(top, 1));
+      run = fmaxf(run, __shfl_xor(run, 2));
+      if (lane % 4 == 0) put(g.runs + ((int64_t)row * g.chunks + chunk) * RUNS + tid / 4, run);
+    }
+    if (tid == 0) s.counter = 0;
+    top = block_max(top, s);
+    double sum = 0.0;
+    if (summed) {
+      R.top = top;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) { sum += R.weight(l[i], 0); one_by_one(); }
+      sum = block_sum(sum, s);
+    }
+    if (lane == 0) atomicAdd(&s.counter, n);
+    __syncthreads();
+    if (tid == 0) {
+      const int64_t at = (int64_t)row * g.chunks + chunk;
+      put(g.top + at, top);
+      put(g.n + at, s.counter);
+      put(g.sum + at, sum);
+    }
+  }
+  // all of this block's values have reached memory before it is counted
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) {
+    s.last = __hip_atomic_fetch_add(g.count + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)g.chunks - 1;
+    if (s.last) put(g.count + row, 0u);
+  }
+  __syncthreads();
+  if (!s.last) return;
+
+  // The row's largest, its number of tokens, and its sum
+  const int64_t first = (int64_t)row * g.chunks;
+  const float chunk_top = tid < g.chunks ? get(g.top + first + tid) : -INFINITY;
+  const float top = block_max(chunk_top, s);
+  uint64_t before;
+  const uint64_t n_all = scan(tid < g.chunks ? get(g.n + first + tid) : 0u, before, s.wave_a);
+  if (n_all == 0) { R.write(-1, 0.0, 0); return; }
+  R.top = top;
+  const uint32_t top_key = route_key(top);
+  const float u = a.u[row];
+  const double one = ldexp(1.0, g.shift);
+  // How the row is gone through in the end, and with which target
+  int r0 = 0, r1 = g.chunks, what = R.WEIGHT;
+  typename Row<TYPE>::Left left{route_key(-3.402823466e38f), 0xffffffffu, by_m ? least : 0.0};
+  double sum = 0.0, rest = 0.0;
+  int kept = (int)n_all;
+  const bool all_left = !greedy && k == 0 && !by_p && !by_m;
+  auto drawn = [&](uint64_t all) { return !(u > 0.f) ? 0 : u >= 1.f ? all - 1 : min((uint64_t)((double)u * (double)all), all - 1); };
+  if (greedy) {
+    // in the first chunk that has it
+    const unsigned long long has = __ballot(chunk_top == top);
+    __syncthreads();
+    if (lane == 0) s.wave_a[wave] = has ? wave * 64 + __builtin_ctzll(has) : ~0ull;
+    __syncthreads();
+#pragma unroll 1
+    for (int w = WAVES - 1; w >= 0; --w) r0 = s.wave_a[w] != ~0ull ? (int)s.wave_a[w] : r0;
+    r1 = r0 + 1;
+    what = R.SAME;
+    left.key = top_key;
+    kept = 1;
+  }
+  if (summed) {
+    const double share = tid < g.chunks ? get(g.sum + first + tid) * R.weight(chunk_top, 0) : 0.0;
+    sum = block_sum(share, s);
+    if (all_left) {
+      // the chunk in which u falls
+      double x = share;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const double y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+      }
+      __syncthreads();
+      if (lane == 63) s.wave_d[wave] = x;
+      if (tid == 0) s.found[0] = 0;
+      __syncthreads();
+      double base = 0.0;
+      for (int w = 0; w < wave; ++w) base += s.wave_d[w];
+      const double begin = base + x - share, target = !(u > 0.f) ? 0.0 : u >= 1.f ? sum : (double)u * sum;
+      // (the last that begins at or before the target and is not empty: sums of doubles may leave a gap between two)
+      if (share > 0.0 && begin <= target) atomicMax(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)tid);
+      __syncthreads();
+      r0 = (int)s.found[0];
+      r1 = r0 + 1;
+      if (tid == r0) s.wave_d[0] = target - begin;
+      __syncthreads();
+      rest = fmax(s.wave_d[0], 0.0);
+    }
+  }
+  if (!greedy && !all_left) {
+  // What can be left lies at or above `bound`
+  float bound = -3.402823466e38f;
+  if (k > 0) {
+    // the k-th largest of the runs' maxima, by 22 leading bits of its key (a little below it)
+    const int runs = g.chunks * RUNS;
+    uint32_t lo = 0;
+    if (k <= runs) {
+      uint32_t need = k;
+      for (int level = 0; level < 2; ++level) {
+        __syncthreads();
+        for (int i = tid; i < BINS; i += THREADS) s.hist.n[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < runs; i += THREADS) {
+          const uint32_t key = route_key(get(g.runs + (int64_t)row * runs + i));
+          if (level == 0) atomicAdd(&s.hist.n[2047 - (key >> 21)], 1u);
+          else if ((key >> 21) == (lo >> 21)) atomicAdd(&s.hist.n[2047 - ((key >> 10) & 2047)], 1u);
+        }
+        __syncthreads();
+        const uint32_t n0 = s.hist.n[2 * tid], n1 = s.hist.n[2 * tid + 1];
+        uint64_t x;
+        scan(n0 + n1, x, s.wave_a);
+        if (x < need && need <= x + n0 + n1) {
+          const bool second = need > x + n0;
+          s.found[0] = 2047 - (2 * tid + second);
+          s.found[1] = need - x - (second ? n0 : 0);
+        }
+        __syncthreads();
+        lo |= (uint32_t)s.found[0] << (level == 0 ? 21 : 10);
+        need = (uint32_t)s.found[1];
+      }
+      bound = fmaxf(bound, value_of(lo));
+    }
+  } else if (by_p) {
+    const double c = (1.0 - p) * (1.0 - 1e-6) * sum / a.vocab;
+    if (c > 0.0 && c < 1.0 && top < INFINITY) bound = fmaxf(bound, a_little_below((double)top + log(c) * (double)t));
+  }
+  // (with both top_k and top_p the sum of all k is needed, those below min_p too)
+  if (by_m && !(k > 0 && by_p) && top < INFINITY) bound = fmaxf(bound, a_little_below((double)top + log(least) * (double)t));
+  bound = fminf(bound, top);
+  const uint32_t bound_key = route_key(bound);
+
+  // Few: in order, all at once
+  const int few = k > 0 && k > LIST ? LIST + 1 : R.collect(bound_key, top_key);
+  if (few <= LIST) {
+    R.sort(few);
+    uint64_t e[2], w[2];
+    bool fine[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      e[i] = 2 * tid + i < few ? s.list[2 * tid + i] : 0;
+      const float l = value_of((uint32_t)(e[i] >> 32));
+      w[i] = 2 * tid + i < few && (k == 0 || 2 * tid + i < k) ? R.whole(l) : 0;
+      fine[i] = 2 * tid + i < few && (k == 0 || 2 * tid + i < k) && (!by_m || R.weight(l, 0) >= least);
+    }
+    uint64_t x;
+    const uint64_t all = scan(w[0] + w[1], x, s.wave_a);
+    if (by_p) {
+      const double whole_sum = k > 0 ? (double)all : sum * one;
+      const double goal = p * whole_sum;
+      // (left while the sum before it has not reached the goal)
+      fine[0] = fine[0] && (2 * tid == 0 || (double)x < goal);
+      fine[1] = fine[1] && (double)(x + w[0]) < goal;
+    }
+    uint64_t unused;
+    kept = (int)scan((uint64_t)fine[0] + fine[1], unused, s.wave_b);
+    // in ascending index: what is left are the first `kept` of the list
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (fine[i]) s.list[2 * tid + i] = e[i] << 32 | e[i] >> 32;
+    R.sort(kept);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      e[i] = 2 * tid + i < kept ? s.list[2 * tid + i] : 0;
+      w[i] = 2 * tid + i < kept ? R.whole(value_of((uint32_t)e[i])) : 0;
+    }
+    const uint64_t total = scan(w[0] + w[1], x, s.wave_a);
+    const uint64_t target = drawn(total);
+    if (x <= target && target < x + w[0] + w[1]) {
+      const bool second = target >= x + w[0];
+      s.found[0] = second ? e[1] : e[0];
+      s.found[1] = second ? w[1] : w[0];
+    }
+    __syncthreads();
+    R.write((int)~(uint32_t)(s.found[0] >> 32), (double)s.found[1] / (double)total, kept);
+    return;
+  }
+  // Many: the border by number, then by sum
+  uint64_t w_all = (uint64_t)(sum * one);
+  for (int by_n = 1; by_n >= 0; --by_n) {
+    if (by_n ? k == 0 : !by_p) continue;
+    const auto b = R.border(bound_key, top_key, by_n, by_n ? (uint64_t)k : max((uint64_t)1, (uint64_t)ceil(p * (double)w_all)));
+    left.key = b.key;
+    left.index = b.index;
+    kept = (int)b.n;
+    w_all = b.w;
+  }
+  if (by_m) kept = (int)R.add_up(0, g.chunks, R.NUMBER, left);
+  }
+  uint64_t total = R.add_up(r0, r1, what, left);
+  uint64_t target = greedy ? 0 : drawn(total);
+  if (all_left) {
+    if (total > 0) {
+      target = u >= 1.f ? total - 1 : min((uint64_t)(rest * one), total - 1);
+    } else {  // (a chunk of weights that are all below the smallest integer)
+      r0 = 0;
+      r1 = g.chunks;
+      total = R.add_up(r0, r1, what, left);
+      target = drawn(total);
+    }
+  }
+  const int at = R.locate(r0, r1, what, left, target);
+  const double w = R.weight(R.logit(at), 0);
+  R.write(at, greedy ? 1.0 : all_left ? w / sum : w * one / (double)total, kept);
+}
+
+bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+int check(const si_sample_t* a, const char* who) {
+  if (!a) return set_error(SI_EINVAL, "%s: descriptor is NULL", who);
+  if (a->type != SI_F32 && a->type != SI_BF16) return set_error(SI_EINVAL, "%s: unknown type %d", who, a->type);
+  if (a->rows < 0 || a->rows > SI_SAMPLE_MAX_ROWS || a->vocab < 1 || a->vocab > SI_SAMPLE_MAX_VOCAB) return set_error(SI_EINVAL, "%s: rows %d, vocab %d", who, a->rows, a->vocab);
+  if ((int64_t)a->rows * ((a->vocab + CHUNK - 1) / CHUNK) >= (1 << 22)) return set_error(SI_EINVAL, "%s: too many rows in one call (%d of %d)", who, a->rows, a->vocab);
+  return SI_OK;
+}
+
+// Places in the scratch; returns its size
+int64_t lay_out(const si_sample_t& a, Args* g) {
+  const int64_t chunks = (a.vocab + CHUNK - 1) / CHUNK, n = a.rows * chunks;
+  char* p = static_cast<char*>(a.scratch);
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    char* q = p + at;
+    at += (bytes + 15) / 16 * 16;
+    return q;
+  };
+  // (the counters first, for any number of rows: they stay where they are, and 0, in calls of other sizes)
+  uint32_t* count = reinterpret_cast<uint32_t*>(take(4ll * SI_SAMPLE_MAX_ROWS));
+  double* sum = reinterpret_cast<double*>(take(8 * n));
+  float* top = reinterpret_cast<float*>(take(4 * n));
+  uint32_t* each = reinterpret_cast<uint32_t*>(take(4 * n));
+  float* runs = reinterpret_cast<float*>(take(4 * n * RUNS));
+  if (g) {
+    g->chunks = (int)chunks;
+    g->count = count;
+    g->sum = sum;
+    g->top = top;
+    g->n = each;
+    g->runs = runs;
+  }
+  return at;
+}
+
+}  // namespace
+}  // namespace si
+
+extern "C" int64_t si_sample_scratch_bytes(const si_sample_t* a) {
+  using namespace si;
+  if (int rc = check(a, "si_sample_scratch_bytes")) return rc;
+  return lay_out(*a, nullptr);
+}
+
+extern "C" int si_sample(const si_sample_t* a, void* stream) {
+  using namespace si;
+  const char* who = "si_sample";
+  if (int rc = check(a, who)) return rc;
+  if (a->rows == 0) return SI_OK;  // (an empty tensor's address may be NULL)
+  if (!a->logits || !a->u || !a->token || !a->scratch) return set_error(SI_EINVAL, "%s: logits, u, token or scratch is NULL", who);
+  if (misaligned(a->logits, a->type == SI_F32 ? 4 : 2) || misaligned(a->temperature, 4) || misaligned(a->top_k, 4) || misaligned(a->top_p, 4) || misaligned(a->min_p, 4) ||
+      misaligned(a->u, 4) || misaligned(a->token, 4) || misaligned(a->prob, 4) || misaligned(a->kept, 4) || misaligned(a->scratch, 16))
+    return set_error(SI_EINVAL, "%s: a pointer is not aligned to its element (scratch: to 16 bytes)", who);
+  if (a->stride < a->vocab && a->stride != 0) return set_error(SI_EINVAL, "%s: stride %lld of rows of %d", who, (long long)a->stride, a->vocab);
+  Args g{};
+  g.a = *a;
+  const int64_t bytes = lay_out(*a, &g);
+  if (a->scratch_bytes < bytes) return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed", who, (long long)bytes);
+  int log2 = 0;
+  while ((1 << log2) < a->vocab) ++log2;
+  g.shift = 62 - log2;
+  const dim3 grid((unsigned)(a->rows * g.chunks));
+  if (a->type == SI_BF16) hipLaunchKernelGGL(k_sample<SI_BF16>, grid, dim3(THREADS), 0, (hipStream_t)stream, g);
+  else hipLaunchKernelGGL(k_sample<SI_F32>, grid, dim3(THREADS), 0, (hipStream_t)stream, g);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return set_error(SI_EHIP, "sample launch failed: %s", hipGetErrorString(e));
+  return SI_OK;
+}

@@ -1,0 +1,248 @@
+"""si_sample against the formulas on numpy's doubles.
+
+Token and number of tokens left have to be equal: both sides go by sums of 64 bits (the kernel's weights are rounded to 2^-42 of the largest or finer), and
+the random numbers of the tests stay 10^-7 of the sum away from every border between two tokens, limits 10^-9 (checked here, on the CPU).
+prob: one rounding to fp32 and the sum's 2^-25."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_15715_amd as si
+
+pytestmark = pytest.mark.gpu
+NONE = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+
+
+def one_row(l, t, k, p, least, u):
+    """token, prob, kept; u None: a random number in the middle of a token's share, by its own choice"""
+    l = np.where(np.isnan(l), -np.inf, l.astype(np.float64))
+    if not np.any(l > -np.inf):
+        return -1, 0.0, 0
+    if not t > 0:
+        return int(np.argmax(l)), 1.0, 1
+    top = l.max()
+    with np.errstate(invalid="ignore"):
+        w = np.where(l == top, 1.0, np.where(l == -np.inf, 0.0, np.exp((l - top) / t)))
+    order = np.argsort(-l, kind="stable")
+    order = order[l[order] > -np.inf]
+    if k > 0:
+        order = order[:k]
+    if p < 1:
+        sums = np.cumsum(w[order])
+        goal = max(p, 0.0) * sums[-1]
+        n = 1 + int(np.searchsorted(sums, goal)) if goal > 0 else 1
+        order = order[:n]
+    if least > 0:
+        order = order[w[order] >= min(least, 1.0)]
+    left = np.sort(order)
+    sums = np.cumsum(w[left])
+    if not 0 < u < 1:  # the first or last that has a weight, as the description counts them
+        at = np.flatnonzero(w[left] >= 2.0 ** -(62 - int(np.ceil(np.log2(len(l))))))[-1 if u >= 1 else 0]
+    else:
+        at = int(np.searchsorted(sums, u * sums[-1], side="right"))
+    return int(left[at]), w[left[at]] / sums[-1], len(left)
+
+
+def clear_of_borders(l, t, k, p, least, u):
+    """a random number near u that is 1e-7 away from the borders between tokens"""
+    l = np.where(np.isnan(l), -np.inf, l.astype(np.float64))
+    if not np.any(l > -np.inf) or not t > 0 or not 0 < u < 1:
+        return u
+    token = one_row(l, t, k, p, least, u)
+    for _ in range(200):
+        if one_row(l, t, k, p, least, u - 1e-7)[0] == one_row(l, t, k, p, least, u + 1e-7)[0]:
+            return u
+        u = np.float32((u * 7.31 + 0.123) % 1.0)
+    raise AssertionError(token)
+
+
+def sample(logits, par, u, stride=None, outs=True, scratch=None):
+    """logits: tensor [rows][vocab] on the GPU, par: dict of arrays"""
+    R, V = logits.shape
+    cuda = lambda a, t: torch.from_numpy(np.ascontiguousarray(a, t)).cuda()  # noqa: E731
+    keep = {n: cuda(a, np.int32 if n == "top_k" else np.float32) for n, a in par.items() if a is not None}
+    ud = cuda(u, np.float32)
+    token, kept = (torch.full((R,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    prob = torch.full((R,), -9.0, device="cuda")
+    d = si.si_sample_t(logits=logits.data_ptr(), u=ud.data_ptr(), token=token.data_ptr(), prob=prob.data_ptr() if outs else None, kept=kept.data_ptr() if outs else None,
+                       stride=logits.stride(0) if stride is None else stride, rows=R, vocab=V, type=si.SI_BF16 if logits.dtype == torch.bfloat16 else si.SI_F32,
+                       **{n: t.data_ptr() for n, t in keep.items()})
+    d.scratch_bytes = si.si_sample_scratch_bytes(d)
+    if scratch is None:
+        scratch = torch.zeros(d.scratch_bytes, dtype=torch.uint8, device="cuda")
+    d.scratch = scratch.data_ptr()
+    si.si_sample(d, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return token.cpu().numpy(), prob.cpu().numpy(), kept.cpu().numpy()
+
+
+def check(logits, u=None, seed=0, scratch=None, stride=None, **par):
+    R, V = logits.shape
+    l = logits.float().cpu().numpy()
+    rng = np.random.default_rng(seed)
+    u = rng.random(R, dtype=np.float32) if u is None else np.asarray(u, np.float32)
+    full = {n: np.broadcast_to(np.asarray(par.get(n, v)), (R,)) for n, v in NONE.items()}
+    args = [tuple(float(np.float32(full[n][r])) if n != "top_k" else int(full[n][r]) for n in NONE) for r in range(R)]
+    u = np.array([clear_of_borders(l[r], *args[r], u[r]) for r in range(R)], np.float32)
+    print("sample", logits.shape, logits.dtype, {n: v for n, v in par.items() if np.size(v) < 5}, flush=True)
+    token, prob, kept = sample(logits, {n: full[n] if n in par else None for n in NONE}, u, scratch=scratch, stride=stride)
+    for r in range(R):
+        want = one_row(l[r], *args[r], float(u[r]))
+        assert (int(token[r]), int(kept[r])) == (want[0], want[2]), (r, args[r], float(u[r]))
+        assert abs(float(prob[r]) - want[1]) <= (2.0 ** -24 + 2.0 ** -25) * want[1] + 2.0 ** -42, r
+
+
+def normal(R, V, dtype=torch.float32, spread=2.0, peaks=0, seed=0, pad=0):
+    g = torch.Generator().manual_seed(1000 * R + V + seed)
+    x = spread * torch.randn((R, V + pad), generator=g)
+    for r in range(R):
+        if peaks:
+            x[r, torch.randint(0, V, (peaks,), generator=g)] += 10 * torch.rand(peaks, generator=g)
+    return x.to("cuda", dtype)[:, :V]
+
+
+LIMITS = [dict(), dict(temperature=0.7), dict(temperature=0.0), dict(top_k=1), dict(top_k=20), dict(top_k=50, top_p=0.9), dict(top_p=0.5), dict(top_p=0.95, temperature=1.4),
+          dict(min_p=0.05), dict(min_p=0.3, top_p=0.9), dict(top_k=300, top_p=0.8, min_p=0.01, temperature=0.6), dict(top_p=0.0), dict(min_p=2.0)]
+
+
+@pytest.mark.parametrize("limits", LIMITS, ids=str)
+@pytest.mark.parametrize("R, V", [(1, 1), (3, 2), (5, 97), (4, 1000), (2, 8191), (2, 8192), (3, 8193), (5, 32000), (2, 100003)])
+def test_limits_and_sizes(R, V, limits):
+    check(normal(R, V, peaks=5 if V > 10 else 0), **limits)
+    check(normal(R, V, torch.bfloat16, seed=1, peaks=5 if V > 10 else 0, pad=3), **limits)
+
+
+@pytest.mark.parametrize("limits", [dict(top_p=0.9), dict(top_p=0.99, temperature=2.0), dict(top_k=3000), dict(top_k=20000, top_p=0.7), dict(min_p=1e-4), dict(top_k=30000, min_p=1e-5, top_p=0.999),
+                                    dict(top_k=49999)], ids=str)
+def test_many_tokens_are_left(limits):
+    """more than are sorted at once"""
+    check(normal(3, 50000, spread=1.0), **limits)
+    check(normal(2, 70001, torch.bfloat16, spread=0.5), **limits)
+
+
+def test_each_row_has_its_own_limits():
+    rng = np.random.default_rng(4)
+    R = 64
+    check(normal(R, 20011, peaks=20), temperature=rng.choice([0.0, 0.3, 0.8, 1.0, 1.7, -1.0], R), top_k=rng.choice([-3, 0, 1, 2, 40, 5000, 20011, 1 << 30], R),
+          top_p=rng.choice([0.0, 0.3, 0.9, 1.0, 1.5], R), min_p=rng.choice([-1.0, 0.0, 0.02, 0.5, 1.0], R))
+
+
+def test_ties_go_to_the_lowest_index():
+    x = torch.zeros((6, 9000), device="cuda")
+    x[1:, ::3] = 1.0
+    x[3] = -5.0
+    x[4, 7777] = 2.0
+    for limits in (dict(temperature=0.0), dict(top_k=1), dict(top_k=5), dict(top_k=4000), dict(top_p=0.2), dict(top_p=0.75), dict(top_k=3500, top_p=0.9), dict(min_p=0.5), dict(top_k=8999)):
+        check(x, u=[0.1, 0.9, 0.5, 0.33, 0.77, 0.999], **limits)
+    # values that bf16 makes alike
+    check(normal(4, 30000, torch.bfloat16, spread=0.1), top_k=2500)
+    check(normal(4, 30000, torch.bfloat16, spread=0.01), top_p=0.6)
+
+
+def test_masked_rows_nan_and_infinities():
+    inf, nan = float("inf"), float("nan")
+    x = normal(12, 10007)
+    x[0] = -inf
+    x[1] = nan
+    x[2, 1:] = -inf
+    x[3, :10006] = -inf
+    x[4, 5000:] = nan
+    x[5, [17, 9000]] = inf
+    x[6] = inf
+    x[7] = torch.finfo(torch.float32).min
+    x[8, 100:] = torch.finfo(torch.float32).min
+    x[9] = torch.finfo(torch.float32).max
+    x[10, 3] = torch.finfo(torch.float32).max
+    x[11, ::2] = -inf
+    for limits in (dict(), dict(temperature=0.0), dict(top_k=1), dict(top_k=7), dict(top_p=0.5), dict(min_p=0.1), dict(top_k=5, top_p=0.9, min_p=0.01)):
+        for u in (0.001, 0.6):
+            check(x, u=[u] * 12, **limits)
+
+
+def test_random_numbers_at_the_ends_and_bad_limits():
+    nan = float("nan")
+    x = normal(6, 9000)
+    for limits in (dict(), dict(top_k=30), dict(top_p=0.6), dict(top_k=8000), dict(temperature=0.05)):
+        check(x, u=[0.0, -1.0, 1.0, 2.0, 0.25, 1.0], **limits)
+    got = sample(x, dict(temperature=[1.0] * 6, top_k=[0] * 6, top_p=[nan] * 6, min_p=[nan] * 6), [0.5, nan, 0.0, 0.5, 0.5, 0.5])
+    want = sample(x, dict(), [0.5, 0.0, 0.0, 0.5, 0.5, 0.5])
+    assert all(np.array_equal(a, b) for a, b in zip(got, want)) and np.all(got[2] == 9000)
+    assert np.array_equal(sample(x, dict(temperature=[nan] * 6), [0.5] * 6)[0], x.argmax(1).cpu().numpy())
+
+
+@pytest.mark.parametrize("t", [1e-30, 1e-3, 50.0, 1e30, float("inf")])
+def test_temperatures_far_from_one(t):
+    x = normal(3, 20000)
+    for limits in (dict(), dict(top_k=9), dict(top_p=0.5), dict(min_p=0.5)):
+        check(x, u=[0.2, 0.5, 0.9], temperature=t, **limits)
+
+
+def test_the_largest_vocabulary():
+    V = si.SI_SAMPLE_MAX_VOCAB
+    x = normal(1, V, torch.bfloat16)
+    for limits in (dict(), dict(top_k=100), dict(top_p=0.7), dict(temperature=0.0)):
+        check(x, **limits)
+
+
+def test_rows_may_share_their_logits_and_outputs_may_be_left_out():
+    x = normal(1, 5000)
+    wide = x.expand(8, 5000)
+    check(wide, stride=0, top_k=40)
+    tokens = sample(x, dict(), [0.5], outs=False)
+    assert np.all(tokens[1] == -9.0) and np.all(tokens[2] == -9) and tokens[0][0] == sample(x, dict(), [0.5])[0][0]
+
+
+def test_draws_follow_the_distribution():
+    """each of the numbers (i + 1/2) / n draws: a token comes n w / S times, give or take one"""
+    n = 4096
+    x = normal(1, 50).expand(n, 50)
+    u = (np.arange(n) + 0.5) / n
+    token, _, _ = sample(x, dict(top_k=[20] * n), u, stride=0)
+    l = x[0].double().cpu().numpy()
+    order = np.argsort(-l)[:20]
+    w = np.zeros(50)
+    w[order] = np.exp(l[order] - l.max())
+    assert np.all(np.abs(np.bincount(token, minlength=50) - n * w / w.sum()) <= 1)
+
+
+def test_one_scratch_for_calls_of_all_sizes():
+    big = normal(40, 20000)
+    d = si.si_sample_t(rows=64, vocab=70000, type=si.SI_F32)
+    scratch = torch.zeros(si.si_sample_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+    check(big, scratch=scratch, top_p=0.8)
+    check(normal(1, 70000), scratch=scratch, top_k=10)
+    check(normal(64, 50), scratch=scratch)
+    check(normal(2, 65000, torch.bfloat16), scratch=scratch, top_p=0.8)
+    check(normal(64, 9000), scratch=scratch, top_k=5)
+    assert int(scratch[:4 * si.SI_SAMPLE_MAX_ROWS].max()) == 0
+
+
+def test_the_same_every_time():
+    x = normal(16, 100003)
+    u = np.random.default_rng(2).random(16, dtype=np.float32)
+    par = dict(top_p=[0.95] * 8 + [1.0] * 8, top_k=[0] * 12 + [5000] * 4)
+    want = sample(x, par, u)
+    for _ in range(5):
+        assert all(np.array_equal(a, b) for a, b in zip(sample(x, par, u), want))
+
+
+def test_recorded_on_another_stream_and_replayed():
+    R, V = 5, 30000
+    x, u = torch.empty((R, V), device="cuda"), torch.empty(R, device="cuda")
+    top_p = torch.tensor([1.0, 0.9, 0.5, 0.99, 1.0], device="cuda")
+    token = torch.zeros(R, dtype=torch.int32, device="cuda")
+    d = si.si_sample_t(logits=x.data_ptr(), top_p=top_p.data_ptr(), u=u.data_ptr(), token=token.data_ptr(), stride=V, rows=R, vocab=V, type=si.SI_F32)
+    d.scratch_bytes = si.si_sample_scratch_bytes(d)
+    scratch = torch.zeros(d.scratch_bytes, dtype=torch.uint8, device="cuda")
+    d.scratch = scratch.data_ptr()
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        si.si_sample(d, torch.cuda.current_stream().cuda_stream)
+    for i in range(5):
+        x.copy_(normal(R, V, seed=i % 3))
+        u.copy_(torch.rand(R, generator=torch.Generator().manual_seed(i % 3)))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = sample(x, dict(top_p=top_p.cpu().numpy()), u.cpu().numpy())[0]
+        assert np.array_equal(token.cpu().numpy(), want)
