@@ -202,6 +202,22 @@ int si_attend(const si_cache_t* cache, int32_t layer, const si_attend_t* desc, v
  * GPU needed; q, out, lse, scratch and scratch_bytes are not looked at). */
 int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc);
 
+/*
+ * The same attention, for lists in which neighbours share leading pages (si_cache_fork gave them the same prompt): the full pages that neighbouring
+ * entries of the list have in common are attended to by all of their rows together, read once, and each sequence's own tokens beside
+ * them.  Which entries these are, and how many pages, is found on the device from the table, at every call: nothing has to be said, and a list
+ * without shared pages is taken too (as si_attend, a little slower).  A group is a run of neighbours; it is cut where two of them have nothing in
+ * common, or less than half of what one has in common with its other neighbour; all of a group read the pages that they all have in common.
+ * Results are those of si_attend but for the order of sums in fp32; they do not depend on the order in which blocks run, but on which
+ * neighbours a sequence has in the list.
+ * scratch: si_attend_shared_scratch_bytes, else as for si_attend, whose scratch it can be too (and, where it is large enough, the other way round).
+ * Errors: those of si_attend, and SI_EINVAL for n * n_new * n_heads of 2^31 or more.
+ */
+int si_attend_shared(const si_cache_t* cache, int32_t layer, const si_attend_t* desc, void* stream);
+
+/* Bytes of scratch that si_attend_shared needs for these descriptors, and for any with a smaller n or max_len, as si_attend_scratch_bytes. */
+int64_t si_attend_shared_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc);
+
 /* ------------------------------------------------------------------------------------------------ moves of pages
  * All act on every layer at once.  `seqs` and the like are DEVICE int32 [n], n <= SI_CACHE_MAX_LIST.  Pages are taken from the free ones (refs
  * 0) in ascending order, in the order of the list and of the positions, so that results do not depend on scheduling.  The list of

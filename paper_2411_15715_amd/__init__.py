@@ -27,7 +27,8 @@ EXPORTS = ["si_layer_create", "si_layer_split_info", "si_split_counts", "si_laye
            "si_fit_linear", "si_model_times", "si_simulate", "si_solve_split", "si_model_times_ng", "si_solve_ng",
            "si_assign_gpu_memory", "si_profile", "si_measure_peaks",
            # scheinfer_attention.h
-           "si_norm", "si_kv_offsets", "si_cache_append", "si_cache_append_normed", "si_attend", "si_attend_scratch_bytes", "si_cache_scratch_bytes",
+           "si_norm", "si_kv_offsets", "si_cache_append", "si_cache_append_normed", "si_attend", "si_attend_scratch_bytes",
+           "si_attend_shared", "si_attend_shared_scratch_bytes", "si_cache_scratch_bytes",
            "si_cache_trim", "si_cache_extend", "si_cache_fork", "si_cache_compact",
            # scheinfer_sample.h
            "si_sample", "si_sample_scratch_bytes"]
@@ -248,6 +249,10 @@ def lib():
         L.si_attend.argtypes = [pc, i32, ctypes.POINTER(si_attend_t), vp]
         L.si_attend_scratch_bytes.restype = i64
         L.si_attend_scratch_bytes.argtypes = [pc, ctypes.POINTER(si_attend_t)]
+        L.si_attend_shared.restype = ctypes.c_int
+        L.si_attend_shared.argtypes = [pc, i32, ctypes.POINTER(si_attend_t), vp]
+        L.si_attend_shared_scratch_bytes.restype = i64
+        L.si_attend_shared_scratch_bytes.argtypes = [pc, ctypes.POINTER(si_attend_t)]
         L.si_cache_scratch_bytes.restype = i64
         L.si_cache_scratch_bytes.argtypes = [pc]
         L.si_cache_trim.restype = ctypes.c_int
@@ -602,6 +607,17 @@ def si_attend_scratch_bytes(cache, desc) -> int:
 def si_attend(cache, layer, desc, stream=0):
     """Attention of the last n_new tokens of each sequence over the cache; desc: si_attend_t."""
     _check(lib().si_attend(ctypes.byref(cache), layer, ctypes.byref(desc), stream))
+
+
+def si_attend_shared_scratch_bytes(cache, desc) -> int:
+    n = lib().si_attend_shared_scratch_bytes(ctypes.byref(cache), ctypes.byref(desc))
+    _check(min(n, SI_OK))
+    return n
+
+
+def si_attend_shared(cache, layer, desc, stream=0):
+    """si_attend for lists whose neighbours share leading pages (forks): these are read once for all of them; desc: si_attend_t."""
+    _check(lib().si_attend_shared(ctypes.byref(cache), layer, ctypes.byref(desc), stream))
 
 
 def si_cache_scratch_bytes(cache) -> int:

@@ -7,18 +7,10 @@
 #include <cmath>
 
 namespace si {
-namespace {
-
-constexpr int64_t ATTEND_BLOCKS = 1 << 24;  // (a launch has fewer than 2^32 threads)
-
-struct Cut {
-  int block_rows, groups, slices, whole, part_rows, last_joins;
-  int64_t scratch, part_at;
-};
 
 // Rows of a block, row groups, and the slices that a kv head's cache blocks are cut into.
-Cut cut(const si_cache_t& c, const si_attend_t& a) {
-  Cut k{};
+AttendCut cut_attend(const si_cache_t& c, const si_attend_t& a) {
+  AttendCut k{};
   const int rows = a.n_new * (a.n_heads / c.n_kv_heads), B = kv_block(c.type);
   int64_t seen = a.max_len;
   if (a.window) seen = std::min<int64_t>(seen, (int64_t)a.window + a.n_new - 1 + B);
@@ -61,9 +53,9 @@ Cut cut(const si_cache_t& c, const si_attend_t& a) {
   return k;
 }
 
-bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+static bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-int check_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
+int check_attend_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
   if (int rc = check_cache(c, who)) return rc;
   if (!a) return set_error(SI_EINVAL, "%s: descriptor is NULL", who);
   if (a->n < 0 || a->n > 65535) return set_error(SI_EINVAL, "%s: n %d outside 0 .. 65535", who, a->n);
@@ -79,38 +71,61 @@ int check_shape(const si_cache_t* c, const si_attend_t* a, const char* who) {
   return SI_OK;
 }
 
-}  // namespace
-}  // namespace si
-
-extern "C" int64_t si_attend_scratch_bytes(const si_cache_t* c, const si_attend_t* a) {
-  using namespace si;
-  if (int rc = check_shape(c, a, "si_attend_scratch_bytes")) return rc;
-  return cut(*c, *a).scratch;
-}
-
-extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* a, void* stream) {
-  using namespace si;
-  const char* who = "si_attend";
-  if (int rc = check_shape(c, a, who)) return rc;
+// Everything but the scratch; *nothing: there are no sequences
+int check_attend(const si_cache_t* c, int layer, const si_attend_t* a, const char* who, bool* nothing) {
+  *nothing = false;
+  if (int rc = check_attend_shape(c, a, who)) return rc;
   if (int rc = check_layer(c, layer, who)) return rc;
-  if (a->n == 0) return SI_OK;  // (an empty tensor's address may be NULL)
+  if ((*nothing = a->n == 0)) return SI_OK;  // (an empty tensor's address may be NULL)
   if (!a->q || !a->out) return set_error(SI_EINVAL, "%s: q or out is NULL", who);
   if (misaligned(a->q, 2) || misaligned(a->out, 2) || misaligned(a->lse, 4) || misaligned(a->seqs, 4)) return set_error(SI_EINVAL, "%s: a pointer is not aligned to its element", who);
   if (!a->seqs && a->n > c->n_seqs) return set_error(SI_EINVAL, "%s: n %d of %d sequences", who, a->n, c->n_seqs);
   const int64_t row = (int64_t)a->n_heads * c->head_dim;
   if (a->q_stride < row || a->out_stride < row) return set_error(SI_EINVAL, "%s: a stride is smaller than its row", who);
-  const Cut k = cut(*c, *a);
-  if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
-    return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
-  AttendArgs g{*c, *a, layer, a->n_new * (a->n_heads / c->n_kv_heads), k.groups, k.block_rows, k.slices, k.whole, k.part_rows, k.last_joins, 0.f, nullptr, nullptr, nullptr};
-  g.scale2 = (float)((a->scale == 0.f ? 1.0 / std::sqrt((double)c->head_dim) : (double)a->scale) * 1.4426950408889634);
+  return SI_OK;
+}
+
+AttendArgs attend_args(const si_cache_t& c, const si_attend_t& a, int layer, const AttendCut& k) {
+  AttendArgs g{};
+  g.c = c;
+  g.a = a;
+  g.layer = layer;
+  g.rows = a.n_new * (a.n_heads / c.n_kv_heads);
+  g.groups = k.groups;
+  g.block_rows = k.block_rows;
+  g.slices = k.slices;
+  g.whole = k.whole;
+  g.part_rows = k.part_rows;
+  g.last_joins = k.last_joins;
+  g.joins = a.n;
+  g.scale2 = (float)((a.scale == 0.f ? 1.0 / std::sqrt((double)c.head_dim) : (double)a.scale) * 1.4426950408889634);
   if (k.scratch > 0) {
-    char* p = static_cast<char*>(a->scratch);
+    char* p = static_cast<char*>(a.scratch);
     g.count = reinterpret_cast<uint32_t*>(p);
     g.parted = reinterpret_cast<int2*>(p + ATTEND_COUNTERS * 4);
     g.part = reinterpret_cast<float*>(p + k.part_at);
   }
-  const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);
+  return g;
+}
+
+}  // namespace si
+
+extern "C" int64_t si_attend_scratch_bytes(const si_cache_t* c, const si_attend_t* a) {
+  using namespace si;
+  if (int rc = check_attend_shape(c, a, "si_attend_scratch_bytes")) return rc;
+  return cut_attend(*c, *a).scratch;
+}
+
+extern "C" int si_attend(const si_cache_t* c, int32_t layer, const si_attend_t* a, void* stream) {
+  using namespace si;
+  const char* who = "si_attend";
+  bool nothing;
+  if (int rc = check_attend(c, layer, a, who, &nothing)) return rc;
+  if (nothing) return SI_OK;
+  const AttendCut k = cut_attend(*c, *a);
+  if (k.scratch > 0 && (!a->scratch || a->scratch_bytes < k.scratch || misaligned(a->scratch, 16)))
+    return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)k.scratch);
+  const hipError_t e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(attend_args(*c, *a, layer, k), (hipStream_t)stream);
   if (e != hipSuccess) return set_error(SI_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return SI_OK;
 }

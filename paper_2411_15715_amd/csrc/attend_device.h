@@ -29,7 +29,20 @@ namespace si {
 constexpr int ATTEND_WAVES = 4;         // of a block
 constexpr int ATTEND_THREADS = 64 * ATTEND_WAVES;
 constexpr int ATTEND_COUNTERS = 16384;  // sequences times units (kv head, row group) whose parts the last block may join
+constexpr int64_t ATTEND_BLOCKS = 1 << 24;  // of a launch (it has fewer than 2^32 threads)
 constexpr int attend_wide_dim(int type) { return type == SI_KV_E4M3 ? 64 : 128; }  // longest heads of which a wave may have 32 rows
+
+// What a launch attends to: ALL of each sequence; of groups of sequences whose first pages are the same, only these, for all their rows (SHARED: its
+// sums stay as they are); or of each sequence what lies after them, its sums joined with those (OWN).
+enum { ATTEND_ALL, ATTEND_SHARED, ATTEND_OWN };
+
+// Up to block_rows rows of a group, in the order of the list, that attend to the group's pages: a sequence of the SHARED launch
+struct SharedRows {
+  int entry;       // of the list: the sequence whose row of the table is read
+  int first, rows; // rows (entry * n_new + token) * heads per kv head + head, of a kv head
+  int tokens;      // that all of them see but for a window
+  int lo, lo_all;  // with a window: what some row of the group sees begins at lo or later, what all see at lo_all or before
+};
 
 struct AttendArgs {
   si_cache_t c;
@@ -42,14 +55,34 @@ struct AttendArgs {
   int whole;      // a slice for each sequence instead (short ones: nothing to even out, nothing to join)
   int part_rows;  // rows of a unit that the scratch has room for: min(rows, block_rows)
   int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
+  int joins;      // sequences that the join kernel has blocks for
   float scale2;   // scale * log2(e)
   uint32_t* count;  // [ATTEND_COUNTERS], of (sequence, unit); 0 between calls
   int2* parted;     // [n][unit] first slice of a sequence and number of them
   float* part;      // [unit][slice][2][part_rows][D + 2]: o, then m, l of each row; first the sum of a sequence that began before the slice
+  // shared pages (attend_shared.hip): the rows' sums over them [kv head][n * n_new * heads per kv head][D + 4], number of SharedRows and these, and
+  // where each sequence's own tokens begin
+  float* shared_sums;
+  const int32_t* n_shared;
+  const SharedRows* shared;
+  const int32_t* own_from;
 };
+
+// attend.hip: how a call is cut into blocks, and its checks (SI_OK, or an error that names `who`)
+struct AttendCut {
+  int block_rows, groups, slices, whole, part_rows, last_joins;
+  int64_t scratch, part_at;
+};
+AttendCut cut_attend(const si_cache_t& c, const si_attend_t& a);
+int check_attend_shape(const si_cache_t* c, const si_attend_t* a, const char* who);
+int check_attend(const si_cache_t* c, int layer, const si_attend_t* a, const char* who, bool* nothing);
+AttendArgs attend_args(const si_cache_t& c, const si_attend_t& a, int layer, const AttendCut& k);
 
 hipError_t launch_attend_bf16(const AttendArgs& g, hipStream_t stream);
 hipError_t launch_attend_e4m3(const AttendArgs& g, hipStream_t stream);
+// both launches over shared pages
+hipError_t launch_attend_shared_bf16(const AttendArgs& shared, const AttendArgs& own, hipStream_t stream);
+hipError_t launch_attend_shared_e4m3(const AttendArgs& shared, const AttendArgs& own, hipStream_t stream);
 
 #if defined(__HIPCC__)
 namespace {
@@ -118,14 +151,23 @@ __device__ __forceinline__ Unit unit_of(const AttendArgs& g) {
 }
 
 // What the new tokens t0 .. t1 of a sequence see, in positions and in blocks of B
+typedef const int32_t __attribute__((address_space(4))) constant_t;  // scalar loads: of lists that nothing in the launch writes
 struct Span {
   int seq, len, window, first;  // first: where the sight of token 0 ends
   int lo, hi, lo_all, hi_all;   // seen by some of them: [lo, hi), by all of them [lo_all, hi_all)
   int fb, nb;                   // first block and number of them
   int why;
-  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B) {
-    // (scalar loads: nothing in this launch writes the lists)
-    typedef const int32_t __attribute__((address_space(4))) constant_t;
+  __device__ __forceinline__ Span(const AttendArgs& g, const SharedRows& r, int B) {
+    seq = g.a.seqs ? ((constant_t*)(uintptr_t)g.a.seqs)[r.entry] : r.entry;
+    window = g.a.window;
+    len = first = why = 0;
+    hi = hi_all = r.tokens;
+    lo = min(r.lo, hi);
+    lo_all = min(r.lo_all, hi);
+    fb = lo / B;
+    nb = hi > lo ? (hi + B - 1) / B - fb : 0;
+  }
+  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B, int from = 0) {
     const si_cache_t& c = g.c;
     seq = g.a.seqs ? ((constant_t*)(uintptr_t)g.a.seqs)[seq_i] : seq_i;
     len = 0;
@@ -140,8 +182,8 @@ struct Span {
     first = len - g.a.n_new + 1;
     hi = max(0, first + t1);
     hi_all = max(0, first + t0);
-    lo = window ? max(0, first + t0 - window) : 0;
-    lo_all = window ? max(0, first + t1 - window) : 0;
+    lo = window ? max(from, first + t0 - window) : from;
+    lo_all = window ? max(from, first + t1 - window) : from;
     fb = lo / B;
     nb = hi > lo ? (hi + B - 1) / B - fb : 0;
   }
@@ -159,7 +201,33 @@ struct Sum {
   }
 };
 
-__device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, const Sum& s, float scale_v) {
+template <int MODE> __device__ __forceinline__ int own_from(const AttendArgs& g, int seq_i) {
+  if constexpr (MODE == ATTEND_OWN) return ((constant_t*)(uintptr_t)g.own_from)[seq_i];
+  else return 0;
+}
+__device__ __forceinline__ SharedRows shared_rows(const AttendArgs& g, int v) {
+  const constant_t* p = (const constant_t*)(uintptr_t)(g.shared + v);
+  return SharedRows{p[0], p[1], p[2], p[3], p[4], p[5]};
+}
+// the sums of a row of a kv head over shared pages
+__device__ __forceinline__ float* shared_sum(const AttendArgs& g, int kv, int64_t row) {
+  const int64_t rows = (int64_t)g.a.n * g.a.n_new * (g.a.n_heads / g.c.n_kv_heads);
+  return g.shared_sums + (kv * rows + row) * (g.c.head_dim + 4);
+}
+
+// MODE SHARED: the sums as they are, of row `row` of the SharedRows seq_i
+template <int MODE> __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, Sum s, float scale_v) {
+  if constexpr (MODE == ATTEND_SHARED) {
+    float* to = shared_sum(g, kv, ((const constant_t*)(uintptr_t)(g.shared + seq_i))[1] + row);
+    *reinterpret_cast<f32x4*>(to + dim) = s.o;
+    if (dim == 0) *reinterpret_cast<float2*>(to + g.c.head_dim) = make_float2(s.m, s.l);
+    return;
+  }
+  if (MODE == ATTEND_OWN && own_from<MODE>(g, seq_i) > 0) {
+    const float* from = shared_sum(g, kv, (int64_t)seq_i * g.rows + row);
+    const float2 ml = *reinterpret_cast<const float2*>(from + g.c.head_dim);
+    s.add(*reinterpret_cast<const f32x4*>(from + dim), ml.x, ml.y);
+  }
   const int per = g.a.n_heads / g.c.n_kv_heads, j = row / per, head = kv * per + row % per;
   const int64_t r = (int64_t)seq_i * g.a.n_new + j;
   const float inv = s.l == 0.f ? 0.f : scale_v / s.l;
@@ -177,7 +245,7 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn
 // wave loading for itself, TILES requests for every line at the caches: 24 rows over 16 x 8000 positions 108 us, this way 97.)
 // In blocks of 128 rows a wave has 32, in smaller ones 16: two waves with the same cache block hide each other's waits (before the weights had two
 // operands, 20 rows of e4m3 over 29 windows of 9000 positions, 32 a wave and a ring for each wave: 113 us, 16: 91).
-template <int TYPE, int D, int NT, int TILES> struct Attend {
+template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Attend {
   static constexpr int ROWS = 16 * NT, BLOCK_ROWS = ROWS * TILES;              // of a wave, of a block
   static constexpr bool RING = TILES > 1;                                     // K and V come by way of LDS
   static constexpr int E = TYPE == SI_KV_E4M3 ? 16 : 8, B = 4 * E, J = E / 4;  // J score tiles of 16 tokens
@@ -306,16 +374,23 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
   }
 
   static __device__ void run(const AttendArgs& g, Shared& s) {
-    const int block_row0 = unit_of(g).group * BLOCK_ROWS, row_end = min(g.rows, block_row0 + BLOCK_ROWS);
+    const int block_row0 = unit_of(g).group * BLOCK_ROWS;
+    int row_end = min(g.rows, block_row0 + BLOCK_ROWS);  // (SHARED: of each sequence's own)
     if (RING && threadIdx.x == 0) s.again = 0;
-    const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
+    const int n = MODE == ATTEND_SHARED ? *(constant_t*)(uintptr_t)g.n_shared : g.a.n;
+    const int slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
+    if (MODE == ATTEND_SHARED && n == 0) return;
+    auto span_of = [&](int k) {
+      if constexpr (MODE == ATTEND_SHARED) return Span(g, shared_rows(g, k), B);
+      else return Span(g, k, t0, t1, B, own_from<MODE>(g, k));
+    };
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
-    auto blocks_of = [&](int k) { return (int64_t)max(1, Span(g, k, t0, t1, B).nb); };
+    auto blocks_of = [&](int k) { return (int64_t)max(1, span_of(k).nb); };
     const int mine = (n + THREADS - 1) / THREADS, k0 = min(n, (int)threadIdx.x * mine), k1 = min(n, k0 + mine);  // sequences that a thread counts
     int64_t total, before = 0, counted = 0;
     int i = g.whole ? slice : 0;
-    Span sp(g, i, t0, t1, B);
+    Span sp = span_of(i);
     if (n == 1 || g.whole) {
       total = max(1, sp.nb);
     } else {
@@ -345,8 +420,10 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     }
     // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
     int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
+    auto rows_of = [&](int k) { return MODE == ATTEND_SHARED ? shared_rows(g, k).rows : row_end; };
     for (; left > 0; ++i) {
-      if (n > 1 && !g.whole) sp = Span(g, i, t0, t1, B);
+      if (n > 1 && !g.whole) sp = span_of(i);
+      if constexpr (MODE == ATTEND_SHARED) row_end = shared_rows(g, i).rows;
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
       part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
@@ -374,7 +451,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
       for (int k = 0; k < 2; ++k)
         if (un_seq[k] >= 0 && s.arrived[k] == (uint32_t)un_parts[k] - 1) {
           if (threadIdx.x == 0) __hip_atomic_store(g.count + un_seq[k] * gridDim.x + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          join(g, un_seq[k], un_first[k], un_parts[k], block_row0, row_end);
+          join(g, un_seq[k], un_first[k], un_parts[k], block_row0, rows_of(un_seq[k]));
         }
     }
   }
@@ -388,14 +465,29 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     const int stream = wave / TILES, row0 = block_row0 + wave % TILES * ROWS;
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
-    // this lane's rows of q, as right operands; token of a row, or -1
+    // this lane's rows of q, as right operands; token of a row (SHARED: of all tokens of the call), or -1
+    const int64_t row_base = MODE == ATTEND_SHARED ? shared_rows(g, seq_i).first : (int64_t)seq_i * n_new * per;
+    auto token_of = [&](int row) { return MODE == ATTEND_SHARED ? (int)((row_base + row) / per) : row / per; };
+    // what a token sees of this launch's positions
+    auto sees_to = [&](int t) { return MODE == ATTEND_SHARED ? hi : max(0, first + t); };
+    auto sees_from = [&](int t) {
+      if constexpr (MODE == ATTEND_SHARED) {
+        if (!window) return 0;
+        const int e = t / n_new, s = g.a.seqs ? g.a.seqs[e] : e;  // (members of a group have a place in the table)
+        return max(0, c.lens[s] - n_new + 1 + t % n_new - window);
+      } else {
+        return window ? max(0, first + t - window) : 0;
+      }
+    };
     int tok[NT];
     u32x4 q[NT][D / 32];
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       const int row = row0 + 16 * u + col;
-      tok[u] = row < row_end ? row / per : -1;
-      const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + ((int64_t)seq_i * n_new + row / per) * g.a.q_stride + (int64_t)(kv * per + row % per) * D;
+      tok[u] = row < row_end ? token_of(row) : -1;
+      const int64_t q_row = MODE == ATTEND_SHARED ? (row_base + row) / per : (int64_t)seq_i * n_new + row / per;
+      const int q_head = MODE == ATTEND_SHARED ? (int)((row_base + row) % per) : row % per;
+      const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + q_row * g.a.q_stride + (int64_t)(kv * per + q_head) * D;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
         // operand x of K covers, in this lane, elements 32 x + 8 grp of a head (bf16), or half x % 2 of the 16 from 64 (x / 2) + 16 grp on
@@ -422,7 +514,6 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
     const int per_page = c.page_tokens / B, last_entry = (b1 - 1) / per_page;
     struct Place { int entry, at; };
     auto page_of = [&](const Place& w) {
-      typedef const int32_t __attribute__((address_space(4))) constant_t;
       const int page = ((constant_t*)(uintptr_t)table)[min(w.entry, last_entry)];
       return page >= 0 && page < c.n_pages ? page : -1;
     };
@@ -498,7 +589,10 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
         float top = -INFINITY;
-        const int see_hi = tok[u] >= 0 ? max(0, first + tok[u]) : 0, see_lo = window ? max(0, first + tok[u] - window) : 0;
+        const int see_hi = tok[u] >= 0 ? sees_to(tok[u]) : 0;
+        int see_lo = 0;
+        if constexpr (MODE == ATTEND_SHARED) see_lo = EDGE && tok[u] >= 0 ? sees_from(tok[u]) : 0;
+        else see_lo = window ? max(0, first + tok[u] - window) : 0;
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -569,8 +663,8 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
       int mine = t0 + grp * E;
       asm volatile("" : "+v"(mine));
 #pragma unroll 1
-      for (int j = row0 / per; j <= (min(row_end, row0 + ROWS) - 1) / per; ++j) {
-        const u32x4 seen = token_mask(mine, window ? max(0, first + j - window) : 0, max(0, first + j));
+      for (int j = token_of(row0); j <= token_of(min(row_end, row0 + ROWS) - 1); ++j) {
+        const u32x4 seen = token_mask(mine, sees_from(j), sees_to(j));
         v_to([&](int i, u32x4 v) {
           v &= seen;
           const u32x4 v_finite = finite_only(v);
@@ -742,7 +836,7 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
       for (int w = r / ROWS; w < WAVES; w += TILES) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % ROWS][dim]), s.m[w][r % ROWS], s.l[w][r % ROWS]);
       float* to = sums + r * (D + 2);
       if (where_to < 0) {
-        write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
+        write_row<MODE>(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
       } else if (g.last_joins) {
         put2(to + dim, sum.o[0], sum.o[1]);
         put2(to + dim + 2, sum.o[2], sum.o[3]);
@@ -777,24 +871,25 @@ template <int TYPE, int D, int NT, int TILES> struct Attend {
         for (int k = 0; k < AHEAD; ++k)
           if (p0 + k < parts) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
       }
-      write_row(g, seq_i, kv, block_row0 + r, dim, sum, TYPE == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+      write_row<MODE>(g, seq_i, kv, block_row0 + r, dim, sum, TYPE == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
     }
   }
 };
 
-template <int TYPE, int D, int NT, int TILES>
+template <int TYPE, int D, int NT, int TILES, int MODE>
 __global__ __launch_bounds__((Attend<TYPE, D, NT, TILES>::THREADS), (Attend<TYPE, D, NT, TILES>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
-  __shared__ typename Attend<TYPE, D, NT, TILES>::Shared s;
-  Attend<TYPE, D, NT, TILES>::run(g, s);
+  __shared__ typename Attend<TYPE, D, NT, TILES, MODE>::Shared s;
+  Attend<TYPE, D, NT, TILES, MODE>::run(g, s);
 }
 
 // Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
-template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
+template <int D, int MODE> __device__ __forceinline__ void join_row(const AttendArgs& g, int seq_i) {
   constexpr int LANES = D / 4, SHARES = 256 / LANES;
   __shared__ f32x4 s_o[SHARES][LANES];
   __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
-  const int kv = unit_of(g).kv, seq_i = blockIdx.y, row = unit_of(g).group * g.block_rows + blockIdx.z;
-  typedef const int32_t __attribute__((address_space(4))) constant_t;
+  const int kv = unit_of(g).kv, row = unit_of(g).group * g.block_rows + blockIdx.z;
+  if constexpr (MODE == ATTEND_SHARED)
+    if (row >= shared_rows(g, seq_i).rows) return;
   const constant_t* parted = (const constant_t*)(uintptr_t)(g.parted + (int64_t)seq_i * gridDim.x + blockIdx.x);
   const int first = parted[0], parts = parted[1];
   if (row >= g.rows || parts == 1) return;  // (one part is written already)
@@ -822,20 +917,31 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   __syncthreads();
   if (share > 0) return;
   for (int k = 1; k < min(SHARES, parts); ++k) sum.add(s_o[k][lane], s_m[k][lane], s_l[k][lane]);
-  write_row(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+  write_row<MODE>(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+}
+template <int D, int MODE> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
+  if constexpr (MODE == ATTEND_SHARED) {
+    // (how many there are is known on the device only)
+    for (int v = blockIdx.y; v < *(constant_t*)(uintptr_t)g.n_shared; v += gridDim.y) {
+      join_row<D, MODE>(g, v);
+      __syncthreads();
+    }
+  } else {
+    join_row<D, MODE>(g, blockIdx.y);
+  }
 }
 
-template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
+template <int TYPE, int D, int MODE = ATTEND_ALL> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
   // (heads first: blocks go to the dies in turn, and all heads of a slice have the same to do)
   const dim3 grid(g.c.n_kv_heads * g.groups, g.slices);
-  if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   if (g.slices > 1 && !g.whole && !g.last_joins) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_join<D>, dim3(grid.x, g.a.n, g.part_rows), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL((k_join<D, MODE>), dim3(grid.x, g.joins, g.part_rows), dim3(256), 0, stream, g);
   }
   return hipGetLastError();
 }
