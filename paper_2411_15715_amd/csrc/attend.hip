@@ -97,7 +97,6 @@ AttendArgs attend_args(const si_cache_t& c, const si_attend_t& a, int layer, con
   g.whole = k.whole;
   g.part_rows = k.part_rows;
   g.last_joins = k.last_joins;
-  g.joins = a.n;
   g.scale2 = (float)((a.scale == 0.f ? 1.0 / std::sqrt((double)c.head_dim) : (double)a.scale) * 1.4426950408889634);
   if (k.scratch > 0) {
     char* p = static_cast<char*>(a.scratch);

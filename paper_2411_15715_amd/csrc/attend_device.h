@@ -32,16 +32,17 @@ constexpr int ATTEND_COUNTERS = 16384;  // sequences times units (kv head, row g
 constexpr int64_t ATTEND_BLOCKS = 1 << 24;  // of a launch (it has fewer than 2^32 threads)
 constexpr int attend_wide_dim(int type) { return type == SI_KV_E4M3 ? 64 : 128; }  // longest heads of which a wave may have 32 rows
 
-// What a launch attends to: ALL of each sequence; of groups of sequences whose first pages are the same, only these, for all their rows (SHARED: its
-// sums stay as they are); or of each sequence what lies after them, its sums joined with those (OWN).
-enum { ATTEND_ALL, ATTEND_SHARED, ATTEND_OWN };
+// What a launch goes by: ALL of each sequence, or PIECES (attend_shared.hip): up to block_rows rows with the positions that they attend to in it
+enum { ATTEND_ALL, ATTEND_PIECES };
 
-// Up to block_rows rows of a group, in the order of the list, that attend to the group's pages: a sequence of the SHARED launch
-struct SharedRows {
-  int entry;       // of the list: the sequence whose row of the table is read
-  int first, rows; // rows (entry * n_new + token) * heads per kv head + head, of a kv head
-  int tokens;      // that all of them see but for a window
-  int lo, lo_all;  // with a window: what some row of the group sees begins at lo or later, what all see at lo_all or before
+// Of several sequences and the pages that these share, or of one and its own tokens
+struct Piece {
+  int seq;                     // whose row of the table is read
+  int first, rows;             // rows (entry of the list * n_new + token) * heads per kv head + head, of a kv head
+  int lo, hi, lo_all, hi_all;  // positions seen by some of the rows, and by all
+  int fb, nb;                  // first block and number of them
+  int own;                     // -1: shared, all rows see them but for a window; else the entry of the list
+  int sight;                   // own: where the sight of the entry's first new token ends
 };
 
 struct AttendArgs {
@@ -55,17 +56,18 @@ struct AttendArgs {
   int whole;      // a slice for each sequence instead (short ones: nothing to even out, nothing to join)
   int part_rows;  // rows of a unit that the scratch has room for: min(rows, block_rows)
   int last_joins; // the block that finishes last joins the parts of a sequence; else the join kernel does
-  int joins;      // sequences that the join kernel has blocks for
   float scale2;   // scale * log2(e)
   uint32_t* count;  // [ATTEND_COUNTERS], of (sequence, unit); 0 between calls
   int2* parted;     // [n][unit] first slice of a sequence and number of them
   float* part;      // [unit][slice][2][part_rows][D + 2]: o, then m, l of each row; first the sum of a sequence that began before the slice
-  // shared pages (attend_shared.hip): the rows' sums over them [kv head][n * n_new * heads per kv head][D + 4], number of SharedRows and these, and
-  // where each sequence's own tokens begin
-  float* shared_sums;
-  const int32_t* n_shared;
-  const SharedRows* shared;
-  const int32_t* own_from;
+  // pieces: their number, they, their blocks one after the other (a piece of none counts as one), and where the sums of those that one block has all of
+  // go: [shared, own][kv head][n * n_new * heads per kv head][D + 4], o, then m, l
+  const int32_t* n_pieces;
+  const Piece* pieces;
+  const int64_t* begins;  // [n_pieces + 1]
+  float* sums;
+  const int2* group;      // [n] first piece of an entry's group (-1: none), first entry of it
+  int chunks;             // pieces of an entry's own tokens
 };
 
 // attend.hip: how a call is cut into blocks, and its checks (SI_OK, or an error that names `who`)
@@ -80,9 +82,9 @@ AttendArgs attend_args(const si_cache_t& c, const si_attend_t& a, int layer, con
 
 hipError_t launch_attend_bf16(const AttendArgs& g, hipStream_t stream);
 hipError_t launch_attend_e4m3(const AttendArgs& g, hipStream_t stream);
-// both launches over shared pages
-hipError_t launch_attend_shared_bf16(const AttendArgs& shared, const AttendArgs& own, hipStream_t stream);
-hipError_t launch_attend_shared_e4m3(const AttendArgs& shared, const AttendArgs& own, hipStream_t stream);
+// pieces, and the joining of their sums
+hipError_t launch_attend_pieces_bf16(const AttendArgs& g, hipStream_t stream);
+hipError_t launch_attend_pieces_e4m3(const AttendArgs& g, hipStream_t stream);
 
 #if defined(__HIPCC__)
 namespace {
@@ -157,17 +159,17 @@ struct Span {
   int lo, hi, lo_all, hi_all;   // seen by some of them: [lo, hi), by all of them [lo_all, hi_all)
   int fb, nb;                   // first block and number of them
   int why;
-  __device__ __forceinline__ Span(const AttendArgs& g, const SharedRows& r, int B) {
-    seq = g.a.seqs ? ((constant_t*)(uintptr_t)g.a.seqs)[r.entry] : r.entry;
+  int own;                      // of a piece
+  __device__ __forceinline__ Span(const AttendArgs& g, const Piece& p) {
+    seq = p.seq;
     window = g.a.window;
-    len = first = why = 0;
-    hi = hi_all = r.tokens;
-    lo = min(r.lo, hi);
-    lo_all = min(r.lo_all, hi);
-    fb = lo / B;
-    nb = hi > lo ? (hi + B - 1) / B - fb : 0;
+    len = why = 0;
+    first = p.sight;
+    lo = p.lo; hi = p.hi; lo_all = p.lo_all; hi_all = p.hi_all;
+    fb = p.fb; nb = p.nb;
+    own = p.own;
   }
-  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B, int from = 0) {
+  __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B) {
     const si_cache_t& c = g.c;
     seq = g.a.seqs ? ((constant_t*)(uintptr_t)g.a.seqs)[seq_i] : seq_i;
     len = 0;
@@ -182,8 +184,9 @@ struct Span {
     first = len - g.a.n_new + 1;
     hi = max(0, first + t1);
     hi_all = max(0, first + t0);
-    lo = window ? max(from, first + t0 - window) : from;
-    lo_all = window ? max(from, first + t1 - window) : from;
+    lo = window ? max(0, first + t0 - window) : 0;
+    lo_all = window ? max(0, first + t1 - window) : 0;
+    own = 0;
     fb = lo / B;
     nb = hi > lo ? (hi + B - 1) / B - fb : 0;
   }
@@ -201,33 +204,17 @@ struct Sum {
   }
 };
 
-template <int MODE> __device__ __forceinline__ int own_from(const AttendArgs& g, int seq_i) {
-  if constexpr (MODE == ATTEND_OWN) return ((constant_t*)(uintptr_t)g.own_from)[seq_i];
-  else return 0;
+__device__ __forceinline__ Piece piece_of(const AttendArgs& g, int i) {
+  const constant_t* p = (const constant_t*)(uintptr_t)(g.pieces + i);
+  return Piece{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10]};
 }
-__device__ __forceinline__ SharedRows shared_rows(const AttendArgs& g, int v) {
-  const constant_t* p = (const constant_t*)(uintptr_t)(g.shared + v);
-  return SharedRows{p[0], p[1], p[2], p[3], p[4], p[5]};
-}
-// the sums of a row of a kv head over shared pages
-__device__ __forceinline__ float* shared_sum(const AttendArgs& g, int kv, int64_t row) {
+// the sums of a row of a kv head over shared positions, over its own
+__device__ __forceinline__ float* piece_sum(const AttendArgs& g, bool own, int kv, int64_t row) {
   const int64_t rows = (int64_t)g.a.n * g.a.n_new * (g.a.n_heads / g.c.n_kv_heads);
-  return g.shared_sums + (kv * rows + row) * (g.c.head_dim + 4);
+  return g.sums + ((own ? g.c.n_kv_heads + kv : kv) * rows + row) * (g.c.head_dim + 4);
 }
 
-// MODE SHARED: the sums as they are, of row `row` of the SharedRows seq_i
-template <int MODE> __device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, Sum s, float scale_v) {
-  if constexpr (MODE == ATTEND_SHARED) {
-    float* to = shared_sum(g, kv, ((const constant_t*)(uintptr_t)(g.shared + seq_i))[1] + row);
-    *reinterpret_cast<f32x4*>(to + dim) = s.o;
-    if (dim == 0) *reinterpret_cast<float2*>(to + g.c.head_dim) = make_float2(s.m, s.l);
-    return;
-  }
-  if (MODE == ATTEND_OWN && own_from<MODE>(g, seq_i) > 0) {
-    const float* from = shared_sum(g, kv, (int64_t)seq_i * g.rows + row);
-    const float2 ml = *reinterpret_cast<const float2*>(from + g.c.head_dim);
-    s.add(*reinterpret_cast<const f32x4*>(from + dim), ml.x, ml.y);
-  }
+__device__ __forceinline__ void write_row(const AttendArgs& g, int seq_i, int kv, int row, int dim, const Sum& s, float scale_v) {
   const int per = g.a.n_heads / g.c.n_kv_heads, j = row / per, head = kv * per + row % per;
   const int64_t r = (int64_t)seq_i * g.a.n_new + j;
   const float inv = s.l == 0.f ? 0.f : scale_v / s.l;
@@ -375,14 +362,13 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
 
   static __device__ void run(const AttendArgs& g, Shared& s) {
     const int block_row0 = unit_of(g).group * BLOCK_ROWS;
-    int row_end = min(g.rows, block_row0 + BLOCK_ROWS);  // (SHARED: of each sequence's own)
+    int row_end = min(g.rows, block_row0 + BLOCK_ROWS);  // (PIECES: each piece's own)
     if (RING && threadIdx.x == 0) s.again = 0;
-    const int n = MODE == ATTEND_SHARED ? *(constant_t*)(uintptr_t)g.n_shared : g.a.n;
+    const int n = MODE == ATTEND_PIECES ? *(constant_t*)(uintptr_t)g.n_pieces : g.a.n;
     const int slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
-    if (MODE == ATTEND_SHARED && n == 0) return;
     auto span_of = [&](int k) {
-      if constexpr (MODE == ATTEND_SHARED) return Span(g, shared_rows(g, k), B);
-      else return Span(g, k, t0, t1, B, own_from<MODE>(g, k));
+      if constexpr (MODE == ATTEND_PIECES) return Span(g, piece_of(g, k));
+      else return Span(g, k, t0, t1, B);
     };
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
@@ -391,7 +377,9 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     int64_t total, before = 0, counted = 0;
     int i = g.whole ? slice : 0;
     Span sp = span_of(i);
-    if (n == 1 || g.whole) {
+    if constexpr (MODE == ATTEND_PIECES) {
+      total = g.begins[n];
+    } else if (n == 1 || g.whole) {
       total = max(1, sp.nb);
     } else {
       for (int k = k0; k < k1; ++k) counted += blocks_of(k);
@@ -407,7 +395,13 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       begin = slice_end(slice - 1);
       left = slice < G ? slice_end(slice) - begin : 0;
     }
-    if (n > 1 && !g.whole) {
+    if constexpr (MODE == ATTEND_PIECES) {
+      for (int k = threadIdx.x; k < n; k += THREADS)
+        if (g.begins[k] <= begin && begin < g.begins[k + 1]) { s.first = k; s.begin = begin - g.begins[k]; }
+      __syncthreads();
+      i = __builtin_amdgcn_readfirstlane(s.first);
+      begin = __builtin_amdgcn_readfirstlane((int)s.begin);
+    } else if (n > 1 && !g.whole) {
       if (before <= begin && begin < before + counted)
         for (int k = k0; k < k1; ++k) {
           const int64_t nb = blocks_of(k);
@@ -420,14 +414,13 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     }
     // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
     int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
-    auto rows_of = [&](int k) { return MODE == ATTEND_SHARED ? shared_rows(g, k).rows : row_end; };
     for (; left > 0; ++i) {
-      if (n > 1 && !g.whole) sp = span_of(i);
-      if constexpr (MODE == ATTEND_SHARED) row_end = shared_rows(g, i).rows;
+      if (MODE == ATTEND_PIECES || (n > 1 && !g.whole)) sp = span_of(i);
+      if constexpr (MODE == ATTEND_PIECES) row_end = piece_of(g, i).rows;
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
       part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
-      if (g.slices > 1 && !g.whole) {
+      if (MODE == ATTEND_PIECES || (g.slices > 1 && !g.whole)) {
         const int64_t first_block = slice_end(slice) - left - off;
         const int first = where_to < 0 ? slice : slice_of(first_block), parts = where_to < 0 ? 1 : slice_of(first_block + nb - 1) - first + 1;
         if (where_to == 0) { un_seq[0] = i; un_first[0] = first; un_parts[0] = parts; }
@@ -451,7 +444,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       for (int k = 0; k < 2; ++k)
         if (un_seq[k] >= 0 && s.arrived[k] == (uint32_t)un_parts[k] - 1) {
           if (threadIdx.x == 0) __hip_atomic_store(g.count + un_seq[k] * gridDim.x + blockIdx.x, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          join(g, un_seq[k], un_first[k], un_parts[k], block_row0, rows_of(un_seq[k]));
+          join(g, un_seq[k], un_first[k], un_parts[k], block_row0, row_end);
         }
     }
   }
@@ -465,14 +458,18 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     const int stream = wave / TILES, row0 = block_row0 + wave % TILES * ROWS;
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
-    // this lane's rows of q, as right operands; token of a row (SHARED: of all tokens of the call), or -1
-    const int64_t row_base = MODE == ATTEND_SHARED ? shared_rows(g, seq_i).first : (int64_t)seq_i * n_new * per;
-    auto token_of = [&](int row) { return MODE == ATTEND_SHARED ? (int)((row_base + row) / per) : row / per; };
-    // what a token sees of this launch's positions
-    auto sees_to = [&](int t) { return MODE == ATTEND_SHARED ? hi : max(0, first + t); };
+    // this lane's rows of q, as right operands; token of a row (PIECES: of all tokens of the call), or -1
+    const int row_base = MODE == ATTEND_PIECES ? piece_of(g, seq_i).first : 0;
+    auto token_of = [&](int row) { return (row_base + row) / per; };
+    // what a token sees
+    auto sees_to = [&](int t) {
+      if constexpr (MODE == ATTEND_PIECES) return sp.own < 0 ? hi : max(0, first + t - sp.own * n_new);
+      else return max(0, first + t);
+    };
     auto sees_from = [&](int t) {
-      if constexpr (MODE == ATTEND_SHARED) {
+      if constexpr (MODE == ATTEND_PIECES) {
         if (!window) return 0;
+        if (sp.own >= 0) return max(0, first + t - sp.own * n_new - window);
         const int e = t / n_new, s = g.a.seqs ? g.a.seqs[e] : e;  // (members of a group have a place in the table)
         return max(0, c.lens[s] - n_new + 1 + t % n_new - window);
       } else {
@@ -485,8 +482,8 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     for (int u = 0; u < NT; ++u) {
       const int row = row0 + 16 * u + col;
       tok[u] = row < row_end ? token_of(row) : -1;
-      const int64_t q_row = MODE == ATTEND_SHARED ? (row_base + row) / per : (int64_t)seq_i * n_new + row / per;
-      const int q_head = MODE == ATTEND_SHARED ? (int)((row_base + row) % per) : row % per;
+      const int64_t q_row = MODE == ATTEND_PIECES ? token_of(row) : (int64_t)seq_i * n_new + row / per;
+      const int q_head = (row_base + row) % per;
       const uint16_t* p = static_cast<const uint16_t*>(g.a.q) + q_row * g.a.q_stride + (int64_t)(kv * per + q_head) * D;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
@@ -591,7 +588,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
         float top = -INFINITY;
         const int see_hi = tok[u] >= 0 ? sees_to(tok[u]) : 0;
         int see_lo = 0;
-        if constexpr (MODE == ATTEND_SHARED) see_lo = EDGE && tok[u] >= 0 ? sees_from(tok[u]) : 0;
+        if constexpr (MODE == ATTEND_PIECES) see_lo = EDGE && tok[u] >= 0 ? sees_from(tok[u]) : 0;
         else see_lo = window ? max(0, first + tok[u] - window) : 0;
 #pragma unroll
         for (int j = 0; j < J; ++j)
@@ -836,7 +833,13 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       for (int w = r / ROWS; w < WAVES; w += TILES) sum.add(*reinterpret_cast<const f32x4*>(&s.o[w][r % ROWS][dim]), s.m[w][r % ROWS], s.l[w][r % ROWS]);
       float* to = sums + r * (D + 2);
       if (where_to < 0) {
-        write_row<MODE>(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
+        if constexpr (MODE == ATTEND_PIECES) {
+          float* out = piece_sum(g, sp.own >= 0, kv, row_base + r);
+          *reinterpret_cast<f32x4*>(out + dim) = sum.o;
+          if (dim == 0) *reinterpret_cast<float2*>(out + D) = make_float2(sum.m, sum.l);
+        } else {
+          write_row(g, seq_i, kv, block_row0 + r, dim, sum, scale_v);
+        }
       } else if (g.last_joins) {
         put2(to + dim, sum.o[0], sum.o[1]);
         put2(to + dim + 2, sum.o[2], sum.o[3]);
@@ -871,7 +874,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
         for (int k = 0; k < AHEAD; ++k)
           if (p0 + k < parts) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
       }
-      write_row<MODE>(g, seq_i, kv, block_row0 + r, dim, sum, TYPE == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+      write_row(g, seq_i, kv, block_row0 + r, dim, sum, TYPE == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
     }
   }
 };
@@ -883,13 +886,11 @@ __global__ __launch_bounds__((Attend<TYPE, D, NT, TILES>::THREADS), (Attend<TYPE
 }
 
 // Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
-template <int D, int MODE> __device__ __forceinline__ void join_row(const AttendArgs& g, int seq_i) {
+template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   constexpr int LANES = D / 4, SHARES = 256 / LANES;
   __shared__ f32x4 s_o[SHARES][LANES];
   __shared__ float s_m[SHARES][LANES], s_l[SHARES][LANES];
-  const int kv = unit_of(g).kv, row = unit_of(g).group * g.block_rows + blockIdx.z;
-  if constexpr (MODE == ATTEND_SHARED)
-    if (row >= shared_rows(g, seq_i).rows) return;
+  const int kv = unit_of(g).kv, seq_i = blockIdx.y, row = unit_of(g).group * g.block_rows + blockIdx.z;
   const constant_t* parted = (const constant_t*)(uintptr_t)(g.parted + (int64_t)seq_i * gridDim.x + blockIdx.x);
   const int first = parted[0], parts = parted[1];
   if (row >= g.rows || parts == 1) return;  // (one part is written already)
@@ -917,18 +918,51 @@ template <int D, int MODE> __device__ __forceinline__ void join_row(const Attend
   __syncthreads();
   if (share > 0) return;
   for (int k = 1; k < min(SHARES, parts); ++k) sum.add(s_o[k][lane], s_m[k][lane], s_l[k][lane]);
-  write_row<MODE>(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
+  write_row(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
 }
-template <int D, int MODE> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
-  if constexpr (MODE == ATTEND_SHARED) {
-    // (how many there are is known on the device only)
-    for (int v = blockIdx.y; v < *(constant_t*)(uintptr_t)g.n_shared; v += gridDim.y) {
-      join_row<D, MODE>(g, v);
-      __syncthreads();
+
+// Joins what a row has over shared positions and over its own, each in parts or whole: D / 4 threads a row.
+template <int D> __global__ __launch_bounds__(256) void k_join_pieces(AttendArgs g) {
+  constexpr int LANES = D / 4, ROWS = 256 / LANES;
+  const int per = g.a.n_heads / g.c.n_kv_heads, of_entry = g.a.n_new * per, all = g.a.n * of_entry;
+  const int kv = blockIdx.x, row = blockIdx.y * ROWS + threadIdx.x / LANES, dim = threadIdx.x % LANES * 4;
+  if (threadIdx.x / LANES >= ROWS || row >= all) return;
+  const int entry = row / of_entry, n_own = g.a.n * g.chunks, n_shared = *g.n_pieces - n_own;
+  const int2 group = g.group[entry];
+  Sum sum;
+  auto add = [&](int piece, int at, bool own) {  // row `at` of the piece
+    const int2 parted = g.parted[(int64_t)piece * g.c.n_kv_heads + kv];
+    if (parted.y == 1) {
+      const float* from = piece_sum(g, own, kv, row);
+      const float2 ml = *reinterpret_cast<const float2*>(from + D);
+      sum.add(*reinterpret_cast<const f32x4*>(from + dim), ml.x, ml.y);
+      return;
     }
-  } else {
-    join_row<D, MODE>(g, blockIdx.y);
+    const int part_floats = g.part_rows * (D + 2);
+    const float* from = g.part + ((int64_t)kv * g.slices + parted.x) * 2 * part_floats + at * (D + 2);
+    constexpr int AHEAD = 8;
+    for (int p0 = 0; p0 < parted.y; p0 += AHEAD) {
+      float2 v[AHEAD][3];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int q = min(p0 + k, parted.y - 1);  // (all but the first hold the piece from before)
+        const float* p = from + (int64_t)(2 * q + (q == 0 ? 1 : 0)) * part_floats;
+        v[k][0] = *reinterpret_cast<const float2*>(p + dim);
+        v[k][1] = *reinterpret_cast<const float2*>(p + dim + 2);
+        v[k][2] = *reinterpret_cast<const float2*>(p + D);
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (p0 + k < parted.y) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
+    }
+  };
+  if (group.x >= 0) {
+    const int at = row - group.y * of_entry;
+    add(group.x + at / g.block_rows, at % g.block_rows, false);
   }
+  const int at = row - entry * of_entry;
+  add(n_shared + entry * g.chunks + at / g.block_rows, at % g.block_rows, true);
+  write_row(g, entry, kv, at, dim, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
 }
 
 template <int TYPE, int D, int MODE = ATTEND_ALL> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
@@ -938,10 +972,13 @@ template <int TYPE, int D, int MODE = ATTEND_ALL> hipError_t launch(const Attend
   else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
   else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  if (g.slices > 1 && !g.whole && !g.last_joins) {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<D, MODE>), dim3(grid.x, g.joins, g.part_rows), dim3(256), 0, stream, g);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if constexpr (MODE == ATTEND_PIECES) {
+    const int rows = 256 / (D / 4);
+    hipLaunchKernelGGL(k_join_pieces<D>, dim3(grid.x, (unsigned)((g.a.n * g.a.n_new * (g.a.n_heads / g.c.n_kv_heads) + rows - 1) / rows)), dim3(256), 0, stream, g);
+  } else if (g.slices > 1 && !g.whole && !g.last_joins) {
+    hipLaunchKernelGGL(k_join<D>, dim3(grid.x, g.a.n, g.part_rows), dim3(256), 0, stream, g);
   }
   return hipGetLastError();
 }

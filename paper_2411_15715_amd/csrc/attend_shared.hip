@@ -3,8 +3,8 @@
 // Softmax splits over positions: with m, l, o of a row over the shared positions and over its own,
 //   m' = max m,  l' = sum l 2^(m - m'),  o' = sum o 2^(m - m')
 // so neighbours of the list whose tables begin with the same pages attend to these as rows of one sequence, which is read once for all of them and
-// fills the matrix instructions, and each to what it alone has.  Launches: the plan, shared pages, own tokens (whose last step adds the
-// sums over the shared ones), with a joining launch after either where parts are left.
+// fills the matrix instructions, and each to what it alone has.  Three launches: the plan makes pieces of both kinds, shared and own; their
+// blocks, one after the other, are cut into equal slices as those of whole sequences are in si_attend; and every row's sums are joined.
 #include "si_internal.h"
 #include "si_error.h"
 #include "attend_device.h"
@@ -19,14 +19,15 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 struct PlanArgs {
   si_cache_t c;
   const int32_t* seqs;
-  int n, n_new, per, window, block_rows;
+  int n, n_new, per, window, block_rows, chunks;
   uint32_t* count;      // [1], 0 between calls
   int32_t* common;      // [n] full pages that an entry of the list has in common with the one before
-  int32_t* first_of;    // [n] first entry of an entry's group
   int32_t* tokens_of;   // [n] of a group's first entry: tokens in its shared pages
-  int32_t* n_shared;
-  SharedRows* shared;
-  int32_t* own_from;    // [n]
+  int32_t* piece_of;    // [n] of a group's first entry: its first piece, or -1
+  int32_t* n_pieces;
+  Piece* pieces;        // the groups', then those of each entry's own tokens
+  int64_t* begins;      // [n_pieces + 1]
+  int2* group;          // [n] first piece of an entry's group (-1: none), first entry of it
 };
 
 __device__ __forceinline__ int seq_at(const PlanArgs& g, int e) { return g.seqs ? g.seqs[e] : e; }
@@ -58,7 +59,12 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
   __shared__ int s_first, s_last, s_offset[WAVES];
   __shared__ Run s_run[WAVES];
   __shared__ int s_begins[WAVES];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, e = blockIdx.x;
+  __shared__ int64_t s_sum[WAVES];
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, e = blockIdx.x, B = kv_block(g.c.type);
+  if (tid == 0) {
+    const int s = seq_at(g, e), bad = s < 0 || s >= g.c.n_seqs ? SI_CACHE_BAD_SEQ : g.c.lens[s] < 0 || g.c.lens[s] > g.c.max_pages * g.c.page_tokens ? SI_CACHE_BAD_LEN : 0;
+    if (bad) atomicOr(g.c.status, bad);
+  }
   int common = 0;
   if (e > 0) {
     const int most = min(len_at(g, e), len_at(g, e - 1)) / g.c.page_tokens;
@@ -129,52 +135,88 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
       if (w < wave) at += s_offset[w];
       n_shared += s_offset[w];
     }
-    if (in) g.first_of[i] = r.first;
+    if (in) g.group[i].y = r.first;
     if (ends) {
       g.tokens_of[r.first] = tokens;
+      g.piece_of[r.first] = mine > 0 ? at : -1;
+      const int lo = g.window ? min(tokens, max(0, r.shortest - g.n_new + 1 - g.window)) : 0, lo_all = g.window ? min(tokens, max(0, r.longest - g.window)) : 0;
       for (int k = 0; k < mine; ++k)
-        g.shared[at + k] = SharedRows{r.first, r.first * g.n_new * g.per + k * g.block_rows, min(g.block_rows, rows - k * g.block_rows), tokens,
-                                      g.window ? max(0, r.shortest - g.n_new + 1 - g.window) : 0, g.window ? max(0, r.longest - g.window) : 0};
+        g.pieces[at + k] = Piece{seq_at(g, r.first), r.first * g.n_new * g.per + k * g.block_rows, min(g.block_rows, rows - k * g.block_rows), lo, tokens, lo_all, tokens,
+                                 lo / B, tokens > lo ? tokens / B - lo / B : 0, -1, 0};
     }
     carry = next;
   }
-  if (tid == 0) *g.n_shared = n_shared;
   __syncthreads();
-  for (int i = tid; i < g.n; i += THREADS) g.own_from[i] = g.tokens_of[g.first_of[i]];
+  const int n_own = g.n * g.chunks, of_entry = g.n_new * g.per;
+  for (int k = tid; k < n_own; k += THREADS) {
+    const int i = k / g.chunks, row0 = (k - i * g.chunks) * g.block_rows, rows = min(g.block_rows, of_entry - row0), first = g.group[i].y, from = g.tokens_of[first];
+    const int sight = len_at(g, i) - g.n_new + 1, t0 = row0 / g.per, t1 = (row0 + rows - 1) / g.per;
+    const int hi = max(0, sight + t1), lo = g.window ? max(from, sight + t0 - g.window) : from;
+    g.pieces[n_shared + k] = Piece{seq_at(g, i), i * of_entry + row0, rows, lo, hi, g.window ? max(from, sight + t1 - g.window) : from, max(0, sight + t0),
+                                   lo / B, hi > lo ? (hi + B - 1) / B - lo / B : 0, i, sight};
+    if (row0 == 0) g.group[i].x = g.piece_of[first];
+  }
+  __syncthreads();
+  const int n_pieces = n_shared + n_own;
+  int64_t done = 0;
+  for (int k0 = 0; k0 < n_pieces; k0 += THREADS) {
+    const int k = k0 + tid;
+    const int64_t mine = k < n_pieces ? max(1, g.pieces[k].nb) : 0;
+    int64_t x = mine;
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t o = __shfl_up(x, d);
+      if (lane >= d) x += o;
+    }
+    __syncthreads();
+    if (lane == 63) s_sum[wave] = x;
+    __syncthreads();
+    x += done - mine;
+    for (int w = 0; w < WAVES; ++w) {
+      if (w < wave) x += s_sum[w];
+      done += s_sum[w];
+    }
+    if (k < n_pieces) g.begins[k] = x;
+  }
+  if (tid == 0) {
+    g.begins[n_pieces] = done;
+    *g.n_pieces = n_pieces;
+  }
 }
 
 struct Layout {
-  AttendCut own;
-  int block_rows, slices, most;  // of the launch over shared pages; most: SharedRows
-  int64_t parted, part, sums, n_shared, shared, own_from, common, first_of, tokens_of, bytes;
+  AttendCut alone;           // of si_attend
+  bool pieces;               // else the call is si_attend
+  int block_rows, chunks, slices;
+  int64_t parted, part, sums, n_pieces, list, begins, group, common, tokens_of, piece_of, bytes;
 };
 
 Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
   Layout l{};
-  l.own = cut_attend(c, a);
-  const int64_t rows = (int64_t)a.n * a.n_new * (a.n_heads / c.n_kv_heads), each = (a.max_len + kv_block(c.type) - 1) / kv_block(c.type);
+  l.alone = cut_attend(c, a);
+  const int of_entry = a.n_new * (a.n_heads / c.n_kv_heads);
+  const int64_t rows = (int64_t)a.n * of_entry;
+  l.pieces = a.n > 1 && rows <= 200000;  // (the joining launch has a block for 4 rows and more)
   const int wide = c.head_dim <= attend_wide_dim(c.type) ? 128 : 64;
-  int most_rows = 16;  // (whatever max_len is)
-  while (most_rows < rows && most_rows < wide) most_rows *= 2;
-  l.block_rows = each > 20 ? most_rows : std::min(most_rows, 64);
+  for (l.block_rows = 16; l.block_rows < rows && l.block_rows < wide;) l.block_rows *= 2;
+  l.chunks = (of_entry + l.block_rows - 1) / l.block_rows;
   l.slices = std::max(1, (c.head_dim <= 128 ? 512 : 256) / c.n_kv_heads);
-  l.most = (int)(rows / l.block_rows + a.n / 2 + 1);
-  const int64_t most = rows / 16 + a.n / 2 + 1;
-  int64_t at = std::max<int64_t>(l.own.scratch, ATTEND_COUNTERS * 4);  // (the counters are at the same place in every call's scratch)
+  const int64_t most = rows / 16 + a.n / 2 + 1 + (int64_t)a.n * ((of_entry + 15) / 16);
+  int64_t at = std::max<int64_t>(l.alone.scratch, ATTEND_COUNTERS * 4);  // (the counters are at the same place in every call's scratch)
   auto take = [&](int64_t bytes) {
     const int64_t q = (at + 15) / 16 * 16;
     at = q + bytes;
     return q;
   };
   l.parted = take(most * c.n_kv_heads * 8);
-  l.part = take(l.slices > 1 ? (int64_t)c.n_kv_heads * l.slices * 2 * most_rows * (c.head_dim + 2) * 4 : 0);
-  l.sums = take(c.n_kv_heads * rows * (c.head_dim + 4) * 4);
-  l.n_shared = take(4);
-  l.shared = take(most * (int64_t)sizeof(SharedRows));
-  l.own_from = take(a.n * 4ll);
+  l.part = take((int64_t)c.n_kv_heads * l.slices * 2 * l.block_rows * (c.head_dim + 2) * 4);
+  l.sums = take(2 * c.n_kv_heads * rows * (c.head_dim + 4) * 4);
+  l.n_pieces = take(4);
+  l.list = take(most * (int64_t)sizeof(Piece));
+  l.begins = take((most + 1) * 8);
+  l.group = take(a.n * 8ll);
   l.common = take(a.n * 4ll);
-  l.first_of = take(a.n * 4ll);
   l.tokens_of = take(a.n * 4ll);
+  l.piece_of = take(a.n * 4ll);
   l.bytes = (at + 15) / 16 * 16;
   return l;
 }
@@ -205,26 +247,31 @@ extern "C" int si_attend_shared(const si_cache_t* c, int32_t layer, const si_att
   if (!a->scratch || a->scratch_bytes < l.bytes || (reinterpret_cast<uintptr_t>(a->scratch) & 15) != 0)
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)l.bytes);
   char* p = static_cast<char*>(a->scratch);
-  AttendArgs own = attend_args(*c, *a, layer, l.own);
-  own.shared_sums = reinterpret_cast<float*>(p + l.sums);
-  own.n_shared = reinterpret_cast<int32_t*>(p + l.n_shared);
-  own.shared = reinterpret_cast<SharedRows*>(p + l.shared);
-  own.own_from = reinterpret_cast<int32_t*>(p + l.own_from);
-  AttendArgs shared = own;
-  shared.rows = shared.block_rows = shared.part_rows = l.block_rows;
-  shared.groups = 1;
-  shared.slices = l.slices;
-  shared.whole = shared.last_joins = 0;
-  shared.joins = std::min(l.most, 8);
-  shared.count = reinterpret_cast<uint32_t*>(p);
-  shared.parted = reinterpret_cast<int2*>(p + l.parted);
-  shared.part = reinterpret_cast<float*>(p + l.part);
-  PlanArgs plan{*c, a->seqs, a->n, a->n_new, a->n_heads / c->n_kv_heads, a->window, l.block_rows, reinterpret_cast<uint32_t*>(p),
-                reinterpret_cast<int32_t*>(p + l.common), reinterpret_cast<int32_t*>(p + l.first_of), reinterpret_cast<int32_t*>(p + l.tokens_of),
-                reinterpret_cast<int32_t*>(p + l.n_shared), reinterpret_cast<SharedRows*>(p + l.shared), reinterpret_cast<int32_t*>(p + l.own_from)};
-  hipLaunchKernelGGL(k_share, dim3(a->n), dim3(THREADS), 0, (hipStream_t)stream, plan);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess) e = (c->type == SI_KV_BF16 ? launch_attend_shared_bf16 : launch_attend_shared_e4m3)(shared, own, (hipStream_t)stream);
+  AttendArgs g = attend_args(*c, *a, layer, l.alone);
+  hipError_t e = hipSuccess;
+  if (!l.pieces) {
+    e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);
+  } else {
+    g.rows = g.block_rows = g.part_rows = l.block_rows;
+    g.groups = 1;
+    g.slices = l.slices;
+    g.whole = g.last_joins = 0;
+    g.parted = reinterpret_cast<int2*>(p + l.parted);
+    g.part = reinterpret_cast<float*>(p + l.part);
+    g.sums = reinterpret_cast<float*>(p + l.sums);
+    g.chunks = l.chunks;
+    const PlanArgs plan{*c, a->seqs, a->n, a->n_new, a->n_heads / c->n_kv_heads, a->window, l.block_rows, l.chunks, reinterpret_cast<uint32_t*>(p),
+                        reinterpret_cast<int32_t*>(p + l.common), reinterpret_cast<int32_t*>(p + l.tokens_of), reinterpret_cast<int32_t*>(p + l.piece_of),
+                        reinterpret_cast<int32_t*>(p + l.n_pieces), reinterpret_cast<Piece*>(p + l.list), reinterpret_cast<int64_t*>(p + l.begins),
+                        reinterpret_cast<int2*>(p + l.group)};
+    g.n_pieces = plan.n_pieces;
+    g.pieces = plan.pieces;
+    g.begins = plan.begins;
+    g.group = plan.group;
+    hipLaunchKernelGGL(k_share, dim3(a->n), dim3(THREADS), 0, (hipStream_t)stream, plan);
+    e = hipGetLastError();
+    if (e == hipSuccess) e = (c->type == SI_KV_BF16 ? launch_attend_pieces_bf16 : launch_attend_pieces_e4m3)(g, (hipStream_t)stream);
+  }
   if (e != hipSuccess) return set_error(SI_EHIP, "attention launch failed: %s", hipGetErrorString(e));
   return SI_OK;
 }
