@@ -24,28 +24,31 @@ typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int EACH = 8;                    // neighbouring elements of a thread
-constexpr int CHUNK = THREADS * EACH;
-constexpr int MAX_CHUNKS = SI_SAMPLE_MAX_VOCAB / CHUNK;
-constexpr int RUNS = THREADS / 4;          // of a chunk, 4 threads each
+constexpr int ROUND = THREADS * EACH;      // elements that a block takes at once
+constexpr int MAX_ROUNDS = SI_SAMPLE_MAX_VOCAB / ROUND;
+constexpr int RUNS = THREADS / 4;          // of a round, 4 threads each
+constexpr int WIDE = 4;                    // rounds of a chunk where there are many
 constexpr int BINS = 2048, LIST = 2048;    // two a thread
 
 struct Args {
   si_sample_t a;
-  int chunks;
+  int rounds;      // of a row
+  int chunks;      // of a row: 1 or WIDE rounds each
+  int per;         // rounds of a chunk
   int shift;       // a weight of 1 is 2^shift
   uint32_t* count; // [rows] chunks done; 0 between calls
   double* sum;     // [rows][chunks]
   float* top;      // [rows][chunks]
   uint32_t* n;     // [rows][chunks] elements above -infinity
-  float* runs;     // [rows][chunks * RUNS]
+  float* runs;     // [rows][rounds * RUNS]
 };
 
 struct Shared {
   union {
-    struct { uint64_t w[BINS]; uint32_t n[BINS]; } hist;
+    uint64_t hist[BINS];
     uint64_t list[LIST];
   };
-  uint64_t part[MAX_CHUNKS * WAVES];  // sums of runs of 512 elements
+  uint64_t part[MAX_ROUNDS * WAVES];  // sums of runs of 512 elements
   uint64_t wave_a[WAVES], wave_b[WAVES];
   double pow2[256];                   // 2^(i / 256)
   double wave_d[WAVES];
@@ -128,53 +131,66 @@ template <int TYPE> struct Row {
   double rate;      // 256 log2(e) / T
 
   // 2^shift e^((l - top) / T) = 2^(shift + n / 256) 2^(f / 256) with n the integer next to 256 log2(e) (l - top) / T and |f| <= 1/2: a table of 256 and four
-  // terms of the series, some 2^-52 of the value off.  What is as large as the largest has 2^shift, infinite or not; -infinity has 0 at any temperature.
+  // terms of the series, some 2^-52 of the value off.  Where the largest is infinite, it alone has a weight; -infinity has 0 at any temperature (the
+  // larger of NaN and a number is the number).
   __device__ __forceinline__ double weight(float l, int shift) const {
+    if (top == INFINITY) return l == INFINITY ? ldexp(1.0, shift) : 0.0;
     const double y = fmax(((double)l - (double)top) * rate, -3e5), r = rint(y), z = (y - r) * 0.0027076061740622863;
     const int n = (int)r;
-    const double e = ldexp(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0), (n >> 8) + shift);
-    return l == top ? ldexp(1.0, shift) : l == -INFINITY ? 0.0 : e;
+    return ldexp(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0), (n >> 8) + shift);
+  }
+  __device__ __forceinline__ uint64_t whole(float l) const {
+    const double v = weight(l, g.shift - 32);
+    const uint32_t hi = (uint32_t)v;
+    return composite(hi, (uint32_t)((v - (double)hi) * 0x1p32));
+  }
+  // 2^31 of the weight of `of` (l at most) in fp32
+  __device__ __forceinline__ uint32_t roughly(float l, float of, float rate32) const {
+    return l == of ? 1u << 31 : (uint32_t)(__builtin_amdgcn_exp2f(fmaxf((l - of) * rate32, -100.f)) * 0x1p31f);
   }
 
-  // EACH elements from `at` on, NaN and what is beyond the row as -infinity
+  // EACH elements of a round, on their way; beyond the row's end -infinity
   struct Raw { u32x4 v[TYPE == SI_BF16 ? 1 : 2]; };
-  __device__ __forceinline__ void load(int at, float (&l)[EACH]) const {
+  __device__ __forceinline__ Raw fetch(int at) const {
+    Raw r;
     if (at + EACH <= vocab) {
       if constexpr (TYPE == SI_BF16) {
-        const u32x4 v = *reinterpret_cast<const u32x4_a2*>(logits + (int64_t)at * 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { l[2 * i] = __uint_as_float(v[i] << 16); l[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+        r.v[0] = *reinterpret_cast<const u32x4_a2*>(logits + (int64_t)at * 2);
       } else {
-        const u32x4 v = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4), w = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4 + 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { l[i] = __uint_as_float(v[i]); l[4 + i] = __uint_as_float(w[i]); }
+        r.v[0] = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4);
+        r.v[1] = *reinterpret_cast<const u32x4_a4*>(logits + (int64_t)at * 4 + 16);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        l[i] = -INFINITY;
-        if (at + i < vocab) {
-          if constexpr (TYPE == SI_BF16) l[i] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(logits)[at + i] << 16);
-          else l[i] = reinterpret_cast<const float*>(logits)[at + i];
+        if constexpr (TYPE == SI_BF16) {
+          const uint32_t x = at + i < vocab ? reinterpret_cast<const uint16_t*>(logits)[at + i] : 0xff80u;
+          r.v[0][i / 2] = i % 2 ? r.v[0][i / 2] | x << 16 : x;
+        } else {
+          r.v[i / 4][i % 4] = at + i < vocab ? reinterpret_cast<const uint32_t*>(logits)[at + i] : 0xff800000u;
         }
       }
     }
+    return r;
+  }
+  // NaN counts as -infinity
+  __device__ __forceinline__ void widen(const Raw& r, float (&l)[EACH]) const {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+    for (int i = 0; i < EACH; ++i) {
+      if constexpr (TYPE == SI_BF16) l[i] = __uint_as_float(i % 2 ? r.v[0][i / 2] & 0xffff0000u : r.v[0][i / 2] << 16);
+      else l[i] = __uint_as_float(r.v[i / 4][i % 4]);
+      l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+    }
   }
-  __device__ __forceinline__ uint64_t whole(float l) const {
-    const double v = weight(l, g.shift);
-    const uint32_t hi = (uint32_t)(v * 0x1p-32);
-    return composite(hi, (uint32_t)fma(-0x1p32, (double)hi, v));
-  }
-
-  // f(first element, its EACH elements) for all of the row
-  template <class F> __device__ __forceinline__ void each(F f) const {
-    for (int r = 0; r < g.chunks; ++r) {
+  // f(first element, its EACH elements, round) for the rounds [r0, r1), the next round on its way meanwhile
+  template <class F> __device__ __forceinline__ void each(int r0, int r1, F f) const {
+    Raw next = fetch(r0 * ROUND + tid * EACH);
+    for (int r = r0; r < r1; ++r) {
+      const int at = r * ROUND + tid * EACH;
       float l[EACH];
-      const int at = r * CHUNK + tid * EACH;
-      load(at, l);
-      f(at, l);
+      widen(next, l);
+      if (r + 1 < r1) next = fetch(at + ROUND);
+      if (!f(at, l, r)) break;
     }
   }
 
@@ -195,16 +211,14 @@ template <int TYPE> struct Row {
   // Their sums over runs of 512 tokens of the rounds [r0, r1), into s.part; returns the sum of all
   __device__ __forceinline__ uint64_t add_up(int r0, int r1, int what, const Left& left) const {
     __syncthreads();
-    for (int r = r0; r < r1; ++r) {
-      float l[EACH];
-      const int at = r * CHUNK + tid * EACH;
-      load(at, l);
+    each(r0, r1, [&](int at, const float (&l)[EACH], int r) {
       uint64_t sum = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
       sum = wave_total(sum);
       if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = sum;
-    }
+      return true;
+    });
     __syncthreads();
     const int parts = (r1 - r0) * WAVES;
     uint64_t before;
@@ -226,8 +240,8 @@ template <int TYPE> struct Row {
     uint64_t rest = s.found[1];
     if (tid < 64) {
       float l[EACH];
-      const int at = r0 * CHUNK + run * 64 * EACH + lane * EACH;
-      load(at, l);
+      const int at = r0 * ROUND + run * 64 * EACH + lane * EACH;
+      widen(fetch(at), l);
       uint64_t sum = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
@@ -260,10 +274,25 @@ template <int TYPE> struct Row {
   }
 
   // the list's first n entries in descending order (n <= LIST); every thread's part is in LDS before and after
-  __device__ __forceinline__ int sort(int n) const {
-    int size = 64;
-    while (size < n) size *= 2;
+  __device__ __forceinline__ void sort(int n) const {
     __syncthreads();
+    if (n <= 64) {  // one a lane of one wave
+      if (tid < 64) {
+        uint64_t v = tid < n ? s.list[tid] : 0;
+#pragma unroll
+        for (int k = 2; k <= 64; k *= 2)
+#pragma unroll
+          for (int j = k / 2; j > 0; j /= 2) {
+            const uint64_t o = __shfl_xor(v, j);
+            v = ((tid & j) == 0) == ((tid & k) == 0) ? max(v, o) : min(v, o);
+          }
+        s.list[tid] = v;
+      }
+      __syncthreads();
+      return;
+    }
+    int size = 128;
+    while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += THREADS) s.list[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int j = k / 2; j > 0; j /= 2) {
@@ -276,98 +305,143 @@ template <int TYPE> struct Row {
         }
       }
     __syncthreads();
-    return size;
   }
 
-  // elements with a key in [lo, hi] into the list, as (key, ~index); returns their number, which may be above LIST
-  __device__ __forceinline__ int collect(uint32_t lo, uint32_t hi) const {
+  // what a wave has to say, into the list as (key, ~index); s.counter counts beyond LIST too
+  __device__ __forceinline__ void listed(bool in, uint32_t key, int index) const {
+    const unsigned long long who = __ballot(in);
+    if (who == 0) return;
+    uint32_t to = 0;
+    if (tid % 64 == 0) to = atomicAdd(&s.counter, (uint32_t)__popcll(who));
+    to = __builtin_amdgcn_readfirstlane(to) + __popcll(who & ((1ull << (tid % 64)) - 1));
+    if (in && to < LIST) s.list[to] = composite(key, ~(uint32_t)index);
+  }
+  // elements with a key of lo or more into the list; returns their number, or some number above LIST
+  __device__ __forceinline__ int collect(uint32_t lo) const {
     __syncthreads();
     if (tid == 0) s.counter = 0;
     __syncthreads();
-    each([&](int at, const float (&l)[EACH]) {
+    each(0, g.rounds, [&](int at, const float (&l)[EACH], int) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const uint32_t key = route_key(l[i]);
-        const bool in = key >= lo && key <= hi && l[i] > -INFINITY;
-        if (in) {
-          const uint32_t to = atomicAdd(&s.counter, 1u);
-          if (to < LIST) s.list[to] = composite(key, ~(uint32_t)(at + i));
-        }
+        listed(key >= lo && l[i] > -INFINITY, key, at + i);
       }
+      // (a wave may see a count of the round that others are in: it only goes on for nothing)
+      return *(volatile uint32_t*)&s.counter <= LIST;
     });
     __syncthreads();
     return (int)s.counter;
   }
 
-  struct Border { uint32_t key, index; uint64_t n, w; };  // the last token left, and how many they are with it and their sum
+  // The last token left, how many they are with it and the sum of their weights; summed: s.part holds the sums of what is left
+  struct Border { uint32_t key, index; uint64_t n, w; bool summed; };
 
-  // Border of the first token at which the number (by_n) or the sum of those up to it reaches `need`, among keys of [lo, hi]: those above hi do not exist
+  // Border of the first token at which the number (by_n) or the sum of those up to it reaches `need`, among keys of [lo, hi] (none is above hi); where none
+  // does, of the last.  A pass puts numbers or rough sums of the range into bins of its leading bits; the next takes what is above the bin in which they reach
+  // `need` exactly, and lists what is in it.  Where that shows another bin, or the list is full, once more with what is left of the range.
   __device__ __forceinline__ Border border(uint32_t lo, uint32_t hi, bool by_n, uint64_t need) const {
-    uint64_t n_above = 0, w_above = 0;
-    uint32_t inside;
+    uint64_t done = 0;  // number or sum above hi, as far as known
+    const float rate32 = (float)(rate / 256);
     for (;;) {
       const uint32_t width = hi - lo;
       const int drop = max(0, 32 - __clz((int)width) - 11);  // (at most BINS bins of 2^drop keys)
       __syncthreads();
-      for (int i = tid; i < BINS; i += THREADS) { s.hist.w[i] = 0; s.hist.n[i] = 0; }
+      for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
+      if (tid == 0) { s.counter = 0; s.found[0] = 0; }
+      const float of = value_of(hi);
       __syncthreads();
-      each([&](int, const float (&l)[EACH]) {
+      each(0, g.rounds, [&](int, const float (&l)[EACH], int) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
           const uint32_t key = route_key(l[i]);
-          if (key >= lo && key <= hi && l[i] > -INFINITY) {
-            const uint32_t b = (hi - key) >> drop;
-            atomicAdd(&s.hist.n[b], 1u);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist.w[b]), (unsigned long long)whole(l[i]));
+          if (key >= lo && key <= hi && l[i] > -INFINITY)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[(hi - key) >> drop]), by_n ? 1ull : (unsigned long long)roughly(l[i], of, rate32));
+        }
+        return true;
+      });
+      __syncthreads();
+      const uint64_t h0 = s.hist[2 * tid], h1 = s.hist[2 * tid + 1], goal = by_n ? need - done : (uint64_t)fmin(fmax((double)(need - done) / weight(of, g.shift) * 0x1p31, 1.0), 1e18);
+      uint64_t x;
+      scan(h0 + h1, x, s.wave_a);
+      // (the last bin that begins below the goal and is not empty: the goal's, or the last of all)
+      if (h1 > 0 && x + h0 < goal) atomicMax(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)(2 * tid + 2));
+      else if (h0 > 0 && x < goal) atomicMax(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)(2 * tid + 1));
+      __syncthreads();
+      const uint32_t bin = max((int)s.found[0] - 1, 0);  // (weights that are all roughly 0: the first)
+      const uint32_t top_of = hi - (bin << drop), low_of = max(lo, top_of - ((1u << drop) - 1));
+      __syncthreads();
+      uint64_t n_above = 0;
+      each(0, g.rounds, [&](int at, const float (&l)[EACH], int r) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          const uint32_t key = route_key(l[i]);
+          const bool there = l[i] > -INFINITY;
+          listed(there && key >= low_of && key <= top_of, key, at + i);
+          if (there && key > top_of) {
+            sum += whole(l[i]);
+            ++n_above;
           }
           one_by_one();
         }
+        sum = wave_total(sum);
+        if (tid % 64 == 0) s.part[r * WAVES + tid / 64] = sum;
+        return true;
       });
-      if (tid == 0) s.found[0] = ~0ull;
       __syncthreads();
-      const uint64_t n0 = s.hist.n[2 * tid], n1 = s.hist.n[2 * tid + 1], w0 = s.hist.w[2 * tid], w1 = s.hist.w[2 * tid + 1];
-      uint64_t n_before, w_before;
-      const uint64_t n_all = scan(n0 + n1, n_before, s.wave_a), w_all = scan(w0 + w1, w_before, s.wave_b);
-      n_before += n_above;
-      w_before += w_above;
-      const uint64_t goal = by_n ? min(need, n_above + n_all) : min(need, w_above + w_all);
-      const uint64_t x0 = by_n ? n_before : w_before, d0 = by_n ? n0 : w0, d1 = by_n ? n1 : w1;
-      if (x0 < goal && goal <= x0 + d0 + d1) {
-        const bool second = goal > x0 + d0;
-        s.found[0] = 2 * tid + second;
-        s.found[1] = n_before + (second ? n0 : 0);
-        s.found[2] = w_before + (second ? w0 : 0);
-        s.found[3] = second ? n1 : n0;
+      uint64_t unused;
+      const int parts = g.rounds * WAVES, inside = (int)s.counter;
+      const uint64_t w_above = scan((2 * tid < parts ? s.part[2 * tid] : 0) + (2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0), unused, s.wave_a);
+      n_above = scan(n_above, unused, s.wave_b);
+      const uint64_t above = by_n ? n_above : w_above;
+      if (above >= need && top_of < hi) {  // the border is above this bin
+        lo = top_of + 1;
+        continue;
       }
-      __syncthreads();
-      const uint32_t bin = (uint32_t)s.found[0];
-      n_above = s.found[1];
-      w_above = s.found[2];
-      inside = (uint32_t)s.found[3];
-      need = goal;
-      hi -= bin << drop;
-      lo = max(lo, hi - ((1u << drop) - 1));
-      if (inside <= LIST || drop == 0) break;
-    }
-    Border r;
-    if (inside <= LIST) {
-      const int n = collect(lo, hi);
-      sort(n);
+      if (inside > LIST && drop > 0) {
+        lo = low_of;
+        hi = top_of;
+        done = above;
+        continue;
+      }
+      if (inside > LIST) {  // more tokens of one logit than the list holds: as many as are needed, from the lowest index
+        const uint64_t each_w = whole(value_of(top_of)), most = inside;
+        const uint64_t k = by_n ? min(need - above, most) : each_w == 0 ? most : min((need - above + each_w - 1) / each_w, most);
+        if (low_of > lo && (by_n ? above + most : above + most * each_w) < need) {
+          hi = low_of - 1;
+          done = by_n ? above + most : above + most * each_w;
+          continue;
+        }
+        const Left same{top_of, 0, 0.0};
+        add_up(0, g.rounds, SAME, same);
+        const int at = locate(0, g.rounds, SAME, same, k - 1);
+        return Border{top_of, (uint32_t)at, n_above + k, w_above + k * each_w, false};
+      }
+      sort(inside);
       uint64_t e[2], w[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        e[i] = 2 * tid + i < n ? s.list[2 * tid + i] : 0;
-        w[i] = 2 * tid + i < n ? whole(value_of((uint32_t)(e[i] >> 32))) : 0;
+        e[i] = 2 * tid + i < inside ? s.list[2 * tid + i] : 0;
+        w[i] = 2 * tid + i < inside ? whole(value_of((uint32_t)(e[i] >> 32))) : 0;
       }
       uint64_t before;
-      scan(w[0] + w[1], before, s.wave_a);
+      const uint64_t listed_w = scan(w[0] + w[1], before, s.wave_a), all = by_n ? n_above + inside : w_above + listed_w;
+      if (all < need && low_of > lo) {  // the border is below this bin
+        hi = low_of - 1;
+        done = all;
+        continue;
+      }
+      const uint64_t last = min(need, all);
       before += w_above;
-      // (the bin holds the border: one of its entries reaches the goal)
+      if (tid == 0) s.found[0] = 0;
+      __syncthreads();
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint64_t at = n_above + 2 * tid + i + 1;
-        const bool here = 2 * tid + i < n && (by_n ? at == need : before < need && need <= before + w[i]);
-        if (here) {
+        if (2 * tid + i < inside && (by_n ? at <= last : before < last || 2 * tid + i == 0))  // left
+          atomicAdd(reinterpret_cast<unsigned long long*>(&s.part[~(uint32_t)e[i] / (64 * EACH)]), (unsigned long long)w[i]);
+        if (2 * tid + i < inside && (by_n ? at == last : (before < last || 2 * tid + i == 0) && (before + w[i] >= last || 2 * tid + i + 1 == inside))) {
           s.found[0] = e[i];
           s.found[1] = at;
           s.found[2] = before + w[i];
@@ -375,17 +449,8 @@ template <int TYPE> struct Row {
         before += w[i];
       }
       __syncthreads();
-      r = Border{(uint32_t)(s.found[0] >> 32), ~(uint32_t)s.found[0], s.found[1], s.found[2]};
-    } else {  // more tokens of one logit than the list holds: as many as are needed, from the lowest index
-      const uint64_t each_w = whole(value_of(lo));
-      const uint64_t k = by_n ? need - n_above : (need - w_above + each_w - 1) / each_w;
-      const Left same{lo, 0, 0.0};
-      add_up(0, g.chunks, SAME, same);
-      const int at = locate(0, g.chunks, SAME, same, k - 1);
-      r = Border{lo, (uint32_t)at, n_above + k, w_above + k * each_w};
+      return Border{(uint32_t)(s.found[0] >> 32), ~(uint32_t)s.found[0], s.found[1], s.found[2], true};
     }
-    __syncthreads();
-    return r;
   }
 
   __device__ __forceinline__ void write(int token, double prob, int kept) const {
@@ -396,63 +461,114 @@ template <int TYPE> struct Row {
   }
 };
 
-template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) {
-  __shared__ Shared s;
-  const int row = blockIdx.x / g.chunks, chunk = blockIdx.x % g.chunks, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const si_sample_t& a = g.a;
-  constexpr int BYTES = TYPE == SI_BF16 ? 2 : 4;
-  const float t = a.temperature ? a.temperature[row] : 1.f;
-  const bool greedy = !(t > 0.f);
-  const int k = a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.vocab ? a.top_k[row] : 0;
-  const float p_given = a.top_p ? a.top_p[row] : 1.f, m_given = a.min_p ? a.min_p[row] : 0.f;
-  const bool by_p = p_given < 1.f, by_m = m_given > 0.f;
-  const double p = fmaxf(p_given, 0.f), least = fminf(m_given, 1.f);
-  const bool summed = !greedy && k == 0 && (by_p || !by_m);
-  Row<TYPE> R{g, s, static_cast<const char*>(a.logits) + (int64_t)row * a.stride * BYTES, a.vocab, row, tid, 0.f, greedy ? 0.0 : 369.3299304675746 / (double)t};
-  if (tid < 256) s.pow2[tid] = exp2(tid / 256.0);
+// What a row is asked for
+struct Wishes {
+  float t;
+  int k;               // 0: no limit
+  bool greedy, by_p, by_m;
+  double p, least;
+  bool summed, all_left;
+  __device__ __forceinline__ Wishes(const si_sample_t& a, int row) {
+    t = a.temperature ? a.temperature[row] : 1.f;
+    greedy = !(t > 0.f);
+    k = a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.vocab ? a.top_k[row] : 0;
+    const float p_given = a.top_p ? a.top_p[row] : 1.f, m_given = a.min_p ? a.min_p[row] : 0.f;
+    by_p = p_given < 1.f;
+    by_m = m_given > 0.f;
+    p = fmaxf(p_given, 0.f);
+    least = fminf(m_given, 1.f);
+    all_left = !greedy && k == 0 && !by_p && !by_m;
+    summed = !greedy && k == 0 && (by_p || !by_m);  // the sum over the whole row is needed
+  }
+};
+template <int TYPE> __device__ __forceinline__ Row<TYPE> row_of(const Args& g, Shared& s, int row, const Wishes& w) {
+  if (threadIdx.x < 256) s.pow2[threadIdx.x] = exp2(threadIdx.x / 256.0);
+  return Row<TYPE>{g, s, static_cast<const char*>(g.a.logits) + (int64_t)row * g.a.stride * (TYPE == SI_BF16 ? 2 : 4), g.a.vocab, row, (int)threadIdx.x, 0.f,
+                   w.greedy ? 0.0 : 369.3299304675746 / (double)w.t};
+}
 
-  {
-    float l[EACH];
-    R.load(chunk * CHUNK + tid * EACH, l);
-    float top = l[0];
-    uint32_t n = 0;
+// A chunk of PER rounds: its maximum, number of tokens, sum, and the maxima of its runs
+template <int TYPE, int PER> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, const Wishes& w, int chunk) {
+  const Args& g = R.g;
+  Shared& s = R.s;
+  const int tid = threadIdx.x, lane = tid % 64, r0 = chunk * PER;
+  typename Row<TYPE>::Raw raw[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) raw[j] = R.fetch((r0 + j) * ROUND + tid * EACH);
+  float top = -INFINITY;
+  uint32_t n = 0;
+  if (tid == 0) s.counter = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    float l[EACH], most = -INFINITY;
+    R.widen(raw[j], l);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      top = fmaxf(top, l[i]);
+      most = fmaxf(most, l[i]);
       n += __popcll(__ballot(l[i] > -INFINITY));
     }
-    if (k > 0) {
-      float run = fmaxf(top, __shfl_xor(top, 1));
-      run = fmaxf(run, __shfl_xor(run, 2));
-      if (lane % 4 == 0) put(g.runs + ((int64_t)row * g.chunks + chunk) * RUNS + tid / 4, run);
+    top = fmaxf(top, most);
+    if (w.k > 0 && r0 + j < g.rounds) {
+      most = fmaxf(most, __shfl_xor(most, 1));
+      most = fmaxf(most, __shfl_xor(most, 2));
+      if (lane % 4 == 0) put(g.runs + ((int64_t)R.row * g.rounds + r0 + j) * RUNS + tid / 4, most);
     }
-    if (tid == 0) s.counter = 0;
-    top = block_max(top, s);
-    double sum = 0.0;
-    if (summed) {
-      R.top = top;
+  }
+  top = block_max(top, s);
+  double sum = 0.0;
+  if (w.summed) {
+    R.top = top;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      float l[EACH];
+      R.widen(raw[j], l);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { sum += R.weight(l[i], 0); one_by_one(); }
-      sum = block_sum(sum, s);
     }
-    if (lane == 0) atomicAdd(&s.counter, n);
-    __syncthreads();
-    if (tid == 0) {
-      const int64_t at = (int64_t)row * g.chunks + chunk;
-      put(g.top + at, top);
-      put(g.n + at, s.counter);
-      put(g.sum + at, sum);
-    }
+    sum = block_sum(sum, s);
   }
-  // all of this block's values have reached memory before it is counted
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (lane == 0) atomicAdd(&s.counter, n);
   __syncthreads();
   if (tid == 0) {
-    s.last = __hip_atomic_fetch_add(g.count + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)g.chunks - 1;
-    if (s.last) put(g.count + row, 0u);
+    const int64_t at = (int64_t)R.row * g.chunks + chunk;
+    put(g.top + at, top);
+    put(g.n + at, s.counter);
+    put(g.sum + at, sum);
   }
-  __syncthreads();
-  if (!s.last) return;
+}
+
+// Many rows: a launch for the chunks alone, two blocks a compute unit
+template <int TYPE> __global__ __launch_bounds__(THREADS, 8) void k_sample_sums(Args g) {
+  __shared__ Shared s;
+  const int row = blockIdx.x / g.chunks;
+  const Wishes w(g.a, row);
+  Row<TYPE> R = row_of<TYPE>(g, s, row, w);
+  sums_of_chunk<TYPE, WIDE>(R, w, blockIdx.x % g.chunks);
+}
+
+// ALONE: the chunks too, and the block of a row that finishes last goes on; else a block a row
+template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) {
+  __shared__ Shared s;
+  const int row = ALONE ? blockIdx.x / g.chunks : blockIdx.x, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const si_sample_t& a = g.a;
+  const Wishes w(a, row);
+  Row<TYPE> R = row_of<TYPE>(g, s, row, w);
+  if constexpr (ALONE) {
+    sums_of_chunk<TYPE, 1>(R, w, blockIdx.x % g.chunks);
+    // all of this block's values have reached memory before it is counted
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+      s.last = __hip_atomic_fetch_add(g.count + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)g.chunks - 1;
+      if (s.last) put(g.count + row, 0u);
+    }
+    __syncthreads();
+    if (!s.last) return;
+  }
+  const float t = w.t;
+  const int k = w.k;
+  const bool greedy = w.greedy, by_p = w.by_p, by_m = w.by_m, summed = w.summed, all_left = w.all_left;
+  const double p = w.p, least = w.least;
 
   // The row's largest, its number of tokens, and its sum
   const int64_t first = (int64_t)row * g.chunks;
@@ -466,11 +582,12 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
   const float u = a.u[row];
   const double one = ldexp(1.0, g.shift);
   // How the row is gone through in the end, and with which target
-  int r0 = 0, r1 = g.chunks, what = R.WEIGHT;
+  int r0 = 0, r1 = g.rounds, what = R.WEIGHT;
   typename Row<TYPE>::Left left{route_key(-3.402823466e38f), 0xffffffffu, by_m ? least : 0.0};
   double sum = 0.0, rest = 0.0;
   int kept = (int)n_all;
-  const bool all_left = !greedy && k == 0 && !by_p && !by_m;
+  uint64_t w_all = 0;
+  bool added = false;  // s.part has the sums of what is left
   auto drawn = [&](uint64_t all) { return !(u > 0.f) ? 0 : u >= 1.f ? all - 1 : min((uint64_t)((double)u * (double)all), all - 1); };
   if (greedy) {
     // in the first chunk that has it
@@ -480,7 +597,8 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
     __syncthreads();
 #pragma unroll 1
     for (int w = WAVES - 1; w >= 0; --w) r0 = s.wave_a[w] != ~0ull ? (int)s.wave_a[w] : r0;
-    r1 = r0 + 1;
+    r0 *= g.per;
+    r1 = min(r0 + g.per, g.rounds);
     what = R.SAME;
     left.key = top_key;
     kept = 1;
@@ -507,9 +625,10 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
       if (share > 0.0 && begin <= target) atomicMax(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)tid);
       __syncthreads();
       r0 = (int)s.found[0];
-      r1 = r0 + 1;
       if (tid == r0) s.wave_d[0] = target - begin;
       __syncthreads();
+      r0 *= g.per;
+      r1 = min(r0 + g.per, g.rounds);
       rest = fmax(s.wave_d[0], 0.0);
     }
   }
@@ -518,21 +637,21 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
   float bound = -3.402823466e38f;
   if (k > 0) {
     // the k-th largest of the runs' maxima, by 22 leading bits of its key (a little below it)
-    const int runs = g.chunks * RUNS;
+    const int runs = g.rounds * RUNS;
     uint32_t lo = 0;
     if (k <= runs) {
       uint32_t need = k;
       for (int level = 0; level < 2; ++level) {
         __syncthreads();
-        for (int i = tid; i < BINS; i += THREADS) s.hist.n[i] = 0;
+        for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
         __syncthreads();
         for (int i = tid; i < runs; i += THREADS) {
           const uint32_t key = route_key(get(g.runs + (int64_t)row * runs + i));
-          if (level == 0) atomicAdd(&s.hist.n[2047 - (key >> 21)], 1u);
-          else if ((key >> 21) == (lo >> 21)) atomicAdd(&s.hist.n[2047 - ((key >> 10) & 2047)], 1u);
+          if (level == 0) atomicAdd(reinterpret_cast<uint32_t*>(&s.hist[2047 - (key >> 21)]), 1u);
+          else if ((key >> 21) == (lo >> 21)) atomicAdd(reinterpret_cast<uint32_t*>(&s.hist[2047 - ((key >> 10) & 2047)]), 1u);
         }
         __syncthreads();
-        const uint32_t n0 = s.hist.n[2 * tid], n1 = s.hist.n[2 * tid + 1];
+        const uint32_t n0 = (uint32_t)s.hist[2 * tid], n1 = (uint32_t)s.hist[2 * tid + 1];
         uint64_t x;
         scan(n0 + n1, x, s.wave_a);
         if (x < need && need <= x + n0 + n1) {
@@ -556,7 +675,7 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
   const uint32_t bound_key = route_key(bound);
 
   // Few: in order, all at once
-  const int few = k > 0 && k > LIST ? LIST + 1 : R.collect(bound_key, top_key);
+  const int few = k > LIST ? LIST + 1 : R.collect(bound_key);
   if (few <= LIST) {
     R.sort(few);
     uint64_t e[2], w[2];
@@ -602,7 +721,7 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
     return;
   }
   // Many: the border by number, then by sum
-  uint64_t w_all = (uint64_t)(sum * one);
+  w_all = (uint64_t)(sum * one);
   for (int by_n = 1; by_n >= 0; --by_n) {
     if (by_n ? k == 0 : !by_p) continue;
     const auto b = R.border(bound_key, top_key, by_n, by_n ? (uint64_t)k : max((uint64_t)1, (uint64_t)ceil(p * (double)w_all)));
@@ -610,24 +729,25 @@ template <int TYPE> __global__ __launch_bounds__(THREADS) void k_sample(Args g) 
     left.index = b.index;
     kept = (int)b.n;
     w_all = b.w;
+    added = b.summed && !by_m;
   }
-  if (by_m) kept = (int)R.add_up(0, g.chunks, R.NUMBER, left);
+  if (by_m) kept = (int)R.add_up(0, g.rounds, R.NUMBER, left);
   }
-  uint64_t total = R.add_up(r0, r1, what, left);
+  uint64_t total = added ? w_all : R.add_up(r0, r1, what, left);
   uint64_t target = greedy ? 0 : drawn(total);
   if (all_left) {
     if (total > 0) {
       target = u >= 1.f ? total - 1 : min((uint64_t)(rest * one), total - 1);
     } else {  // (a chunk of weights that are all below the smallest integer)
       r0 = 0;
-      r1 = g.chunks;
+      r1 = g.rounds;
       total = R.add_up(r0, r1, what, left);
       target = drawn(total);
     }
   }
   const int at = R.locate(r0, r1, what, left, target);
-  const double w = R.weight(R.logit(at), 0);
-  R.write(at, greedy ? 1.0 : all_left ? w / sum : w * one / (double)total, kept);
+  const double mine = R.weight(R.logit(at), 0);
+  R.write(at, greedy ? 1.0 : all_left ? mine / sum : mine * one / (double)total, kept);
 }
 
 bool misaligned(const void* p, int to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
@@ -636,13 +756,13 @@ int check(const si_sample_t* a, const char* who) {
   if (!a) return set_error(SI_EINVAL, "%s: descriptor is NULL", who);
   if (a->type != SI_F32 && a->type != SI_BF16) return set_error(SI_EINVAL, "%s: unknown type %d", who, a->type);
   if (a->rows < 0 || a->rows > SI_SAMPLE_MAX_ROWS || a->vocab < 1 || a->vocab > SI_SAMPLE_MAX_VOCAB) return set_error(SI_EINVAL, "%s: rows %d, vocab %d", who, a->rows, a->vocab);
-  if ((int64_t)a->rows * ((a->vocab + CHUNK - 1) / CHUNK) >= (1 << 22)) return set_error(SI_EINVAL, "%s: too many rows in one call (%d of %d)", who, a->rows, a->vocab);
+  if ((int64_t)a->rows * ((a->vocab + ROUND - 1) / ROUND) >= (1 << 22)) return set_error(SI_EINVAL, "%s: too many rows in one call (%d of %d)", who, a->rows, a->vocab);
   return SI_OK;
 }
 
 // Places in the scratch; returns its size
 int64_t lay_out(const si_sample_t& a, Args* g) {
-  const int64_t chunks = (a.vocab + CHUNK - 1) / CHUNK, n = a.rows * chunks;
+  const int64_t rounds = (a.vocab + ROUND - 1) / ROUND, n = a.rows * rounds;
   char* p = static_cast<char*>(a.scratch);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -657,7 +777,7 @@ int64_t lay_out(const si_sample_t& a, Args* g) {
   uint32_t* each = reinterpret_cast<uint32_t*>(take(4 * n));
   float* runs = reinterpret_cast<float*>(take(4 * n * RUNS));
   if (g) {
-    g->chunks = (int)chunks;
+    g->rounds = (int)rounds;
     g->count = count;
     g->sum = sum;
     g->top = top;
@@ -693,9 +813,25 @@ extern "C" int si_sample(const si_sample_t* a, void* stream) {
   int log2 = 0;
   while ((1 << log2) < a->vocab) ++log2;
   g.shift = 62 - log2;
-  const dim3 grid((unsigned)(a->rows * g.chunks));
-  if (a->type == SI_BF16) hipLaunchKernelGGL(k_sample<SI_BF16>, grid, dim3(THREADS), 0, (hipStream_t)stream, g);
-  else hipLaunchKernelGGL(k_sample<SI_F32>, grid, dim3(THREADS), 0, (hipStream_t)stream, g);
+  // One launch where the chunks fill the chip twice at most (its blocks have registers for the row's end: one a compute unit)
+  const bool alone = (int64_t)a->rows * g.rounds <= 512;
+  g.per = alone ? 1 : WIDE;
+  g.chunks = (g.rounds + g.per - 1) / g.per;
+  const dim3 chunks((unsigned)(a->rows * g.chunks)), rows((unsigned)a->rows), block(THREADS);
+  const hipStream_t st = (hipStream_t)stream;
+  if (!alone) {
+    if (a->type == SI_BF16) hipLaunchKernelGGL(k_sample_sums<SI_BF16>, chunks, block, 0, st, g);
+    else hipLaunchKernelGGL(k_sample_sums<SI_F32>, chunks, block, 0, st, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return set_error(SI_EHIP, "sample launch failed: %s", hipGetErrorString(e));
+  }
+  if (a->type == SI_BF16) {
+    if (alone) hipLaunchKernelGGL((k_sample<SI_BF16, true>), chunks, block, 0, st, g);
+    else hipLaunchKernelGGL((k_sample<SI_BF16, false>), rows, block, 0, st, g);
+  } else {
+    if (alone) hipLaunchKernelGGL((k_sample<SI_F32, true>), chunks, block, 0, st, g);
+    else hipLaunchKernelGGL((k_sample<SI_F32, false>), rows, block, 0, st, g);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(SI_EHIP, "sample launch failed: %s", hipGetErrorString(e));
   return SI_OK;
