@@ -29,6 +29,7 @@ constexpr int MAX_ROUNDS = SI_SAMPLE_MAX_VOCAB / ROUND;
 constexpr int RUNS = THREADS / 4;          // of a round, 4 threads each
 constexpr int WIDE = 4;                    // rounds of a chunk where there are many
 constexpr int BINS = 2048, LIST = 2048;    // two a thread
+constexpr int QUEUE = 128;                 // of a wave
 
 struct Args {
   si_sample_t a;
@@ -50,6 +51,7 @@ struct Shared {
   };
   uint64_t part[MAX_ROUNDS * WAVES];  // sums of runs of 512 elements
   uint64_t wave_a[WAVES], wave_b[WAVES];
+  float queue[WAVES][QUEUE];
   double pow2[256];                   // 2^(i / 256)
   double wave_d[WAVES];
   float wave_f[WAVES];
@@ -62,12 +64,24 @@ template <class T> __device__ __forceinline__ void put(T* p, T v) { __hip_atomic
 template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+// order-preserving, of what widen() gives
+__device__ __forceinline__ uint32_t key_of(float l) {
+  const uint32_t u = __float_as_uint(l);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number: below it -infinity
+
 __device__ __forceinline__ float a_little_below(double v) {
   const float f = (float)v;
   return f - fabsf(f) * 1e-6f - 1e-30f;
 }
 __device__ __forceinline__ uint64_t composite(uint32_t hi, uint32_t lo) { return (uint64_t)hi << 32 | lo; }
 
+// LDS of a wave: its accesses are in order, only the compiler has to keep it
+__device__ __forceinline__ void wave_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
 // Elements of a thread one after the other: eight series at once do not fit the registers of 16 waves
 __device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
 
@@ -131,19 +145,24 @@ template <int TYPE> struct Row {
   double rate;      // 256 log2(e) / T
 
   // 2^shift e^((l - top) / T) = 2^(shift + n / 256) 2^(f / 256) with n the integer next to 256 log2(e) (l - top) / T and |f| <= 1/2: a table of 256 and four
-  // terms of the series, some 2^-52 of the value off.  Where the largest is infinite, it alone has a weight; -infinity has 0 at any temperature (the
-  // larger of NaN and a number is the number).
+  // terms of the series, some 2^-52 of the value off.  Where the largest is infinite, it alone has a weight; what is -infinity or far below has
+  // 2^-976 (the larger of NaN and a number is the number).  Adding 1.5 2^52 rounds to an integer and leaves it in the low bits; the power of two goes
+  // to the exponent's bits (conversions and ldexp of doubles are slow: 134 MB of logits 57 us with them).
   __device__ __forceinline__ double weight(float l, int shift) const {
     if (top == INFINITY) return l == INFINITY ? ldexp(1.0, shift) : 0.0;
-    const double y = fmax(((double)l - (double)top) * rate, -3e5), r = rint(y), z = (y - r) * 0.0027076061740622863;
-    const int n = (int)r;
-    return ldexp(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0), (n >> 8) + shift);
+    constexpr double ROUND_IT = 0x1.8p52;
+    const double y = fmax(((double)l - (double)top) * rate, -250000.0), up = y + ROUND_IT, z = (y - (up - ROUND_IT)) * 0.0027076061740622863;
+    const int n = (int)__double_as_longlong(up);
+    const long long e = __double_as_longlong(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0));
+    return __longlong_as_double(e + ((long long)((n >> 8) + shift) << 52));
   }
+  // the same as an integer, what is below 1 cut off
   __device__ __forceinline__ uint64_t whole(float l) const {
-    const double v = weight(l, g.shift - 32);
-    const uint32_t hi = (uint32_t)v;
-    return composite(hi, (uint32_t)((v - (double)hi) * 0x1p32));
+    const uint64_t v = (uint64_t)__double_as_longlong(weight(l, g.shift));
+    const int exponent = (int)(v >> 52) - 1023;  // (at most 62, as the weights are)
+    return exponent < 0 ? 0 : ((v & 0xfffffffffffffull) | 1ull << 52) << 10 >> (62 - exponent);
   }
+
   // 2^31 of the weight of `of` (l at most) in fp32
   __device__ __forceinline__ uint32_t roughly(float l, float of, float rate32) const {
     return l == of ? 1u << 31 : (uint32_t)(__builtin_amdgcn_exp2f(fmaxf((l - of) * rate32, -100.f)) * 0x1p31f);
@@ -173,13 +192,13 @@ template <int TYPE> struct Row {
     }
     return r;
   }
-  // NaN counts as -infinity
+  // NaN counts as -infinity, -0 as 0
   __device__ __forceinline__ void widen(const Raw& r, float (&l)[EACH]) const {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       if constexpr (TYPE == SI_BF16) l[i] = __uint_as_float(i % 2 ? r.v[0][i / 2] & 0xffff0000u : r.v[0][i / 2] << 16);
       else l[i] = __uint_as_float(r.v[i / 4][i % 4]);
-      l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+      l[i] = (l[i] == l[i] ? l[i] : -INFINITY) + 0.f;
     }
   }
   // f(first element, its EACH elements, round) for the rounds [r0, r1), the next round on its way meanwhile
@@ -201,7 +220,7 @@ template <int TYPE> struct Row {
     double least;         // and what a weight has to reach (0: nothing)
   };
   __device__ __forceinline__ uint64_t adds(int what, const Left& left, float l, int i) const {
-    const uint32_t key = route_key(l);
+    const uint32_t key = key_of(l);
     if (l == -INFINITY) return 0;
     if (what == SAME) return key == left.key;
     if (key < left.key || (key == left.key && (uint32_t)i > left.index)) return 0;
@@ -324,8 +343,8 @@ template <int TYPE> struct Row {
     each(0, g.rounds, [&](int at, const float (&l)[EACH], int) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        const uint32_t key = route_key(l[i]);
-        listed(key >= lo && l[i] > -INFINITY, key, at + i);
+        const uint32_t key = key_of(l[i]);
+        listed(key >= lo, key, at + i);
       }
       // (a wave may see a count of the round that others are in: it only goes on for nothing)
       return *(volatile uint32_t*)&s.counter <= LIST;
@@ -354,8 +373,8 @@ template <int TYPE> struct Row {
       each(0, g.rounds, [&](int, const float (&l)[EACH], int) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-          const uint32_t key = route_key(l[i]);
-          if (key >= lo && key <= hi && l[i] > -INFINITY)
+          const uint32_t key = key_of(l[i]);
+          if (key >= lo && key <= hi)
             atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[(hi - key) >> drop]), by_n ? 1ull : (unsigned long long)roughly(l[i], of, rate32));
         }
         return true;
@@ -371,20 +390,31 @@ template <int TYPE> struct Row {
       const uint32_t bin = max((int)s.found[0] - 1, 0);  // (weights that are all roughly 0: the first)
       const uint32_t top_of = hi - (bin << drop), low_of = max(lo, top_of - ((1u << drop) - 1));
       __syncthreads();
+      // What is above goes through a queue of its wave, so that weights are formed by 64 lanes that have one each.  (By the lanes that found them, a third
+      // of 131072 or not: 50 vector instructions an element, this way 25.)
       uint64_t n_above = 0;
+      float* queue = s.queue[tid / 64];
       each(0, g.rounds, [&](int at, const float (&l)[EACH], int r) {
         uint64_t sum = 0;
+        uint32_t n = 0, used = 0;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-          const uint32_t key = route_key(l[i]);
-          const bool there = l[i] > -INFINITY;
-          listed(there && key >= low_of && key <= top_of, key, at + i);
-          if (there && key > top_of) {
-            sum += whole(l[i]);
-            ++n_above;
+          const uint32_t key = key_of(l[i]);
+          listed(key >= low_of && key <= top_of, key, at + i);
+          const bool above = key > top_of;
+          const unsigned long long who = __ballot(above);
+          if (above) queue[(n + __popcll(who & ((1ull << (tid % 64)) - 1))) % QUEUE] = l[i];
+          n += __popcll(who);
+          wave_lds();
+          if (n - used >= 64) {
+            sum += whole(queue[(used + tid % 64) % QUEUE]);
+            used += 64;
+            wave_lds();
           }
-          one_by_one();
         }
+        if (used + tid % 64 < n) sum += whole(queue[(used + tid % 64) % QUEUE]);
+        wave_lds();
+        if (tid % 64 == 0) n_above += n;
         sum = wave_total(sum);
         if (tid % 64 == 0) s.part[r * WAVES + tid / 64] = sum;
         return true;
@@ -487,51 +517,49 @@ template <int TYPE> __device__ __forceinline__ Row<TYPE> row_of(const Args& g, S
                    w.greedy ? 0.0 : 369.3299304675746 / (double)w.t};
 }
 
-// A chunk of PER rounds: its maximum, number of tokens, sum, and the maxima of its runs
-template <int TYPE, int PER> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, const Wishes& w, int chunk) {
+// A chunk of g.per rounds: its maximum, number of tokens, sum, and the maxima of its runs.  A wave goes on by itself, with a maximum of its own
+// to which it brings its sum; the waves are joined at the end.
+template <int TYPE> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, const Wishes& w, int chunk) {
   const Args& g = R.g;
   Shared& s = R.s;
-  const int tid = threadIdx.x, lane = tid % 64, r0 = chunk * PER;
-  typename Row<TYPE>::Raw raw[PER];
-#pragma unroll
-  for (int j = 0; j < PER; ++j) raw[j] = R.fetch((r0 + j) * ROUND + tid * EACH);
-  float top = -INFINITY;
+  const int tid = threadIdx.x, lane = tid % 64, r0 = chunk * g.per, r1 = min(r0 + g.per, g.rounds);
   uint32_t n = 0;
+  double sum = 0.0;
+  R.top = -INFINITY;
   if (tid == 0) s.counter = 0;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    float l[EACH], most = -INFINITY;
-    R.widen(raw[j], l);
+  __syncthreads();  // (and the table is there)
+  R.each(r0, r1, [&](int, const float (&l)[EACH], int r) {
+    float most = l[0];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       most = fmaxf(most, l[i]);
       n += __popcll(__ballot(l[i] > -INFINITY));
     }
-    top = fmaxf(top, most);
-    if (w.k > 0 && r0 + j < g.rounds) {
-      most = fmaxf(most, __shfl_xor(most, 1));
-      most = fmaxf(most, __shfl_xor(most, 2));
-      if (lane % 4 == 0) put(g.runs + ((int64_t)R.row * g.rounds + r0 + j) * RUNS + tid / 4, most);
+    if (w.k > 0) {
+      float run = fmaxf(most, __shfl_xor(most, 1));
+      run = fmaxf(run, __shfl_xor(run, 2));
+      if (lane % 4 == 0) put(g.runs + ((int64_t)R.row * g.rounds + r) * RUNS + tid / 4, run);
     }
-  }
-  top = block_max(top, s);
-  double sum = 0.0;
-  if (w.summed) {
-    R.top = top;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      float l[EACH];
-      R.widen(raw[j], l);
+    most = value_of(wave_max(key_of(most)));
+    if (most > R.top) {
+      const float before = R.top;
+      R.top = most;
+      if (w.summed && sum > 0.0) sum *= R.weight(before, 0);
+    }
+    if (w.summed && R.top > -INFINITY) {
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { sum += R.weight(l[i], 0); one_by_one(); }
     }
-    sum = block_sum(sum, s);
-  }
+    return true;
+  });
+  const float mine = R.top;
+  R.top = block_max(mine, s);
+  if (w.summed) sum = block_sum(mine > -INFINITY ? sum * R.weight(mine, 0) : 0.0, s);
   if (lane == 0) atomicAdd(&s.counter, n);
   __syncthreads();
   if (tid == 0) {
     const int64_t at = (int64_t)R.row * g.chunks + chunk;
-    put(g.top + at, top);
+    put(g.top + at, R.top);
     put(g.n + at, s.counter);
     put(g.sum + at, sum);
   }
@@ -543,7 +571,7 @@ template <int TYPE> __global__ __launch_bounds__(THREADS, 8) void k_sample_sums(
   const int row = blockIdx.x / g.chunks;
   const Wishes w(g.a, row);
   Row<TYPE> R = row_of<TYPE>(g, s, row, w);
-  sums_of_chunk<TYPE, WIDE>(R, w, blockIdx.x % g.chunks);
+  sums_of_chunk<TYPE>(R, w, blockIdx.x % g.chunks);
 }
 
 // ALONE: the chunks too, and the block of a row that finishes last goes on; else a block a row
@@ -554,7 +582,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   const Wishes w(a, row);
   Row<TYPE> R = row_of<TYPE>(g, s, row, w);
   if constexpr (ALONE) {
-    sums_of_chunk<TYPE, 1>(R, w, blockIdx.x % g.chunks);
+    sums_of_chunk<TYPE>(R, w, blockIdx.x % g.chunks);
     // all of this block's values have reached memory before it is counted
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -578,12 +606,12 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   const uint64_t n_all = scan(tid < g.chunks ? get(g.n + first + tid) : 0u, before, s.wave_a);
   if (n_all == 0) { R.write(-1, 0.0, 0); return; }
   R.top = top;
-  const uint32_t top_key = route_key(top);
+  const uint32_t top_key = key_of(top);
   const float u = a.u[row];
   const double one = ldexp(1.0, g.shift);
   // How the row is gone through in the end, and with which target
   int r0 = 0, r1 = g.rounds, what = R.WEIGHT;
-  typename Row<TYPE>::Left left{route_key(-3.402823466e38f), 0xffffffffu, by_m ? least : 0.0};
+  typename Row<TYPE>::Left left{LOWEST_KEY, 0xffffffffu, by_m ? least : 0.0};
   double sum = 0.0, rest = 0.0;
   int kept = (int)n_all;
   uint64_t w_all = 0;
@@ -646,7 +674,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
         for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
         __syncthreads();
         for (int i = tid; i < runs; i += THREADS) {
-          const uint32_t key = route_key(get(g.runs + (int64_t)row * runs + i));
+          const uint32_t key = key_of(get(g.runs + (int64_t)row * runs + i));
           if (level == 0) atomicAdd(reinterpret_cast<uint32_t*>(&s.hist[2047 - (key >> 21)]), 1u);
           else if ((key >> 21) == (lo >> 21)) atomicAdd(reinterpret_cast<uint32_t*>(&s.hist[2047 - ((key >> 10) & 2047)]), 1u);
         }
@@ -672,7 +700,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   // (with both top_k and top_p the sum of all k is needed, those below min_p too)
   if (by_m && !(k > 0 && by_p) && top < INFINITY) bound = fmaxf(bound, a_little_below((double)top + log(least) * (double)t));
   bound = fminf(bound, top);
-  const uint32_t bound_key = route_key(bound);
+  const uint32_t bound_key = max(key_of(bound + 0.f), LOWEST_KEY);
 
   // Few: in order, all at once
   const int few = k > LIST ? LIST + 1 : R.collect(bound_key);
