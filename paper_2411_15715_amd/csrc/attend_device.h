@@ -32,17 +32,27 @@ constexpr int ATTEND_COUNTERS = 16384;  // sequences times units (kv head, row g
 constexpr int64_t ATTEND_BLOCKS = 1 << 24;  // of a launch (it has fewer than 2^32 threads)
 constexpr int attend_wide_dim(int type) { return type == SI_KV_E4M3 ? 64 : 128; }  // longest heads of which a wave may have 32 rows
 
-// What a launch goes by: ALL of each sequence, or PIECES (attend_shared.hip): up to block_rows rows with the positions that they attend to in it
+// What blocks go by: ALL of each sequence, or PIECES (attend_shared.hip): up to block_rows rows of one, with the positions that they attend to
 enum { ATTEND_ALL, ATTEND_PIECES };
 
-// Of several sequences and the pages that these share, or of one and its own tokens
 struct Piece {
   int seq;                     // whose row of the table is read
   int first, rows;             // rows (entry of the list * n_new + token) * heads per kv head + head, of a kv head
   int lo, hi, lo_all, hi_all;  // positions seen by some of the rows, and by all
   int fb, nb;                  // first block and number of them
-  int own;                     // -1: shared, all rows see them but for a window; else the entry of the list
-  int sight;                   // own: where the sight of the entry's first new token ends
+  int entry, sight;            // of the list; where the sight of its first new token ends (both not of shared pieces)
+};
+// Pieces whose blocks, one after the other (a piece of none counts as one), are cut into equal slices.  The plan says where each begins.
+struct SliceStart {
+  int piece, off, left;   // first piece, its first block from the piece's first, blocks of the slice
+};
+struct PieceList {
+  int slices;
+  const Piece* pieces;
+  const SliceStart* starts;  // [slices]
+  const int2* parted;        // [pieces] first slice of a piece and number of them
+  float* part;               // sums of unfinished ones, as in AttendArgs, rows of `stride` floats
+  int part_rows, stride;
 };
 
 struct AttendArgs {
@@ -60,13 +70,11 @@ struct AttendArgs {
   uint32_t* count;  // [ATTEND_COUNTERS], of (sequence, unit); 0 between calls
   int2* parted;     // [n][unit] first slice of a sequence and number of them
   float* part;      // [unit][slice][2][part_rows][D + 2]: o, then m, l of each row; first the sum of a sequence that began before the slice
-  // pieces: their number, they, their blocks one after the other (a piece of none counts as one), and where the sums of those that one block has all of
-  // go: [shared, own][kv head][n * n_new * heads per kv head][D + 4], o, then m, l
-  const int32_t* n_pieces;
-  const Piece* pieces;
-  const int64_t* begins;  // [n_pieces + 1]
+  // pieces: of sequences that share positions (attend_wide.h), and of each sequence's own; where the sums of those that one block has all of go:
+  // [shared, own][kv head][n * n_new * heads per kv head][D + 4], o, then m, l
+  PieceList shared, own;
   float* sums;
-  const int2* group;      // [n] first piece of an entry's group (-1: none), first entry of it
+  const int2* group;      // [n] first shared piece of an entry's group (-1: none), first entry of it
   int chunks;             // pieces of an entry's own tokens
 };
 
@@ -159,7 +167,7 @@ struct Span {
   int lo, hi, lo_all, hi_all;   // seen by some of them: [lo, hi), by all of them [lo_all, hi_all)
   int fb, nb;                   // first block and number of them
   int why;
-  int own;                      // of a piece
+  int entry;                    // of a piece
   __device__ __forceinline__ Span(const AttendArgs& g, const Piece& p) {
     seq = p.seq;
     window = g.a.window;
@@ -167,7 +175,7 @@ struct Span {
     first = p.sight;
     lo = p.lo; hi = p.hi; lo_all = p.lo_all; hi_all = p.hi_all;
     fb = p.fb; nb = p.nb;
-    own = p.own;
+    entry = p.entry;
   }
   __device__ __forceinline__ Span(const AttendArgs& g, int seq_i, int t0, int t1, int B) {
     const si_cache_t& c = g.c;
@@ -186,7 +194,7 @@ struct Span {
     hi_all = max(0, first + t0);
     lo = window ? max(0, first + t0 - window) : 0;
     lo_all = window ? max(0, first + t1 - window) : 0;
-    own = 0;
+    entry = 0;
     fb = lo / B;
     nb = hi > lo ? (hi + B - 1) / B - fb : 0;
   }
@@ -204,9 +212,13 @@ struct Sum {
   }
 };
 
-__device__ __forceinline__ Piece piece_of(const AttendArgs& g, int i) {
-  const constant_t* p = (const constant_t*)(uintptr_t)(g.pieces + i);
+__device__ __forceinline__ Piece piece_of(const PieceList& l, int i) {
+  const constant_t* p = (const constant_t*)(uintptr_t)(l.pieces + i);
   return Piece{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10]};
+}
+__device__ __forceinline__ SliceStart slice_start(const PieceList& l, int slice) {
+  const constant_t* p = (const constant_t*)(uintptr_t)(l.starts + slice);
+  return SliceStart{p[0], p[1], p[2]};
 }
 // the sums of a row of a kv head over shared positions, over its own
 __device__ __forceinline__ float* piece_sum(const AttendArgs& g, bool own, int kv, int64_t row) {
@@ -360,26 +372,33 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     return total;
   }
 
+  // (of PIECES the first blocks have shared ones: attend_wide.h)
+  static __device__ __forceinline__ int slice_of_block(const AttendArgs& g) { return (int)blockIdx.y - (MODE == ATTEND_PIECES ? g.shared.slices : 0); }
+  static __device__ __forceinline__ void run_own_pieces(const AttendArgs& g, Shared& s) {
+    if (RING && threadIdx.x == 0) s.again = 0;
+    const SliceStart start = slice_start(g.own, slice_of_block(g));
+    for (int i = start.piece, off = start.off, left = start.left; left > 0; ++i) {
+      const Piece p = piece_of(g.own, i);
+      const int nb = max(1, p.nb), take = min(nb - off, left);
+      part(g, s, Span(g, p), i, 0, p.rows, p.fb + off, p.nb > 0 ? p.fb + off + take : p.fb, take == nb ? -1 : off > 0 ? 0 : 1);
+      off = 0;
+      left -= take;
+    }
+  }
+
   static __device__ void run(const AttendArgs& g, Shared& s) {
     const int block_row0 = unit_of(g).group * BLOCK_ROWS;
-    int row_end = min(g.rows, block_row0 + BLOCK_ROWS);  // (PIECES: each piece's own)
+    const int row_end = min(g.rows, block_row0 + BLOCK_ROWS);
     if (RING && threadIdx.x == 0) s.again = 0;
-    const int n = MODE == ATTEND_PIECES ? *(constant_t*)(uintptr_t)g.n_pieces : g.a.n;
-    const int slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
-    auto span_of = [&](int k) {
-      if constexpr (MODE == ATTEND_PIECES) return Span(g, piece_of(g, k));
-      else return Span(g, k, t0, t1, B);
-    };
+    const int n = g.a.n, slice = blockIdx.y, per = g.a.n_heads / g.c.n_kv_heads, t0 = block_row0 / per, t1 = (row_end - 1) / per;
     // The slice: blocks [begin, begin + left) from the first of sequence `i` on.  A sequence of no blocks counts as one, so that somebody
     // writes its rows.
-    auto blocks_of = [&](int k) { return (int64_t)max(1, span_of(k).nb); };
+    auto blocks_of = [&](int k) { return (int64_t)max(1, Span(g, k, t0, t1, B).nb); };
     const int mine = (n + THREADS - 1) / THREADS, k0 = min(n, (int)threadIdx.x * mine), k1 = min(n, k0 + mine);  // sequences that a thread counts
     int64_t total, before = 0, counted = 0;
     int i = g.whole ? slice : 0;
-    Span sp = span_of(i);
-    if constexpr (MODE == ATTEND_PIECES) {
-      total = g.begins[n];
-    } else if (n == 1 || g.whole) {
+    Span sp(g, i, t0, t1, B);
+    if (n == 1 || g.whole) {
       total = max(1, sp.nb);
     } else {
       for (int k = k0; k < k1; ++k) counted += blocks_of(k);
@@ -395,13 +414,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       begin = slice_end(slice - 1);
       left = slice < G ? slice_end(slice) - begin : 0;
     }
-    if constexpr (MODE == ATTEND_PIECES) {
-      for (int k = threadIdx.x; k < n; k += THREADS)
-        if (g.begins[k] <= begin && begin < g.begins[k + 1]) { s.first = k; s.begin = begin - g.begins[k]; }
-      __syncthreads();
-      i = __builtin_amdgcn_readfirstlane(s.first);
-      begin = __builtin_amdgcn_readfirstlane((int)s.begin);
-    } else if (n > 1 && !g.whole) {
+    if (n > 1 && !g.whole) {
       if (before <= begin && begin < before + counted)
         for (int k = k0; k < k1; ++k) {
           const int64_t nb = blocks_of(k);
@@ -415,12 +428,11 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     // unfinished sums of the slice, at its begin and at its end: sequence (-1: none), its first slice and their number
     int un_seq[2] = {-1, -1}, un_first[2] = {0, 0}, un_parts[2] = {1, 1};
     for (; left > 0; ++i) {
-      if (MODE == ATTEND_PIECES || (n > 1 && !g.whole)) sp = span_of(i);
-      if constexpr (MODE == ATTEND_PIECES) row_end = piece_of(g, i).rows;
+      if (n > 1 && !g.whole) sp = Span(g, i, t0, t1, B);
       const int nb = max(1, sp.nb), off = (int)begin, take = (int)min<int64_t>(nb - off, left), where_to = take == nb ? -1 : off > 0 ? 0 : 1;
       if (sp.why && off == 0 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(g.c.status, sp.why);
       part(g, s, sp, i, block_row0, row_end, sp.fb + off, sp.nb > 0 ? sp.fb + off + take : sp.fb, where_to);
-      if (MODE == ATTEND_PIECES || (g.slices > 1 && !g.whole)) {
+      if (g.slices > 1 && !g.whole) {
         const int64_t first_block = slice_end(slice) - left - off;
         const int first = where_to < 0 ? slice : slice_of(first_block), parts = where_to < 0 ? 1 : slice_of(first_block + nb - 1) - first + 1;
         if (where_to == 0) { un_seq[0] = i; un_first[0] = first; un_parts[0] = parts; }
@@ -459,23 +471,12 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     const int window = sp.window, first = sp.first, lo = sp.lo, hi = sp.hi, lo_all = sp.lo_all, hi_all = sp.hi_all;
 
     // this lane's rows of q, as right operands; token of a row (PIECES: of all tokens of the call), or -1
-    const int row_base = MODE == ATTEND_PIECES ? piece_of(g, seq_i).first : 0;
+    const int row_base = MODE == ATTEND_PIECES ? piece_of(g.own, seq_i).first : 0;
     auto token_of = [&](int row) { return (row_base + row) / per; };
-    // what a token sees
-    auto sees_to = [&](int t) {
-      if constexpr (MODE == ATTEND_PIECES) return sp.own < 0 ? hi : max(0, first + t - sp.own * n_new);
-      else return max(0, first + t);
-    };
-    auto sees_from = [&](int t) {
-      if constexpr (MODE == ATTEND_PIECES) {
-        if (!window) return 0;
-        if (sp.own >= 0) return max(0, first + t - sp.own * n_new - window);
-        const int e = t / n_new, s = g.a.seqs ? g.a.seqs[e] : e;  // (members of a group have a place in the table)
-        return max(0, c.lens[s] - n_new + 1 + t % n_new - window);
-      } else {
-        return window ? max(0, first + t - window) : 0;
-      }
-    };
+    // what a token sees (PIECES: of all of the call)
+    const int token0 = MODE == ATTEND_PIECES ? sp.entry * n_new : 0;
+    auto sees_to = [&](int t) { return max(0, first + t - token0); };
+    auto sees_from = [&](int t) { return window ? max(0, first + t - token0 - window) : 0; };
     int tok[NT];
     u32x4 q[NT][D / 32];
 #pragma unroll
@@ -587,9 +588,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       for (int u = 0; u < NT; ++u) {
         float top = -INFINITY;
         const int see_hi = tok[u] >= 0 ? sees_to(tok[u]) : 0;
-        int see_lo = 0;
-        if constexpr (MODE == ATTEND_PIECES) see_lo = EDGE && tok[u] >= 0 ? sees_from(tok[u]) : 0;
-        else see_lo = window ? max(0, first + tok[u] - window) : 0;
+        const int see_lo = sees_from(tok[u]);
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -826,7 +825,8 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
     }
     __syncthreads();
     const int items = (row_end - block_row0) * (D / 4);
-    float* sums = g.part + (((int64_t)blockIdx.x * g.slices + blockIdx.y) * 2 + max(where_to, 0)) * (g.part_rows * (D + 2));
+    float* sums = MODE == ATTEND_PIECES ? g.own.part + (((int64_t)blockIdx.x * g.own.slices + slice_of_block(g)) * 2 + max(where_to, 0)) * (g.own.part_rows * (D + 2))
+                                        : g.part + (((int64_t)blockIdx.x * g.slices + blockIdx.y) * 2 + max(where_to, 0)) * (g.part_rows * (D + 2));
     for (int i = threadIdx.x; i < items; i += THREADS) {
       const int r = i / (D / 4), dim = i % (D / 4) * 4;
       Sum sum;
@@ -834,7 +834,7 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
       float* to = sums + r * (D + 2);
       if (where_to < 0) {
         if constexpr (MODE == ATTEND_PIECES) {
-          float* out = piece_sum(g, sp.own >= 0, kv, row_base + r);
+          float* out = piece_sum(g, true, kv, row_base + r);
           *reinterpret_cast<f32x4*>(out + dim) = sum.o;
           if (dim == 0) *reinterpret_cast<float2*>(out + D) = make_float2(sum.m, sum.l);
         } else {
@@ -879,10 +879,10 @@ template <int TYPE, int D, int NT, int TILES, int MODE = ATTEND_ALL> struct Atte
   }
 };
 
-template <int TYPE, int D, int NT, int TILES, int MODE>
+template <int TYPE, int D, int NT, int TILES>
 __global__ __launch_bounds__((Attend<TYPE, D, NT, TILES>::THREADS), (Attend<TYPE, D, NT, TILES>::WAVES_PER_SIMD)) void k_attend(AttendArgs g) {
-  __shared__ typename Attend<TYPE, D, NT, TILES, MODE>::Shared s;
-  Attend<TYPE, D, NT, TILES, MODE>::run(g, s);
+  __shared__ typename Attend<TYPE, D, NT, TILES>::Shared s;
+  Attend<TYPE, D, NT, TILES>::run(g, s);
 }
 
 // Joins the parts of a sequence: a block has one row, and its threads a share of the parts of 4 elements each.
@@ -921,63 +921,16 @@ template <int D> __global__ __launch_bounds__(256) void k_join(AttendArgs g) {
   write_row(g, seq_i, kv, row, 4 * lane, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
 }
 
-// Joins what a row has over shared positions and over its own, each in parts or whole: D / 4 threads a row.
-template <int D> __global__ __launch_bounds__(256) void k_join_pieces(AttendArgs g) {
-  constexpr int LANES = D / 4, ROWS = 256 / LANES;
-  const int per = g.a.n_heads / g.c.n_kv_heads, of_entry = g.a.n_new * per, all = g.a.n * of_entry;
-  const int kv = blockIdx.x, row = blockIdx.y * ROWS + threadIdx.x / LANES, dim = threadIdx.x % LANES * 4;
-  if (threadIdx.x / LANES >= ROWS || row >= all) return;
-  const int entry = row / of_entry, n_own = g.a.n * g.chunks, n_shared = *g.n_pieces - n_own;
-  const int2 group = g.group[entry];
-  Sum sum;
-  auto add = [&](int piece, int at, bool own) {  // row `at` of the piece
-    const int2 parted = g.parted[(int64_t)piece * g.c.n_kv_heads + kv];
-    if (parted.y == 1) {
-      const float* from = piece_sum(g, own, kv, row);
-      const float2 ml = *reinterpret_cast<const float2*>(from + D);
-      sum.add(*reinterpret_cast<const f32x4*>(from + dim), ml.x, ml.y);
-      return;
-    }
-    const int part_floats = g.part_rows * (D + 2);
-    const float* from = g.part + ((int64_t)kv * g.slices + parted.x) * 2 * part_floats + at * (D + 2);
-    constexpr int AHEAD = 8;
-    for (int p0 = 0; p0 < parted.y; p0 += AHEAD) {
-      float2 v[AHEAD][3];
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int q = min(p0 + k, parted.y - 1);  // (all but the first hold the piece from before)
-        const float* p = from + (int64_t)(2 * q + (q == 0 ? 1 : 0)) * part_floats;
-        v[k][0] = *reinterpret_cast<const float2*>(p + dim);
-        v[k][1] = *reinterpret_cast<const float2*>(p + dim + 2);
-        v[k][2] = *reinterpret_cast<const float2*>(p + D);
-      }
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k)
-        if (p0 + k < parted.y) sum.add(f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y}, v[k][2].x, v[k][2].y);
-    }
-  };
-  if (group.x >= 0) {
-    const int at = row - group.y * of_entry;
-    add(group.x + at / g.block_rows, at % g.block_rows, false);
-  }
-  const int at = row - entry * of_entry;
-  add(n_shared + entry * g.chunks + at / g.block_rows, at % g.block_rows, true);
-  write_row(g, entry, kv, at, dim, sum, g.c.type == SI_KV_E4M3 && g.c.scale_v ? g.c.scale_v[kv] : 1.f);
-}
-
-template <int TYPE, int D, int MODE = ATTEND_ALL> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
+template <int TYPE, int D> hipError_t launch(const AttendArgs& g, hipStream_t stream) {
   // (heads first: blocks go to the dies in turn, and all heads of a slice have the same to do)
   const dim3 grid(g.c.n_kv_heads * g.groups, g.slices);
-  if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4, MODE>), grid, dim3(ATTEND_THREADS), 0, stream, g);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if constexpr (MODE == ATTEND_PIECES) {
-    const int rows = 256 / (D / 4);
-    hipLaunchKernelGGL(k_join_pieces<D>, dim3(grid.x, (unsigned)((g.a.n * g.a.n_new * (g.a.n_heads / g.c.n_kv_heads) + rows - 1) / rows)), dim3(256), 0, stream, g);
-  } else if (g.slices > 1 && !g.whole && !g.last_joins) {
+  if (g.block_rows == 16) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 1>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 32) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 2>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if (g.block_rows == 64) hipLaunchKernelGGL((k_attend<TYPE, D, 1, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  else if constexpr (D <= attend_wide_dim(TYPE)) hipLaunchKernelGGL((k_attend<TYPE, D, 2, 4>), grid, dim3(ATTEND_THREADS), 0, stream, g);
+  if (g.slices > 1 && !g.whole && !g.last_joins) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_join<D>, dim3(grid.x, g.a.n, g.part_rows), dim3(256), 0, stream, g);
   }
   return hipGetLastError();

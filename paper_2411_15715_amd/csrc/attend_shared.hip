@@ -16,18 +16,23 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 
+// Pieces as the plan writes them
+struct PlanList {
+  int slices;
+  Piece* pieces;
+  SliceStart* starts;
+  int2* parted;
+};
 struct PlanArgs {
   si_cache_t c;
   const int32_t* seqs;
-  int n, n_new, per, window, block_rows, chunks;
-  uint32_t* count;      // [1], 0 between calls
-  int32_t* common;      // [n] full pages that an entry of the list has in common with the one before
-  int32_t* tokens_of;   // [n] of a group's first entry: tokens in its shared pages
-  int32_t* piece_of;    // [n] of a group's first entry: its first piece, or -1
-  int32_t* n_pieces;
-  Piece* pieces;        // the groups', then those of each entry's own tokens
-  int64_t* begins;      // [n_pieces + 1]
-  int2* group;          // [n] first piece of an entry's group (-1: none), first entry of it
+  int n, n_new, per, window, wide_rows, block_rows, chunks;
+  uint32_t* count;       // [1], 0 between calls
+  int32_t* common;       // [n] full pages that an entry of the list has in common with the one before
+  int32_t* tokens_of;    // [n] of a group's first entry: tokens in its shared pages
+  int32_t* piece_of;     // [n] of a group's first entry: its first piece, or -1
+  PlanList shared, own;  // the groups' pieces, of up to wide_rows rows, and those of each entry's own tokens
+  int2* group;           // [n] first piece of an entry's group (-1: none), first entry of it
 };
 
 __device__ __forceinline__ int seq_at(const PlanArgs& g, int e) { return g.seqs ? g.seqs[e] : e; }
@@ -122,7 +127,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
     for (int w = 0; w < WAVES; ++w) next = s_begins[w] ? s_run[w] : joined(next, s_run[w]);
     // (beyond the last entry a run is empty and changes nothing)
     const int members = i - r.first + 1, tokens = ends && members > 1 ? r.pages * g.c.page_tokens : 0, rows = members * g.n_new * g.per;
-    const int mine = tokens > 0 ? (rows + g.block_rows - 1) / g.block_rows : 0;
+    const int mine = tokens > 0 ? (rows + g.wide_rows - 1) / g.wide_rows : 0;
     int at = mine;
     for (int d = 1; d < 64; d *= 2) {
       const int o = __shfl_up(at, d);
@@ -141,7 +146,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
       g.piece_of[r.first] = mine > 0 ? at : -1;
       const int lo = g.window ? min(tokens, max(0, r.shortest - g.n_new + 1 - g.window)) : 0, lo_all = g.window ? min(tokens, max(0, r.longest - g.window)) : 0;
       for (int k = 0; k < mine; ++k)
-        g.pieces[at + k] = Piece{seq_at(g, r.first), r.first * g.n_new * g.per + k * g.block_rows, min(g.block_rows, rows - k * g.block_rows), lo, tokens, lo_all, tokens,
+        g.shared.pieces[at + k] = Piece{seq_at(g, r.first), r.first * g.n_new * g.per + k * g.wide_rows, min(g.wide_rows, rows - k * g.wide_rows), lo, tokens, lo_all, tokens,
                                  lo / B, tokens > lo ? tokens / B - lo / B : 0, -1, 0};
     }
     carry = next;
@@ -152,42 +157,59 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
     const int i = k / g.chunks, row0 = (k - i * g.chunks) * g.block_rows, rows = min(g.block_rows, of_entry - row0), first = g.group[i].y, from = g.tokens_of[first];
     const int sight = len_at(g, i) - g.n_new + 1, t0 = row0 / g.per, t1 = (row0 + rows - 1) / g.per;
     const int hi = max(0, sight + t1), lo = g.window ? max(from, sight + t0 - g.window) : from;
-    g.pieces[n_shared + k] = Piece{seq_at(g, i), i * of_entry + row0, rows, lo, hi, g.window ? max(from, sight + t1 - g.window) : from, max(0, sight + t0),
-                                   lo / B, hi > lo ? (hi + B - 1) / B - lo / B : 0, i, sight};
+    g.own.pieces[k] = Piece{seq_at(g, i), i * of_entry + row0, rows, lo, hi, g.window ? max(from, sight + t1 - g.window) : from, max(0, sight + t0),
+                     lo / B, hi > lo ? (hi + B - 1) / B - lo / B : 0, i, sight};
     if (row0 == 0) g.group[i].x = g.piece_of[first];
   }
   __syncthreads();
-  const int n_pieces = n_shared + n_own;
-  int64_t done = 0;
-  for (int k0 = 0; k0 < n_pieces; k0 += THREADS) {
-    const int k = k0 + tid;
-    const int64_t mine = k < n_pieces ? max(1, g.pieces[k].nb) : 0;
-    int64_t x = mine;
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t o = __shfl_up(x, d);
-      if (lane >= d) x += o;
-    }
-    __syncthreads();
-    if (lane == 63) s_sum[wave] = x;
-    __syncthreads();
-    x += done - mine;
-    for (int w = 0; w < WAVES; ++w) {
-      if (w < wave) x += s_sum[w];
-      done += s_sum[w];
-    }
-    if (k < n_pieces) g.begins[k] = x;
-  }
-  if (tid == 0) {
-    g.begins[n_pieces] = done;
-    *g.n_pieces = n_pieces;
-  }
+  // Equal slices of each list's blocks: slice w is [end(w - 1), end(w)) with end(w) = (w + 1) total / G.  (Quotients by way of double: exact, as the dividends
+  // stay below 2^53.)
+  auto cut = [&](const PlanList& list, int n) {
+    auto scan = [&](auto f) {  // f(piece, its blocks, blocks before it) for all; returns the number of blocks
+      int64_t done = 0;
+      for (int k0 = 0; k0 < n; k0 += THREADS) {
+        const int k = k0 + tid;
+        const int64_t mine = k < n ? max(1, list.pieces[k].nb) : 0;
+        int64_t x = mine;
+        for (int d = 1; d < 64; d *= 2) {
+          const int64_t o = __shfl_up(x, d);
+          if (lane >= d) x += o;
+        }
+        __syncthreads();
+        if (lane == 63) s_sum[wave] = x;
+        __syncthreads();
+        x += done - mine;
+        for (int w = 0; w < WAVES; ++w) {
+          if (w < wave) x += s_sum[w];
+          done += s_sum[w];
+        }
+        if (k < n) f(k, mine, x);
+      }
+      return done;
+    };
+    const int64_t total = scan([](int, int64_t, int64_t) {}), G = min<int64_t>(list.slices, total);
+    auto quotient = [](int64_t x, int64_t y) { return (int64_t)((double)x / (double)y); };
+    auto end = [&](int64_t w) { return quotient((w + 1) * total, G); };
+    auto slice_of = [&](int64_t block) { return (int)quotient((block + 1) * G - 1, total); };  // the one whose end is the first beyond the block
+    scan([&](int k, int64_t mine, int64_t x) {
+      const int first = slice_of(x), last = slice_of(x + mine - 1);
+      list.parted[k] = make_int2(first, last - first + 1);
+      for (int w = first; w <= last; ++w)  // those that begin in this piece
+        if (end(w - 1) >= x) list.starts[w] = SliceStart{k, (int)(end(w - 1) - x), (int)(end(w) - end(w - 1))};
+    });
+    for (int w = (int)G + tid; w < list.slices; w += THREADS) list.starts[w] = SliceStart{0, 0, 0};
+  };
+  cut(g.shared, n_shared);
+  cut(g.own, n_own);
 }
+
+constexpr int WIDE = 128;  // rows of a shared piece
 
 struct Layout {
   AttendCut alone;           // of si_attend
   bool pieces;               // else the call is si_attend
-  int block_rows, chunks, slices;
-  int64_t parted, part, sums, n_pieces, list, begins, group, common, tokens_of, piece_of, bytes;
+  int block_rows, chunks, shared_slices, own_slices;
+  int64_t shared_parted, own_parted, shared_part, own_part, sums, shared, own, shared_starts, own_starts, group, common, tokens_of, piece_of, bytes;
 };
 
 Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
@@ -196,23 +218,27 @@ Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
   const int of_entry = a.n_new * (a.n_heads / c.n_kv_heads);
   const int64_t rows = (int64_t)a.n * of_entry;
   l.pieces = a.n > 1 && rows <= 200000;  // (the joining launch has a block for 4 rows and more)
-  const int wide = c.head_dim <= attend_wide_dim(c.type) ? 128 : 64;
-  for (l.block_rows = 16; l.block_rows < rows && l.block_rows < wide;) l.block_rows *= 2;
+  for (l.block_rows = 16; l.block_rows < of_entry && l.block_rows < 64;) l.block_rows *= 2;
   l.chunks = (of_entry + l.block_rows - 1) / l.block_rows;
-  l.slices = std::max(1, (c.head_dim <= 128 ? 512 : 256) / c.n_kv_heads);
-  const int64_t most = rows / 16 + a.n / 2 + 1 + (int64_t)a.n * ((of_entry + 15) / 16);
+  const int64_t each = (a.max_len + kv_block(c.type) - 1) / kv_block(c.type), turns = (rows + WIDE - 1) / WIDE * each * c.n_kv_heads / 256;
+  l.shared_slices = std::max(1, (turns > 24 && c.head_dim < 192 ? 512 : 256) / c.n_kv_heads);
+  l.own_slices = std::max(1, 256 / c.n_kv_heads);
+  const int64_t shared = rows / WIDE + a.n / 2 + 1, own = (int64_t)a.n * l.chunks;
   int64_t at = std::max<int64_t>(l.alone.scratch, ATTEND_COUNTERS * 4);  // (the counters are at the same place in every call's scratch)
   auto take = [&](int64_t bytes) {
     const int64_t q = (at + 15) / 16 * 16;
     at = q + bytes;
     return q;
   };
-  l.parted = take(most * c.n_kv_heads * 8);
-  l.part = take((int64_t)c.n_kv_heads * l.slices * 2 * l.block_rows * (c.head_dim + 2) * 4);
+  l.shared_parted = take(shared * 8);
+  l.own_parted = take(own * 8);
+  l.shared_part = take((int64_t)c.n_kv_heads * l.shared_slices * 2 * WIDE * (c.head_dim + 4) * 4);
+  l.own_part = take((int64_t)c.n_kv_heads * l.own_slices * 2 * std::min(of_entry, l.block_rows) * (c.head_dim + 2) * 4);
   l.sums = take(2 * c.n_kv_heads * rows * (c.head_dim + 4) * 4);
-  l.n_pieces = take(4);
-  l.list = take(most * (int64_t)sizeof(Piece));
-  l.begins = take((most + 1) * 8);
+  l.shared = take(shared * (int64_t)sizeof(Piece));
+  l.own = take(own * (int64_t)sizeof(Piece));
+  l.shared_starts = take(l.shared_slices * (int64_t)sizeof(SliceStart));
+  l.own_starts = take(l.own_slices * (int64_t)sizeof(SliceStart));
   l.group = take(a.n * 8ll);
   l.common = take(a.n * 4ll);
   l.tokens_of = take(a.n * 4ll);
@@ -252,22 +278,20 @@ extern "C" int si_attend_shared(const si_cache_t* c, int32_t layer, const si_att
   if (!l.pieces) {
     e = (c->type == SI_KV_BF16 ? launch_attend_bf16 : launch_attend_e4m3)(g, (hipStream_t)stream);
   } else {
-    g.rows = g.block_rows = g.part_rows = l.block_rows;
+    const auto ints = [&](int64_t at) { return reinterpret_cast<int32_t*>(p + at); };
+    const int part_rows = std::min(a->n_new * (a->n_heads / c->n_kv_heads), l.block_rows);
+    const PlanList shared{l.shared_slices, reinterpret_cast<Piece*>(p + l.shared), reinterpret_cast<SliceStart*>(p + l.shared_starts), reinterpret_cast<int2*>(p + l.shared_parted)};
+    const PlanList mine{l.own_slices, reinterpret_cast<Piece*>(p + l.own), reinterpret_cast<SliceStart*>(p + l.own_starts), reinterpret_cast<int2*>(p + l.own_parted)};
+    const PlanArgs plan{*c, a->seqs, a->n, a->n_new, a->n_heads / c->n_kv_heads, a->window, WIDE, l.block_rows, l.chunks, reinterpret_cast<uint32_t*>(p), ints(l.common),
+                        ints(l.tokens_of), ints(l.piece_of), shared, mine, reinterpret_cast<int2*>(p + l.group)};
+    g.rows = g.block_rows = l.block_rows;
     g.groups = 1;
-    g.slices = l.slices;
     g.whole = g.last_joins = 0;
-    g.parted = reinterpret_cast<int2*>(p + l.parted);
-    g.part = reinterpret_cast<float*>(p + l.part);
+    g.shared = PieceList{l.shared_slices, shared.pieces, shared.starts, shared.parted, reinterpret_cast<float*>(p + l.shared_part), WIDE, c->head_dim + 4};
+    g.own = PieceList{l.own_slices, mine.pieces, mine.starts, mine.parted, reinterpret_cast<float*>(p + l.own_part), part_rows, c->head_dim + 2};
     g.sums = reinterpret_cast<float*>(p + l.sums);
-    g.chunks = l.chunks;
-    const PlanArgs plan{*c, a->seqs, a->n, a->n_new, a->n_heads / c->n_kv_heads, a->window, l.block_rows, l.chunks, reinterpret_cast<uint32_t*>(p),
-                        reinterpret_cast<int32_t*>(p + l.common), reinterpret_cast<int32_t*>(p + l.tokens_of), reinterpret_cast<int32_t*>(p + l.piece_of),
-                        reinterpret_cast<int32_t*>(p + l.n_pieces), reinterpret_cast<Piece*>(p + l.list), reinterpret_cast<int64_t*>(p + l.begins),
-                        reinterpret_cast<int2*>(p + l.group)};
-    g.n_pieces = plan.n_pieces;
-    g.pieces = plan.pieces;
-    g.begins = plan.begins;
     g.group = plan.group;
+    g.chunks = l.chunks;
     hipLaunchKernelGGL(k_share, dim3(a->n), dim3(THREADS), 0, (hipStream_t)stream, plan);
     e = hipGetLastError();
     if (e == hipSuccess) e = (c->type == SI_KV_BF16 ? launch_attend_pieces_bf16 : launch_attend_pieces_e4m3)(g, (hipStream_t)stream);
