@@ -208,6 +208,8 @@ int64_t si_attend_scratch_bytes(const si_cache_t* cache, const si_attend_t* desc
  * them.  Which entries these are, and how many pages, is found on the device from the table, at every call: nothing has to be said, and a list
  * without shared pages is taken too (as si_attend, a little slower).  A group is a run of neighbours; it is cut where two of them have nothing in
  * common, or less than half of what one has in common with its other neighbour; all of a group read the pages that they all have in common.
+ * Calls that read less than 640 MB of keys and values by their max_len and window even if nothing is shared are si_attend's, to the bit: planning
+ * and joining would cost more than they save.
  * Results are those of si_attend but for the order of sums in fp32; they do not depend on the order in which blocks run, but on which
  * neighbours a sequence has in the list.
  * scratch: si_attend_shared_scratch_bytes, else as for si_attend, whose scratch it can be too (and, where it is large enough, the other way round).

@@ -347,7 +347,7 @@ template <int TYPE> struct Row {
         listed(key >= lo, key, at + i);
       }
       // (a wave may see a count of the round that others are in: it only goes on for nothing)
-      return *(volatile uint32_t*)&s.counter <= LIST;
+      return __hip_atomic_load(&s.counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= LIST;
     });
     __syncthreads();
     return (int)s.counter;

@@ -15,6 +15,11 @@ pytestmark = pytest.mark.gpu
 SCRATCH = {}
 
 
+@pytest.fixture(autouse=True)
+def small_calls_by_pieces_too(monkeypatch):
+    monkeypatch.setenv("SI_ATTEND_PIECES", "1")
+
+
 def scratch(n):
     """one piece of memory for all calls of this file: every call has to leave it fit for the next, whatever its shape"""
     if "t" not in SCRATCH or SCRATCH["t"].numel() < n:
@@ -137,6 +142,11 @@ def test_many_sequences():
     run_case(BF, [(128, [1 + i % 50 for i in range(700)])], 1, 2, 1, 64, 64, only=list(range(0, 700, 97)) + [255, 256, 511, 512, 699])
 
 
+def test_more_sequences_than_the_plan_notes_in_shared_memory():
+    groups = [(64 * (1 + i % 2), [1 + (i * j) % 70 for j in range(1 + i % 7)]) for i in range(240)] + [(64, [5] * 300)]
+    run_case(BF, groups, 1, 2, 1, 64, 64, only=list(range(0, 1200, 61)) + [255, 256, 767, 768, 1023, 1024])
+
+
 def test_the_same_sequence_several_times_and_prompts_within_prompts():
     run_case(BF, [(300, [5, 9]), (100, [3])], 2, 4, 2, 64, 64, seqs=[0, 0, 1, 1, 1, 2, 2, 0])
     # two long prompts that begin alike, forked: cut between them
@@ -242,6 +252,23 @@ def test_the_same_bits_every_time_and_one_scratch_with_si_attend():
         si.si_attend(c.desc, 0, desc, torch.cuda.current_stream().cuda_stream)
         again = call(c, q, lens, rows, 1, 16)
         assert np.array_equal(first[0], again[0]) and np.array_equal(first[1], again[1])
+
+
+def test_which_calls_are_si_attend(monkeypatch):
+    """small ones by max_len are, to the bit; larger ones plan their pieces, which the order of their sums tells"""
+    c, lens, rows = shared_cache(BF, [(900, [7, 300, 40, 5, 20])], 64, 2, 64)
+    q = torch.randn((5, 8 * 64), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).cuda()
+    pieces = call(c, q, lens, rows, 1, 8)
+    monkeypatch.delenv("SI_ATTEND_PIECES")
+    small, large = call(c, q, lens, rows, 1, 8), call(c, q, lens, rows, 1, 8, max_len=1 << 20)
+    alone = call_alone(c, q, lens, 1, 8, seqs=rows)
+    assert np.array_equal(small[0], alone[0]) and np.array_equal(small[1], alone[1])
+    assert not np.array_equal(pieces[1], alone[1]) and not np.array_equal(large[1], alone[1])
+    for out, lse in (small, large, pieces):
+        compare(c, q, lens, 1, 8, 0, 0, 0.0, rows, out, lse)
+    windowed = call(c, q, lens, rows, 1, 8, window=100, max_len=1 << 20)
+    alone = call_alone(c, q, lens, 1, 8, window=100, seqs=rows, max_len=1 << 20)
+    assert np.array_equal(windowed[0], alone[0]) and np.array_equal(windowed[1], alone[1])
 
 
 def test_a_recorded_call_follows_forks():
