@@ -1,11 +1,17 @@
-// The next token of a row of logits (scheinfer_sample.h has the formulas), in one launch.
+// The next token of a row of logits (scheinfer_sample.h has the formulas).
 //
 // A block takes a chunk of a row and leaves its maximum, where the row needs it the sum of e^((l - max) / T) in 64 bits, and for top_k the maxima of
-// runs of 32 elements; the block of a row that finishes last does the rest, from the caches.  What can be left is cut down before anything is put in
-// order: with n runs or more the top k lie at or above the k-th largest of the runs' maxima, and a token of less than (1 - top_p) S / vocab cannot be
-// needed for a share of top_p.  Few tokens beyond that bound are sorted in LDS.  Many are counted and summed in LDS by the leading bits of an
-// order-preserving key, the bin with the border again, until what it holds can be sorted.  Weights are integers (2^62 / vocab or more for the
-// largest), so that sums in any order are the same.
+// runs of 32 elements.  One block a row does the rest, from the caches.  What can be left is cut down before anything is put in order: with
+// n runs or more the top k lie at or above the k-th largest of the runs' maxima, a token of less than (1 - top_p) S / vocab cannot be needed for a share
+// of top_p, and min_p is a lowest logit.  Few tokens beyond that bound (2048) are sorted in LDS.  Of many, the border is looked for in bins (border()).
+// Weights are integers (2^62 / vocab or more for the largest), so that sums in any order are the same and a token never depends on scheduling.
+//
+// Chunks of up to 512 blocks and the rest are one launch, the block of a row that finishes last goes on; more chunks have a launch of their own with half the
+// registers, of 4 rounds each.  (One launch for all: 256 rows of 131072 in fp32 161 us, in two 118.)
+// Measured in the kernels: one row of 32000 bf16, top_k 50 and top_p 0.95, 20.7 us, nearly all of it one dependent step after another; 256 x 131072
+// fp32, top_p 0.9, 41 + 78 us, 134 MB once at 3.3 TB/s and then twice at 8 from the caches, bound by vector instructions: 25 for a weight in 64 bits, which
+// a token's border needs (an error of 1e-7 of the sum would move one draw in a hundred here), and 10 for a place in a bin; 61 rows of 100003 with
+// limits of their own 13 + 78 us, a compute unit a row.
 #include "si_internal.h"
 #include "si_error.h"
 #include "scheinfer_attention.h"
@@ -29,7 +35,7 @@ constexpr int MAX_ROUNDS = SI_SAMPLE_MAX_VOCAB / ROUND;
 constexpr int RUNS = THREADS / 4;          // of a round, 4 threads each
 constexpr int WIDE = 4;                    // rounds of a chunk where there are many
 constexpr int BINS = 2048, LIST = 2048;    // two a thread
-constexpr int QUEUE = 128;                 // of a wave
+constexpr int QUEUE = 64 * EACH;           // of a wave
 
 struct Args {
   si_sample_t a;
@@ -55,8 +61,8 @@ struct Shared {
   double pow2[256];                   // 2^(i / 256)
   double wave_d[WAVES];
   float wave_f[WAVES];
-  uint64_t found[4];
-  uint32_t counter, last;
+  uint64_t found[3];
+  uint32_t counter, seen, last;
 };
 
 // what other blocks read within the launch goes past the caches of this die
@@ -64,17 +70,21 @@ template <class T> __device__ __forceinline__ void put(T* p, T v) { __hip_atomic
 template <class T> __device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
-// order-preserving, of what widen() gives
+// order-preserving, of numbers
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t u = __float_as_uint(l);
+  const uint32_t u = __float_as_uint(l + 0.f);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite number: below it -infinity
+// of the largest that a token can have whose key is `key` or less: the key before 0 belongs to -0, which no token has
+__device__ __forceinline__ float value_to(uint32_t key) { return value_of(key == 0x7fffffffu ? key - 1 : key); }
+constexpr float LOWEST = -3.402823466e38f;    // the lowest finite number
+constexpr uint32_t LOWEST_KEY = 0x00800000u;  // its key: below it -infinity
 
 __device__ __forceinline__ float a_little_below(double v) {
   const float f = (float)v;
   return f - fabsf(f) * 1e-6f - 1e-30f;
 }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }  // (the same in all lanes)
 __device__ __forceinline__ uint64_t composite(uint32_t hi, uint32_t lo) { return (uint64_t)hi << 32 | lo; }
 
 // LDS of a wave: its accesses are in order, only the compiler has to keep it
@@ -108,10 +118,21 @@ __device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t& before, uint64_t 
   before += __shfl(x - own, wave);
   return __shfl(x, WAVES - 1);
 }
+// (in registers: by way of LDS a step waits some hundred cycles)
 __device__ __forceinline__ uint64_t wave_total(uint64_t v) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
-  return v;
+  auto turned = [](uint64_t x, auto ctrl) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, decltype(ctrl)::value, 0xf, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+    return x + composite(hi, lo);
+  };
+  v = turned(v, std::integral_constant<int, 0x121>{});  // rotations of rows of 16 lanes by 1, 2, 4, 8
+  v = turned(v, std::integral_constant<int, 0x122>{});
+  v = turned(v, std::integral_constant<int, 0x124>{});
+  v = turned(v, std::integral_constant<int, 0x128>{});
+  const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false), hi = __builtin_amdgcn_permlane16_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+  v = composite(hi[0], lo[0]) + composite(hi[1], lo[1]);
+  const auto lo2 = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false), hi2 = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+  return composite(hi2[0], lo2[0]) + composite(hi2[1], lo2[1]);
 }
 __device__ __forceinline__ double block_sum(double v, Shared& s) {
 #pragma unroll
@@ -150,10 +171,10 @@ template <int TYPE> struct Row {
   // to the exponent's bits (conversions and ldexp of doubles are slow: 134 MB of logits 57 us with them).
   __device__ __forceinline__ double weight(float l, int shift) const {
     if (top == INFINITY) return l == INFINITY ? ldexp(1.0, shift) : 0.0;
-    constexpr double ROUND_IT = 0x1.8p52;
-    const double y = fmax(((double)l - (double)top) * rate, -250000.0), up = y + ROUND_IT, z = (y - (up - ROUND_IT)) * 0.0027076061740622863;
+    constexpr double ROUND_IT = 0x1.8p52, C = 0.0027076061740622863;  // (ln 2 / 256)
+    const double y = fmax(((double)l - (double)top) * rate, -250000.0), up = y + ROUND_IT, f = y - (up - ROUND_IT);
     const int n = (int)__double_as_longlong(up);
-    const long long e = __double_as_longlong(s.pow2[n & 255] * fma(z, fma(z, fma(z, fma(z, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0));
+    const long long e = __double_as_longlong(s.pow2[n & 255] * fma(f, fma(f, fma(f, fma(f, C * C * C * C / 24, C * C * C / 6), C * C / 2), C), 1.0));
     return __longlong_as_double(e + ((long long)((n >> 8) + shift) << 52));
   }
   // the same as an integer, what is below 1 cut off
@@ -161,11 +182,6 @@ template <int TYPE> struct Row {
     const uint64_t v = (uint64_t)__double_as_longlong(weight(l, g.shift));
     const int exponent = (int)(v >> 52) - 1023;  // (at most 62, as the weights are)
     return exponent < 0 ? 0 : ((v & 0xfffffffffffffull) | 1ull << 52) << 10 >> (62 - exponent);
-  }
-
-  // 2^31 of the weight of `of` (l at most) in fp32
-  __device__ __forceinline__ uint32_t roughly(float l, float of, float rate32) const {
-    return l == of ? 1u << 31 : (uint32_t)(__builtin_amdgcn_exp2f(fmaxf((l - of) * rate32, -100.f)) * 0x1p31f);
   }
 
   // EACH elements of a round, on their way; beyond the row's end -infinity
@@ -192,16 +208,15 @@ template <int TYPE> struct Row {
     }
     return r;
   }
-  // NaN counts as -infinity, -0 as 0
+  // As they are: NaN, which counts as -infinity, is in no comparison and has a weight of 0; 0 is added to what becomes a key (-0 counts as 0)
   __device__ __forceinline__ void widen(const Raw& r, float (&l)[EACH]) const {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       if constexpr (TYPE == SI_BF16) l[i] = __uint_as_float(i % 2 ? r.v[0][i / 2] & 0xffff0000u : r.v[0][i / 2] << 16);
       else l[i] = __uint_as_float(r.v[i / 4][i % 4]);
-      l[i] = (l[i] == l[i] ? l[i] : -INFINITY) + 0.f;
     }
   }
-  // f(first element, its EACH elements, round) for the rounds [r0, r1), the next round on its way meanwhile
+  // f(first element, its EACH elements, round) for the rounds [r0, r1), the next round on its way meanwhile (two rounds ahead: the same time)
   template <class F> __device__ __forceinline__ void each(int r0, int r1, F f) const {
     Raw next = fetch(r0 * ROUND + tid * EACH);
     for (int r = r0; r < r1; ++r) {
@@ -213,37 +228,90 @@ template <int TYPE> struct Row {
     }
   }
 
+  // The lowest key of [lo, hi] for which `is` holds, where it holds for hi and for all above one that it holds for: 64 keys at a time, by any one wave
+  template <class F> __device__ __forceinline__ uint32_t lowest_key(uint32_t lo, uint32_t hi, F is) const {
+#pragma unroll 1
+    while (lo < hi) {
+      const uint32_t step = (hi - lo) / 64 + 1;
+      const uint64_t at = lo + (uint64_t)(tid % 64) * step;
+      const unsigned long long who = __ballot(at >= hi || is((uint32_t)at));
+      const uint32_t n = who ? __builtin_ctzll(who) : 64;  // probes for which it does not hold
+      hi = (uint32_t)min((uint64_t)hi, lo + (uint64_t)n * step);
+      if (n > 0) lo += (n - 1) * step + 1;
+    }
+    return lo;
+  }
+
   // What a token adds where the row is gone through in ascending index
-  enum { SAME, NUMBER, WEIGHT };  // 1 with this key; of what is left, 1 or its weight
+  enum { SAME, WEIGHT };  // 1 with this key; of what is left, its weight
   struct Left {
     uint32_t key, index;  // the last that is left
-    double least;         // and what a weight has to reach (0: nothing)
   };
+  __device__ __forceinline__ bool is_left(float last, uint32_t index, float l, int i) const { return l > last || (l == last && (uint32_t)i <= index); }
   __device__ __forceinline__ uint64_t adds(int what, const Left& left, float l, int i) const {
-    const uint32_t key = key_of(l);
-    if (l == -INFINITY) return 0;
-    if (what == SAME) return key == left.key;
-    if (key < left.key || (key == left.key && (uint32_t)i > left.index)) return 0;
-    if (left.least > 0.0 && weight(l, 0) < left.least) return 0;
-    return what == NUMBER ? 1 : whole(l);
+    const float last = value_of(left.key);
+    return what == SAME ? l == last : is_left(last, left.index, l, i) ? whole(l) : 0;
   }
-  // Their sums over runs of 512 tokens of the rounds [r0, r1), into s.part; returns the sum of all
-  __device__ __forceinline__ uint64_t add_up(int r0, int r1, int what, const Left& left) const {
-    __syncthreads();
-    each(r0, r1, [&](int at, const float (&l)[EACH], int r) {
-      uint64_t sum = 0;
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
-      sum = wave_total(sum);
-      if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = sum;
-      return true;
-    });
+  // The sum over s.part of the rounds [r0, r1)
+  __device__ __forceinline__ uint64_t add_parts(int r0, int r1) const {
     __syncthreads();
     const int parts = (r1 - r0) * WAVES;
     uint64_t before;
     return scan((2 * tid < parts ? s.part[2 * tid] : 0) + (2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0), before, s.wave_a);
   }
-  // The first token at which the sum is above `target` (below the sum of all), after add_up with the same
+  // Numbers of tokens with left's key over runs of 512 tokens of the rounds [r0, r1), into s.part; returns the number of all
+  __device__ __forceinline__ uint64_t count_same(int r0, int r1, const Left& left) const {
+    __syncthreads();
+    const float same = value_of(left.key);
+    each(r0, r1, [&](int, const float (&l)[EACH], int r) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) n += __popcll(__ballot(l[i] == same));
+      if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = n;
+      return true;
+    });
+    return add_parts(r0, r1);
+  }
+  // Sums of weights over runs of 512 tokens of the rounds [r0, r1), into s.part; returns their sum and the number of tokens.  in(logit, index): whether it counts;
+  // other(logit, index): looked at besides, for all lanes.  What counts of a round goes through a queue of its wave, so that weights are formed by 64 lanes that
+  // have one each.  (By the lanes that found them, a third of 131072 or not: 50 vector instructions an element, this way 25.)
+  struct Sum { uint64_t w, n; };
+  template <class F, class G> __device__ __forceinline__ Sum add_weights(int r0, int r1, F in, G other) const {
+    __syncthreads();
+    uint64_t all = 0;
+    float* queue = s.queue[tid / 64];
+    each(r0, r1, [&](int at, const float (&l)[EACH], int r) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        other(l[i], at + i);
+        const bool mine = in(l[i], at + i);
+        const unsigned long long who = __ballot(mine);
+        if (who == 0) continue;
+        if (mine) queue[n + __popcll(who & ((1ull << (tid % 64)) - 1))] = l[i];
+        n += __popcll(who);
+      }
+      wave_lds();
+      uint64_t sum = 0;
+      for (uint32_t k = tid % 64; k - tid % 64 < n; k += 128) {  // (two series at a time; -infinity weighs nothing)
+        const float a = k < n ? queue[k] : -INFINITY, b = k + 64 < n ? queue[k + 64] : -INFINITY;
+        sum += whole(a) + whole(b);
+      }
+      wave_lds();
+      if (tid % 64 == 0) all += n;
+      if (n > 0) sum = wave_total(sum);
+      if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = sum;
+      return true;
+    });
+    uint64_t unused;
+    all = scan(all, unused, s.wave_b);
+    return Sum{add_parts(r0, r1), all};
+  }
+  __device__ __forceinline__ Sum add_left(int r0, int r1, const Left& left) const {
+    const float last = value_of(left.key);
+    return add_weights(r0, r1, [&](float l, int i) { return is_left(last, left.index, l, i); }, [](float, int) {});
+  }
+  // The first token at which the sum is above `target` (below the sum of all), with s.part of the same
   __device__ __forceinline__ int locate(int r0, int r1, int what, const Left& left, uint64_t target) const {
     const int parts = (r1 - r0) * WAVES, lane = tid % 64;
     const uint64_t p0 = 2 * tid < parts ? s.part[2 * tid] : 0, p1 = 2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0;
@@ -313,9 +381,11 @@ template <int TYPE> struct Row {
     int size = 128;
     while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += THREADS) s.list[i] = 0;
+    __syncthreads();
     for (int k = 2; k <= size; k *= 2)
       for (int j = k / 2; j > 0; j /= 2) {
-        __syncthreads();
+        if (j >= 64 && k > 128) __syncthreads();  // (to 32, and in all of the first 128, what a wave takes is what it left)
+        else wave_lds();
         if (2 * tid < size) {
           const int i = 2 * tid - tid % j, o = i + j;  // (of 2 j neighbours, those of the first half)
           const uint64_t a = s.list[i], b = s.list[o];
@@ -327,25 +397,22 @@ template <int TYPE> struct Row {
   }
 
   // what a wave has to say, into the list as (key, ~index); s.counter counts beyond LIST too
-  __device__ __forceinline__ void listed(bool in, uint32_t key, int index) const {
+  __device__ __forceinline__ void listed(bool in, float l, int index) const {
     const unsigned long long who = __ballot(in);
     if (who == 0) return;
     uint32_t to = 0;
     if (tid % 64 == 0) to = atomicAdd(&s.counter, (uint32_t)__popcll(who));
     to = __builtin_amdgcn_readfirstlane(to) + __popcll(who & ((1ull << (tid % 64)) - 1));
-    if (in && to < LIST) s.list[to] = composite(key, ~(uint32_t)index);
+    if (in && to < LIST) s.list[to] = composite(key_of(l), ~(uint32_t)index);
   }
-  // elements with a key of lo or more into the list; returns their number, or some number above LIST
-  __device__ __forceinline__ int collect(uint32_t lo) const {
+  // elements of lo or more into the list; returns their number, or some number above LIST
+  __device__ __forceinline__ int collect(float lo) const {
     __syncthreads();
     if (tid == 0) s.counter = 0;
     __syncthreads();
     each(0, g.rounds, [&](int at, const float (&l)[EACH], int) {
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const uint32_t key = key_of(l[i]);
-        listed(key >= lo, key, at + i);
-      }
+      for (int i = 0; i < EACH; ++i) listed(l[i] >= lo, l[i], at + i);
       // (a wave may see a count of the round that others are in: it only goes on for nothing)
       return __hip_atomic_load(&s.counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= LIST;
     });
@@ -357,29 +424,48 @@ template <int TYPE> struct Row {
   struct Border { uint32_t key, index; uint64_t n, w; bool summed; };
 
   // Border of the first token at which the number (by_n) or the sum of those up to it reaches `need`, among keys of [lo, hi] (none is above hi); where none
-  // does, of the last.  A pass puts numbers or rough sums of the range into bins of its leading bits; the next takes what is above the bin in which they reach
-  // `need` exactly, and lists what is in it.  Where that shows another bin, or the list is full, once more with what is left of the range.
+  // does, of the last.  A pass puts numbers or rough sums of the range into bins; the next takes what is above the bin in which they reach `need` exactly,
+  // and lists what is in it.  Where that shows another bin, or the list is full, once more with what is left of the range.  Bins are equal parts of the logits'
+  // range at first, where a lower end is known, and of the keys' then: keys are dense next to 0, where a range that holds it would leave
+  // few bins for the rest, but three times are enough for any values.
   __device__ __forceinline__ Border border(uint32_t lo, uint32_t hi, bool by_n, uint64_t need) const {
-    uint64_t done = 0;  // number or sum above hi, as far as known
-    const float rate32 = (float)(rate / 256);
-    for (;;) {
+    uint64_t done = 0, n_hi = 0;  // number or sum above hi, as far as known; number above hi
+    const float rate32 = (float)fmin(rate / 256, 1e30), range = value_of(hi) - value_of(lo);
+    bool by_value = lo > LOWEST_KEY && range > 1e-30f && range < 1e30f;
+    const float scale = (BINS - 1) / range;
+    for (;; by_value = false) {
       const uint32_t width = hi - lo;
       const int drop = max(0, 32 - __clz((int)width) - 11);  // (at most BINS bins of 2^drop keys)
+      const float of = value_of(hi);
+      const float from = value_of(lo), to = value_to(hi);
       __syncthreads();
       for (int i = tid; i < BINS; i += THREADS) s.hist[i] = 0;
-      if (tid == 0) { s.counter = 0; s.found[0] = 0; }
-      const float of = value_of(hi);
+      if (tid == 0) { s.counter = 0; s.seen = 0; s.found[0] = 0; }
       __syncthreads();
-      each(0, g.rounds, [&](int, const float (&l)[EACH], int) {
+      uint32_t n_range = 0;
+      // (a rough sum: 2^31 of the weight of `of`, in fp32)
+      auto put_all = [&](auto values, auto numbers) {
+        each(0, g.rounds, [&](int, const float (&l)[EACH], int) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-          const uint32_t key = key_of(l[i]);
-          if (key >= lo && key <= hi)
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[(hi - key) >> drop]), by_n ? 1ull : (unsigned long long)roughly(l[i], of, rate32));
-        }
-        return true;
-      });
+          for (int i = 0; i < EACH; ++i) {
+            const bool in = l[i] >= from && l[i] <= to;
+            const unsigned long long who = __ballot(in);
+            if (who == 0) continue;
+            n_range += __popcll(who);
+            if (!in) continue;
+            const float below = of - l[i];
+            const uint32_t bin = values ? min((uint32_t)(below * scale), BINS - 1u) : (hi - key_of(l[i])) >> drop;
+            const uint32_t rough = numbers ? 1u : !values && l[i] == of ? 1u << 31 : (uint32_t)__builtin_amdgcn_exp2f(fmaf(below, -rate32, 31.f));
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]), (unsigned long long)rough);
+          }
+          return true;
+        });
+      };
+      if (by_value) by_n ? put_all(std::true_type{}, std::true_type{}) : put_all(std::true_type{}, std::false_type{});
+      else by_n ? put_all(std::false_type{}, std::true_type{}) : put_all(std::false_type{}, std::false_type{});
+      if (tid % 64 == 0) atomicAdd(&s.seen, n_range);
       __syncthreads();
+      n_range = s.seen;
       const uint64_t h0 = s.hist[2 * tid], h1 = s.hist[2 * tid + 1], goal = by_n ? need - done : (uint64_t)fmin(fmax((double)(need - done) / weight(of, g.shift) * 0x1p31, 1.0), 1e18);
       uint64_t x;
       scan(h0 + h1, x, s.wave_a);
@@ -388,63 +474,53 @@ template <int TYPE> struct Row {
       else if (h0 > 0 && x < goal) atomicMax(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)(2 * tid + 1));
       __syncthreads();
       const uint32_t bin = max((int)s.found[0] - 1, 0);  // (weights that are all roughly 0: the first)
-      const uint32_t top_of = hi - (bin << drop), low_of = max(lo, top_of - ((1u << drop) - 1));
-      __syncthreads();
-      // What is above goes through a queue of its wave, so that weights are formed by 64 lanes that have one each.  (By the lanes that found them, a third
-      // of 131072 or not: 50 vector instructions an element, this way 25.)
-      uint64_t n_above = 0;
-      float* queue = s.queue[tid / 64];
-      each(0, g.rounds, [&](int at, const float (&l)[EACH], int r) {
-        uint64_t sum = 0;
-        uint32_t n = 0, used = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-          const uint32_t key = key_of(l[i]);
-          listed(key >= low_of && key <= top_of, key, at + i);
-          const bool above = key > top_of;
-          const unsigned long long who = __ballot(above);
-          if (above) queue[(n + __popcll(who & ((1ull << (tid % 64)) - 1))) % QUEUE] = l[i];
-          n += __popcll(who);
-          wave_lds();
-          if (n - used >= 64) {
-            sum += whole(queue[(used + tid % 64) % QUEUE]);
-            used += 64;
-            wave_lds();
-          }
+      // The bin, or a range that has all of it: what follows is right for any range
+      uint32_t top_of = hi - (bin << drop), low_of = max(lo, top_of - ((1u << drop) - 1));
+      if (by_value) {
+        top_of = bin == 0 ? hi : min(hi, key_of(of - ((float)bin - 0.01f) / scale));
+        low_of = bin == BINS - 1 ? lo : min(top_of, max(lo, key_of(of - ((float)bin + 1.01f) / scale)));
+      }
+      if (by_n && !by_value) {
+        if (tid == (int)bin / 2) {
+          s.found[1] = x + (bin % 2 ? h0 : 0);
+          s.found[2] = bin % 2 ? h1 : h0;
         }
-        if (used + tid % 64 < n) sum += whole(queue[(used + tid % 64) % QUEUE]);
-        wave_lds();
-        if (tid % 64 == 0) n_above += n;
-        sum = wave_total(sum);
-        if (tid % 64 == 0) s.part[r * WAVES + tid / 64] = sum;
-        return true;
-      });
-      __syncthreads();
-      uint64_t unused;
-      const int parts = g.rounds * WAVES, inside = (int)s.counter;
-      const uint64_t w_above = scan((2 * tid < parts ? s.part[2 * tid] : 0) + (2 * tid + 1 < parts ? s.part[2 * tid + 1] : 0), unused, s.wave_a);
-      n_above = scan(n_above, unused, s.wave_b);
-      const uint64_t above = by_n ? n_above : w_above;
-      if (above >= need && top_of < hi) {  // the border is above this bin
+        __syncthreads();
+        if (s.found[2] > LIST && low_of < top_of) {  // more than can be listed
+          lo = low_of;
+          hi = top_of;
+          done += s.found[1];
+          n_hi += s.found[1];
+          continue;
+        }
+      }
+      const float bin_to = value_to(top_of), bin_from = value_of(low_of);
+      const Sum above = add_weights(0, g.rounds, [&](float l, int) { return l > bin_to; }, [&](float l, int i) { listed(l >= bin_from && l <= bin_to, l, i); });
+      const int inside = (int)s.counter;
+      const uint64_t n_above = above.n, w_above = above.w, reached = by_n ? n_above : w_above;
+      if (reached >= need && top_of < hi) {  // the border is above this bin
         lo = top_of + 1;
         continue;
       }
-      if (inside > LIST && drop > 0) {
+      const bool more = n_hi + n_range > n_above + inside;  // below low_of
+      if (inside > LIST && low_of < top_of) {
         lo = low_of;
         hi = top_of;
-        done = above;
+        done = reached;
+        n_hi = n_above;
         continue;
       }
       if (inside > LIST) {  // more tokens of one logit than the list holds: as many as are needed, from the lowest index
         const uint64_t each_w = whole(value_of(top_of)), most = inside;
-        const uint64_t k = by_n ? min(need - above, most) : each_w == 0 ? most : min((need - above + each_w - 1) / each_w, most);
-        if (low_of > lo && (by_n ? above + most : above + most * each_w) < need) {
+        const uint64_t k = by_n ? min(need - reached, most) : each_w == 0 ? most : min((need - reached + each_w - 1) / each_w, most);
+        if (more && (by_n ? reached + most : reached + most * each_w) < need) {
           hi = low_of - 1;
-          done = by_n ? above + most : above + most * each_w;
+          done = by_n ? reached + most : reached + most * each_w;
+          n_hi = n_above + most;
           continue;
         }
-        const Left same{top_of, 0, 0.0};
-        add_up(0, g.rounds, SAME, same);
+        const Left same{top_of, 0};
+        count_same(0, g.rounds, same);
         const int at = locate(0, g.rounds, SAME, same, k - 1);
         return Border{top_of, (uint32_t)at, n_above + k, w_above + k * each_w, false};
       }
@@ -457,9 +533,10 @@ template <int TYPE> struct Row {
       }
       uint64_t before;
       const uint64_t listed_w = scan(w[0] + w[1], before, s.wave_a), all = by_n ? n_above + inside : w_above + listed_w;
-      if (all < need && low_of > lo) {  // the border is below this bin
+      if (all < need && more) {  // the border is below this bin
         hi = low_of - 1;
         done = all;
+        n_hi = n_above + inside;
         continue;
       }
       const uint64_t last = min(need, all);
@@ -529,18 +606,18 @@ template <int TYPE> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, 
   if (tid == 0) s.counter = 0;
   __syncthreads();  // (and the table is there)
   R.each(r0, r1, [&](int, const float (&l)[EACH], int r) {
-    float most = l[0];
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       most = fmaxf(most, l[i]);
-      n += __popcll(__ballot(l[i] > -INFINITY));
+      n += __popcll(__ballot(l[i] >= LOWEST));  // (a ballot of > -INFINITY is compiled to one of != here, which NaN passes)
     }
     if (w.k > 0) {
       float run = fmaxf(most, __shfl_xor(most, 1));
       run = fmaxf(run, __shfl_xor(run, 2));
       if (lane % 4 == 0) put(g.runs + ((int64_t)R.row * g.rounds + r) * RUNS + tid / 4, run);
     }
-    most = value_of(wave_max(key_of(most)));
+    most = uniform(value_of(wave_max(key_of(most))));
     if (most > R.top) {
       const float before = R.top;
       R.top = most;
@@ -601,7 +678,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   // The row's largest, its number of tokens, and its sum
   const int64_t first = (int64_t)row * g.chunks;
   const float chunk_top = tid < g.chunks ? get(g.top + first + tid) : -INFINITY;
-  const float top = block_max(chunk_top, s);
+  const float top = uniform(block_max(chunk_top, s));
   uint64_t before;
   const uint64_t n_all = scan(tid < g.chunks ? get(g.n + first + tid) : 0u, before, s.wave_a);
   if (n_all == 0) { R.write(-1, 0.0, 0); return; }
@@ -611,11 +688,11 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   const double one = ldexp(1.0, g.shift);
   // How the row is gone through in the end, and with which target
   int r0 = 0, r1 = g.rounds, what = R.WEIGHT;
-  typename Row<TYPE>::Left left{LOWEST_KEY, 0xffffffffu, by_m ? least : 0.0};
+  typename Row<TYPE>::Left left{LOWEST_KEY, 0xffffffffu};
   double sum = 0.0, rest = 0.0;
   int kept = (int)n_all;
   uint64_t w_all = 0;
-  bool added = false;  // s.part has the sums of what is left
+  bool added = false, recount = false;  // s.part has the sums of what is left; kept is to be counted anew
   auto drawn = [&](uint64_t all) { return !(u > 0.f) ? 0 : u >= 1.f ? all - 1 : min((uint64_t)((double)u * (double)all), all - 1); };
   if (greedy) {
     // in the first chunk that has it
@@ -662,7 +739,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   }
   if (!greedy && !all_left) {
   // What can be left lies at or above `bound`
-  float bound = -3.402823466e38f;
+  float bound = LOWEST;
   if (k > 0) {
     // the k-th largest of the runs' maxima, by 22 leading bits of its key (a little below it)
     const int runs = g.rounds * RUNS;
@@ -697,23 +774,32 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
     const double c = (1.0 - p) * (1.0 - 1e-6) * sum / a.vocab;
     if (c > 0.0 && c < 1.0 && top < INFINITY) bound = fmaxf(bound, a_little_below((double)top + log(c) * (double)t));
   }
-  // (with both top_k and top_p the sum of all k is needed, those below min_p too)
-  if (by_m && !(k > 0 && by_p) && top < INFINITY) bound = fmaxf(bound, a_little_below((double)top + log(least) * (double)t));
   bound = fminf(bound, top);
-  const uint32_t bound_key = max(key_of(bound + 0.f), LOWEST_KEY);
+  uint32_t bound_key = max(key_of(bound), LOWEST_KEY);
+  // Weights rise with the logits, so min_p is a lowest key.  (With both top_k and top_p the sum of all k is needed, those below min_p too.)
+  if (by_m) {
+    __syncthreads();
+    if (tid < 64) {
+      const uint32_t key = R.lowest_key(LOWEST_KEY, top_key, [&](uint32_t key) { return R.weight(value_of(key), 0) >= least; });
+      if (tid == 0) s.found[0] = key;
+    }
+    __syncthreads();
+  }
+  const uint32_t m_key = by_m ? (uint32_t)s.found[0] : LOWEST_KEY;
+  if (!(k > 0 && by_p)) bound_key = max(bound_key, m_key);
 
   // Few: in order, all at once
-  const int few = k > LIST ? LIST + 1 : R.collect(bound_key);
+  const int few = k > LIST ? LIST + 1 : R.collect(value_of(bound_key));
   if (few <= LIST) {
-    R.sort(few);
+    if (by_p || (k > 0 && few > k)) R.sort(few);
     uint64_t e[2], w[2];
     bool fine[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       e[i] = 2 * tid + i < few ? s.list[2 * tid + i] : 0;
-      const float l = value_of((uint32_t)(e[i] >> 32));
-      w[i] = 2 * tid + i < few && (k == 0 || 2 * tid + i < k) ? R.whole(l) : 0;
-      fine[i] = 2 * tid + i < few && (k == 0 || 2 * tid + i < k) && (!by_m || R.weight(l, 0) >= least);
+      fine[i] = 2 * tid + i < few && (k == 0 || 2 * tid + i < k);
+      w[i] = fine[i] ? R.whole(value_of((uint32_t)(e[i] >> 32))) : 0;
+      fine[i] = fine[i] && (uint32_t)(e[i] >> 32) >= m_key;
     }
     uint64_t x;
     const uint64_t all = scan(w[0] + w[1], x, s.wave_a);
@@ -726,28 +812,44 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
     }
     uint64_t unused;
     kept = (int)scan((uint64_t)fine[0] + fine[1], unused, s.wave_b);
-    // in ascending index: what is left are the first `kept` of the list
+    if (kept <= 64) {  // in order of the index, at once
+      __syncthreads();
+      if (tid == 0) s.counter = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (fine[i]) s.list[atomicAdd(&s.counter, 1u)] = e[i] << 32 | e[i] >> 32;
+      R.sort(kept);
+      const uint64_t mine = tid < kept ? s.list[tid] : 0, weight = tid < kept ? R.whole(value_of((uint32_t)mine)) : 0;
+      const uint64_t total = scan(weight, x, s.wave_a), target = drawn(total);
+      if (x <= target && target < x + weight) {
+        s.found[0] = mine;
+        s.found[1] = weight;
+      }
+      __syncthreads();
+      R.write((int)~(uint32_t)(s.found[0] >> 32), (double)s.found[1] / (double)total, kept);
+      return;
+    }
+    // into the sums of their runs
+    for (int i = tid; i < g.rounds * WAVES; i += THREADS) s.part[i] = 0;
     __syncthreads();
+    uint64_t last = ~0ull;  // of those that are left
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (fine[i]) s.list[2 * tid + i] = e[i] << 32 | e[i] >> 32;
-    R.sort(kept);
+      if (fine[i]) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.part[~(uint32_t)e[i] / (64 * EACH)]), (unsigned long long)w[i]);
+        last = min(last, e[i]);
+      }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      e[i] = 2 * tid + i < kept ? s.list[2 * tid + i] : 0;
-      w[i] = 2 * tid + i < kept ? R.whole(value_of((uint32_t)e[i])) : 0;
-    }
-    const uint64_t total = scan(w[0] + w[1], x, s.wave_a);
-    const uint64_t target = drawn(total);
-    if (x <= target && target < x + w[0] + w[1]) {
-      const bool second = target >= x + w[0];
-      s.found[0] = second ? e[1] : e[0];
-      s.found[1] = second ? w[1] : w[0];
-    }
+    for (int d = 32; d > 0; d /= 2) last = min(last, (uint64_t)__shfl_xor(last, d));
+    if (tid == 0) s.found[0] = ~0ull;
     __syncthreads();
-    R.write((int)~(uint32_t)(s.found[0] >> 32), (double)s.found[1] / (double)total, kept);
-    return;
-  }
+    if (lane == 0) atomicMin(reinterpret_cast<unsigned long long*>(&s.found[0]), (unsigned long long)last);
+    w_all = R.add_parts(0, g.rounds);
+    left.key = (uint32_t)(s.found[0] >> 32);
+    left.index = ~(uint32_t)s.found[0];
+    added = true;
+  } else {
   // Many: the border by number, then by sum
   w_all = (uint64_t)(sum * one);
   for (int by_n = 1; by_n >= 0; --by_n) {
@@ -757,11 +859,24 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
     left.index = b.index;
     kept = (int)b.n;
     w_all = b.w;
-    added = b.summed && !by_m;
+    added = b.summed;
   }
-  if (by_m) kept = (int)R.add_up(0, g.rounds, R.NUMBER, left);
+  if (m_key > left.key) {
+    left.key = m_key;
+    left.index = 0xffffffffu;
+    added = false;
   }
-  uint64_t total = added ? w_all : R.add_up(r0, r1, what, left);
+  recount = !added;
+  }
+  }
+  uint64_t total = w_all;
+  if (greedy) {
+    total = R.count_same(r0, r1, left);
+  } else if (!added) {
+    const auto sums = R.add_left(r0, r1, left);
+    total = sums.w;
+    if (recount) kept = (int)sums.n;
+  }
   uint64_t target = greedy ? 0 : drawn(total);
   if (all_left) {
     if (total > 0) {
@@ -769,7 +884,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
     } else {  // (a chunk of weights that are all below the smallest integer)
       r0 = 0;
       r1 = g.rounds;
-      total = R.add_up(r0, r1, what, left);
+      total = R.add_left(r0, r1, left).w;
       target = drawn(total);
     }
   }

@@ -120,6 +120,21 @@ def test_many_tokens_are_left(limits):
     check(normal(2, 70001, torch.bfloat16, spread=0.5), **limits)
 
 
+@pytest.mark.parametrize("limits", [dict(top_p=0.9, min_p=1e-3), dict(top_p=0.999, min_p=0.02), dict(top_p=0.3, min_p=1e-6), dict(top_k=4000, top_p=0.5, min_p=0.05),
+                                    dict(top_k=4000, min_p=1e-3), dict(min_p=1e-3), dict(top_k=1500), dict(top_k=1500, top_p=0.95)], ids=str)
+def test_limits_that_meet_among_many(limits):
+    """one limit reached within what another leaves or beyond it; logits that are far from 0, next to it or 0 and -0 in turn, and far apart"""
+    x = normal(6, 60007, spread=1.5)
+    x[1] -= 40.0
+    x[2] *= 1e-3
+    x[3, ::2] = 0.0
+    x[3, 1::2] = -0.0
+    x[3, 50000:] = normal(1, 10007, seed=5)[0]
+    x[4] = x[4].clamp(max=0.0)
+    x[5, 3:9] = torch.tensor([9.0, 500.0, 499.0, 498.5, -2e30, 497.0], device="cuda")
+    check(x, u=[0.2, 0.9, 0.5, 0.66, 0.999, 0.31], **limits)
+
+
 def test_each_row_has_its_own_limits():
     rng = np.random.default_rng(4)
     R = 64
