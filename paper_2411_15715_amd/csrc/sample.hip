@@ -6,12 +6,12 @@
 // of top_p, and min_p is a lowest logit.  Few tokens beyond that bound (2048) are sorted in LDS.  Of many, the border is looked for in bins (border()).
 // Weights are integers (2^62 / vocab or more for the largest), so that sums in any order are the same and a token never depends on scheduling.
 //
-// Chunks of up to 512 blocks and the rest are one launch, the block of a row that finishes last goes on; more chunks have a launch of their own with half the
-// registers, of 4 rounds each.  (One launch for all: 256 rows of 131072 in fp32 161 us, in two 118.)
+// Up to 256 chunks and the rest are one launch, in which the block of a row that finishes last goes on; more have a launch of their own, whose blocks need
+// half the registers.
 // Measured in the kernels: one row of 32000 bf16, top_k 50 and top_p 0.95, 20.7 us, nearly all of it one dependent step after another; 256 x 131072
-// fp32, top_p 0.9, 41 + 78 us, 134 MB once at 3.3 TB/s and then twice at 8 from the caches, bound by vector instructions: 25 for a weight in 64 bits, which
+// fp32, top_p 0.9, 40 + 79 us, 134 MB once at 3.4 TB/s and then twice at 8 from the caches, bound by vector instructions: 25 for a weight in 64 bits, which
 // a token's border needs (an error of 1e-7 of the sum would move one draw in a hundred here), and 10 for a place in a bin; 61 rows of 100003 with
-// limits of their own 13 + 78 us, a compute unit a row.
+// limits of their own 13 + 76 us, a compute unit a row.
 #include "si_internal.h"
 #include "si_error.h"
 #include "scheinfer_attention.h"
@@ -33,14 +33,14 @@ constexpr int EACH = 8;                    // neighbouring elements of a thread
 constexpr int ROUND = THREADS * EACH;      // elements that a block takes at once
 constexpr int MAX_ROUNDS = SI_SAMPLE_MAX_VOCAB / ROUND;
 constexpr int RUNS = THREADS / 4;          // of a round, 4 threads each
-constexpr int WIDE = 4;                    // rounds of a chunk where there are many
+constexpr int WIDE = 4;                    // rounds of a chunk at most
 constexpr int BINS = 2048, LIST = 2048;    // two a thread
 constexpr int QUEUE = 64 * EACH;           // of a wave
 
 struct Args {
   si_sample_t a;
   int rounds;      // of a row
-  int chunks;      // of a row: 1 or WIDE rounds each
+  int chunks;      // of a row: 1 to WIDE rounds each
   int per;         // rounds of a chunk
   int shift;       // a weight of 1 is 2^shift
   uint32_t* count; // [rows] chunks done; 0 between calls
@@ -956,9 +956,11 @@ extern "C" int si_sample(const si_sample_t* a, void* stream) {
   int log2 = 0;
   while ((1 << log2) < a->vocab) ++log2;
   g.shift = 62 - log2;
-  // One launch where the chunks fill the chip twice at most (its blocks have registers for the row's end: one a compute unit)
-  const bool alone = (int64_t)a->rows * g.rounds <= 512;
-  g.per = alone ? 1 : WIDE;
+  // One launch for no more chunks than compute units (its blocks have registers for the row's end: one a unit).  Else chunks that fill the chip twice.
+  // Rows of 100003 fp32 with top_p 0.9 in one launch and in two: 8 rows 69 and 74 us, 32 rows 98 and 74; 256 x 131072: 1116 and 120.
+  const int64_t all = (int64_t)a->rows * g.rounds;
+  const bool alone = all <= 256;
+  g.per = alone ? 1 : (int)std::min<int64_t>(WIDE, (all + 511) / 512);
   g.chunks = (g.rounds + g.per - 1) / g.per;
   const dim3 chunks((unsigned)(a->rows * g.chunks)), rows((unsigned)a->rows), block(THREADS);
   const hipStream_t st = (hipStream_t)stream;
