@@ -292,7 +292,7 @@ typedef struct {
 /*
  * The assignment alone, as si_route; out->idx and out->w are needed (their memory is the call's only working memory: nothing is allocated,
  * any call can be recorded into a HIP graph), the others may be NULL.  Runs on the current HIP device.
- * Errors: SI_EINVAL (NULL or misaligned pointer, T outside 0 .. 2^24 or T * k of 2^31 or more, E outside 1 .. 256, k outside 1 .. E, unknown
+ * Errors: SI_EINVAL (NULL or misaligned pointer, T outside 0 .. 2^24 or T * k above 2^30, E outside 1 .. 256, k outside 1 .. E, unknown
  * score, scale not finite, n_groups negative or no divisor of E, top_groups or group_best outside their groups, fewer than k experts in top_groups
  * groups), SI_EHIP.  T == 0 is a no-op.
  */

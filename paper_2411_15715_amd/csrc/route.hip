@@ -406,7 +406,7 @@ int check_score(const si_score_t* s, int E, int k, const char* who) {
 extern "C" int si_route_scored(const float* logits_dev, int32_t T, int32_t E, int32_t k, const si_score_t* score, const si_routing_out_t* out, void* stream) {
   using namespace si;
   const char* who = "si_route_scored";
-  if (T < 0 || T > (1 << 24) || E < 1 || E > MAX_EXPERTS || k < 1 || k > E || (int64_t)T * k >= ((int64_t)1 << 31))
+  if (T < 0 || T > (1 << 24) || E < 1 || E > MAX_EXPERTS || k < 1 || k > E || (int64_t)T * k > (1 << 30))  // (pairs are counted in 32 bits, in steps of a block)
     return set_error(SI_EINVAL, "%s: bad T=%d E=%d k=%d", who, T, E, k);
   if (int rc = check_score(score, E, k, who)) return rc;
   if (!out) return set_error(SI_EINVAL, "%s: out is NULL", who);

@@ -28,7 +28,7 @@ def test_bad_scores_are_refused(kw):
     assert "si_route_scored" in refused(si.si_route_scored, BASE, 3, 16, 5, si.si_score_t(**kw), ALL)
 
 
-@pytest.mark.parametrize("T, E, k", [(-1, 16, 2), ((1 << 24) + 1, 16, 2), (1 << 24, 256, 128), (3, 0, 1), (3, 257, 2), (3, 16, 0), (3, 16, 17)])
+@pytest.mark.parametrize("T, E, k", [(-1, 16, 2), ((1 << 24) + 1, 16, 2), (1 << 24, 256, 128), (14221746, 151, 151), (1 << 23, 256, 129), (3, 0, 1), (3, 257, 2), (3, 16, 0), (3, 16, 17)])
 def test_bad_sizes_are_refused(T, E, k):
     refused(si.si_route_scored, BASE, T, E, k, si.si_score_t(), ALL)
 
