@@ -93,7 +93,7 @@ template <int TYPE, int D> struct Wide {
     }
     auto sees_from = [&](int t) {  // (members of a group have a place in the table)
       const int e = t / n_new, sq = g.a.seqs ? g.a.seqs[e] : e;
-      return max(0, c.lens[sq] - n_new + 1 + t % n_new - window);
+      return max(0, min(c.lens[sq], c.max_pages * c.page_tokens) - n_new + 1 + t % n_new - window);
     };
     const int see_lo = window && tok >= 0 ? sees_from(tok) : 0;
 

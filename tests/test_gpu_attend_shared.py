@@ -203,6 +203,16 @@ def test_pages_outside_the_pool_and_bad_sequences():
             compare(c, q[s:s + 1], lens, 1, 4, 0, 0, 0.0, [s], out[s:s + 1], lse[s:s + 1])
 
 
+@pytest.mark.parametrize("length", [321, 100000, 0x7fffffff])
+def test_lengths_beyond_the_table_are_cut_under_windows_too(length):
+    c, lens, rows = shared_cache(BF, [(256, [5, 64, 9])], 64, 2, 64, shuffled=False)
+    c.lens[1] = length  # (its 320 tokens fill the table)
+    q = torch.randn((3, 4 * 64), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    out, lse = call(c, q, lens, rows, 1, 4, window=100)
+    assert int(c.status.item()) == si.SI_CACHE_BAD_LEN
+    compare(c, q, lens, 1, 4, 100, 0, 0.0, rows, out, lse)
+
+
 @pytest.mark.parametrize("kind", [BF, F8])
 @pytest.mark.parametrize("per,n_new", [(4, 1), (6, 2), (8, 6)])
 def test_values_that_are_not_finite(kind, per, n_new):
