@@ -231,6 +231,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
 }
 
 constexpr int WIDE = 128;  // rows of a shared piece
+constexpr int MOST_ROWS = 1 << 16;
 
 struct Layout {
   AttendCut alone;           // of si_attend
@@ -243,21 +244,23 @@ struct Layout {
 Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
   Layout l{};
   l.alone = cut_attend(c, a);
-  const int of_entry = a.n_new * (a.n_heads / c.n_kv_heads);
-  const int64_t rows = (int64_t)a.n * of_entry;
+  const int64_t of_entry = (int64_t)a.n_new * (a.n_heads / c.n_kv_heads);
+  // (a block of the joining launch has 4 rows or more, and all rows have two sums; longer lists are si_attend's and need its scratch and that of shorter ones)
+  const int n = (int)std::min<int64_t>(a.n, MOST_ROWS / of_entry);
+  const int64_t rows = n * of_entry;
+  l.bytes = l.alone.scratch;
+  if (n < 2) return l;
   // Pieces cost three launches, some 25 us of planning and joining, so calls that are short anyway are si_attend: those that read less than 640 MB even if
   // no page were shared.  Measured with one prompt for all, heads 32 of 8 x 128 bf16, as pieces and as si_attend: 4 x 611 tokens (12 MB) 24 and 14 us,
   // 64 x 1000 (288 MB) 37 and 18, 64 x 2000 (550 MB) 38 and 31, 256 x 512 (642 MB) 57 and 43, 64 x 4000 (1075 MB) 43 and 68, 64 x 8000 50 and 135.
-  // The joining launch has a block for 4 rows and more.
-  const int64_t sight = a.window > 0 ? std::min<int64_t>(a.max_len, (int64_t)a.window + a.n_new) : a.max_len;
-  const int64_t reads = a.n * sight * c.n_kv_heads * c.head_dim * (c.type == SI_KV_BF16 ? 4 : 2);
-  l.pieces = a.n > 1 && rows <= 200000 && (reads >= 640000000 || std::getenv("SI_ATTEND_PIECES"));  // (the variable: tests of the pieces at small sizes)
+  const double sight = a.window > 0 ? std::min<double>(a.max_len, (double)a.window + a.n_new) : a.max_len, reads = a.n * sight * c.n_kv_heads * c.head_dim * (c.type == SI_KV_BF16 ? 4 : 2);
+  l.pieces = n == a.n && (reads >= 640e6 || std::getenv("SI_ATTEND_PIECES"));  // (the variable: tests of the pieces at small sizes)
   for (l.block_rows = 16; l.block_rows < of_entry && l.block_rows < 64;) l.block_rows *= 2;
-  l.chunks = (of_entry + l.block_rows - 1) / l.block_rows;
+  l.chunks = (int)((of_entry + l.block_rows - 1) / l.block_rows);
   const int64_t each = (a.max_len + kv_block(c.type) - 1) / kv_block(c.type), turns = (rows + WIDE - 1) / WIDE * each * c.n_kv_heads / 256;
   l.shared_slices = std::max(1, (turns > 32 && c.head_dim < 192 ? 512 : 256) / c.n_kv_heads);
-  l.own_slices = std::max(1, std::min(std::max(a.n * l.chunks, 256 / c.n_kv_heads), 512 / c.n_kv_heads));
-  const int64_t shared = rows / WIDE + a.n / 2 + 1, own = (int64_t)a.n * l.chunks;
+  l.own_slices = std::max(1, std::min(std::max(n * l.chunks, 256 / c.n_kv_heads), 512 / c.n_kv_heads));
+  const int64_t shared = rows / WIDE + n / 2 + 1, own = (int64_t)n * l.chunks;
   int64_t at = std::max<int64_t>(l.alone.scratch, ATTEND_COUNTERS * 4);  // (the counters are at the same place in every call's scratch)
   auto take = [&](int64_t bytes) {
     const int64_t q = (at + 15) / 16 * 16;
@@ -267,17 +270,17 @@ Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
   l.shared_parted = take(shared * 8);
   l.own_parted = take(own * 8);
   l.shared_part = take((int64_t)c.n_kv_heads * l.shared_slices * 2 * WIDE * (c.head_dim + 4) * 4);
-  l.own_part = take((int64_t)c.n_kv_heads * l.own_slices * 2 * std::min(of_entry, l.block_rows) * (c.head_dim + 2) * 4);
+  l.own_part = take((int64_t)c.n_kv_heads * l.own_slices * 2 * std::min<int64_t>(of_entry, l.block_rows) * (c.head_dim + 2) * 4);
   l.sums = take(2 * c.n_kv_heads * rows * (c.head_dim + 4) * 4);
   l.shared = take(shared * (int64_t)sizeof(Piece));
   l.own = take(own * (int64_t)sizeof(Piece));
   l.shared_starts = take(l.shared_slices * (int64_t)sizeof(SliceStart));
   l.own_starts = take(l.own_slices * (int64_t)sizeof(SliceStart));
-  l.group = take(a.n * 8ll);
-  l.facts = take(a.n * 8ll);
+  l.group = take(n * 8ll);
+  l.facts = take(n * 8ll);
   l.most = shared;
-  l.local = area_words(a.n, shared, l.chunks) <= AREA;
-  l.area = take(l.local ? 0 : area_words(a.n, shared, l.chunks) * 4);
+  l.local = area_words(n, shared, l.chunks) <= AREA;
+  l.area = take(l.local ? 0 : area_words(n, shared, l.chunks) * 4);
   l.bytes = (at + 15) / 16 * 16;
   return l;
 }

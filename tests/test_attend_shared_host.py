@@ -49,6 +49,18 @@ def test_bad_caches_layers_and_missing_descriptors_are_refused():
     assert L.si_attend_shared(ctypes.byref(cache()), 0, None, None) == si.SI_EINVAL
 
 
+def test_calls_that_are_never_in_pieces_need_no_scratch_for_them():
+    """one sequence, and rows beyond what a plan takes; but what serves a list serves the shorter ones that are planned"""
+    c = cache(head_dim=128, n_kv_heads=8, n_seqs=4096, max_pages=4096)
+    one = attend(n=1, n_new=65536, n_heads=1024, max_len=100000)
+    assert si.si_attend_shared_scratch_bytes(c, one) == si.si_attend_scratch_bytes(c, one)
+    most = si.si_attend_shared_scratch_bytes(c, attend(n=4000, n_new=100, n_heads=64, max_len=5000))
+    assert most < 2 << 30
+    for n in (2, 50, 81, 82, 1000, 3999):
+        a = attend(n=n, n_new=100, n_heads=64, max_len=5000)
+        assert si.si_attend_scratch_bytes(c, a) <= si.si_attend_shared_scratch_bytes(c, a) <= most
+
+
 def test_no_sequences_is_a_no_op():
     si.si_attend_shared(cache(), 0, attend(n=0, q=None, out=None, scratch=None, scratch_bytes=0))
 
