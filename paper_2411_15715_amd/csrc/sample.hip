@@ -60,7 +60,7 @@ struct Shared {
   float queue[WAVES][QUEUE];
   double pow2[256];                   // 2^(i / 256)
   double wave_d[WAVES];
-  float wave_f[WAVES];
+  uint32_t wave_k[WAVES];
   uint64_t found[3];
   uint32_t counter, seen, last;
 };
@@ -95,66 +95,65 @@ __device__ __forceinline__ void wave_lds() {
 // Elements of a thread one after the other: eight series at once do not fit the registers of 16 waves
 __device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
 
+// Steps over the lanes of a wave in registers (by way of LDS each waits some hundred cycles).  MASK: rows of 16 lanes that take part, 0 elsewhere
+template <int CTRL, int MASK = 0xf> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, MASK, 0xf, false); }
+template <int CTRL, int MASK = 0xf> __device__ __forceinline__ uint64_t moved(uint64_t v) {
+  return composite(moved<CTRL, MASK>((uint32_t)(v >> 32)), moved<CTRL, MASK>((uint32_t)v));
+}
+template <int CTRL> __device__ __forceinline__ double moved(double v) { return __longlong_as_double((long long)moved<CTRL>((uint64_t)__double_as_longlong(v))); }
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane) { return composite(of_lane((uint32_t)(v >> 32), lane), of_lane((uint32_t)v, lane)); }
+__device__ __forceinline__ double of_lane(double v, int lane) { return __longlong_as_double((long long)of_lane((uint64_t)__double_as_longlong(v), lane)); }
+constexpr int SHIFT = 0x110, TURN = 0x120, FROM_ROW = 0x142, FROM_HALF = 0x143;  // SHIFT, TURN + n: from the lane n before, in rows of 16
+
+// of the lanes up to this one
+template <class T> __device__ __forceinline__ T scan_row(T v) {  // of 16
+  v += moved<SHIFT + 1>(v);
+  v += moved<SHIFT + 2>(v);
+  v += moved<SHIFT + 4>(v);
+  return v + moved<SHIFT + 8>(v);
+}
+template <class T> __device__ __forceinline__ T scan_wave(T v) {
+  v = scan_row(v);
+  v += moved<FROM_ROW, 0xa>(v);
+  return v + moved<FROM_HALF, 0xc>(v);
+}
+template <class T> __device__ __forceinline__ T total_row(T v) {
+  v += moved<TURN + 1>(v);
+  v += moved<TURN + 2>(v);
+  v += moved<TURN + 4>(v);
+  return v + moved<TURN + 8>(v);
+}
+// the same in all lanes (of doubles, whose sums depend on their order, those of the lanes of one row after the other)
+template <class T> __device__ __forceinline__ T wave_total(T v) {
+  v = total_row(v);
+  return (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
+}
+
 // sum over the block; before: of the threads before this one
-__device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t& before, uint64_t (&waves)[WAVES]) {
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  uint64_t x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+template <class T> __device__ __forceinline__ T scan(T v, T& before, uint64_t (&waves)[WAVES]) {
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const T x = scan_wave(v);
   __syncthreads();
   if (lane == 63) waves[wave] = x;
   __syncthreads();
-  before = x - v;
-  x = waves[lane % WAVES];
-  const uint64_t own = x;
-#pragma unroll
-  for (int d = 1; d < WAVES; d *= 2) {
-    const uint64_t y = __shfl_up(x, d, WAVES);
-    if (lane % WAVES >= d) x += y;
-  }
-  before += __shfl(x - own, wave);
-  return __shfl(x, WAVES - 1);
-}
-// (in registers: by way of LDS a step waits some hundred cycles)
-__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
-  auto turned = [](uint64_t x, auto ctrl) {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, decltype(ctrl)::value, 0xf, 0xf, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
-    return x + composite(hi, lo);
-  };
-  v = turned(v, std::integral_constant<int, 0x121>{});  // rotations of rows of 16 lanes by 1, 2, 4, 8
-  v = turned(v, std::integral_constant<int, 0x122>{});
-  v = turned(v, std::integral_constant<int, 0x124>{});
-  v = turned(v, std::integral_constant<int, 0x128>{});
-  const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false), hi = __builtin_amdgcn_permlane16_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
-  v = composite(hi[0], lo[0]) + composite(hi[1], lo[1]);
-  const auto lo2 = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false), hi2 = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
-  return composite(hi2[0], lo2[0]) + composite(hi2[1], lo2[1]);
+  const T own = (T)waves[lane % WAVES], y = scan_row(own);
+  before = x - v + of_lane((T)(y - own), wave);
+  return of_lane(y, WAVES - 1);
 }
 __device__ __forceinline__ double block_sum(double v, Shared& s) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  v = wave_total(v);
   __syncthreads();
   if (threadIdx.x % 64 == 0) s.wave_d[threadIdx.x / 64] = v;
   __syncthreads();
-  v = s.wave_d[threadIdx.x % WAVES];
-#pragma unroll
-  for (int d = WAVES / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
-  return v;
+  return of_lane(total_row(s.wave_d[threadIdx.x % WAVES]), 0);
 }
-__device__ __forceinline__ float block_max(float v, Shared& s) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+__device__ __forceinline__ float block_max(float v, Shared& s) {  // of numbers
+  const uint32_t key = wave_max(key_of(v));
   __syncthreads();
-  if (threadIdx.x % 64 == 0) s.wave_f[threadIdx.x / 64] = v;
+  if (threadIdx.x % 64 == 0) s.wave_k[threadIdx.x / 64] = key;
   __syncthreads();
-  v = s.wave_f[threadIdx.x % WAVES];
-#pragma unroll
-  for (int d = WAVES / 2; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return uniform(value_of(wave_max(s.wave_k[threadIdx.x % WAVES])));
 }
 
 template <int TYPE> struct Row {
@@ -332,13 +331,7 @@ template <int TYPE> struct Row {
       uint64_t sum = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { sum += adds(what, left, l[i], at + i); one_by_one(); }
-      uint64_t x = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-      }
-      x -= sum;
+      uint64_t x = scan_wave(sum) - sum;
       if (x <= rest && rest < x + sum) {
         int token = -1;
 #pragma unroll
@@ -678,9 +671,9 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   // The row's largest, its number of tokens, and its sum
   const int64_t first = (int64_t)row * g.chunks;
   const float chunk_top = tid < g.chunks ? get(g.top + first + tid) : -INFINITY;
-  const float top = uniform(block_max(chunk_top, s));
-  uint64_t before;
-  const uint64_t n_all = scan(tid < g.chunks ? get(g.n + first + tid) : 0u, before, s.wave_a);
+  const float top = block_max(chunk_top, s);
+  uint32_t before;
+  const uint32_t n_all = scan(tid < g.chunks ? get(g.n + first + tid) : 0u, before, s.wave_a);
   if (n_all == 0) { R.write(-1, 0.0, 0); return; }
   R.top = top;
   const uint32_t top_key = key_of(top);
@@ -757,7 +750,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
         }
         __syncthreads();
         const uint32_t n0 = (uint32_t)s.hist[2 * tid], n1 = (uint32_t)s.hist[2 * tid + 1];
-        uint64_t x;
+        uint32_t x;
         scan(n0 + n1, x, s.wave_a);
         if (x < need && need <= x + n0 + n1) {
           const bool second = need > x + n0;
@@ -810,8 +803,8 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
       fine[0] = fine[0] && (2 * tid == 0 || (double)x < goal);
       fine[1] = fine[1] && (double)(x + w[0]) < goal;
     }
-    uint64_t unused;
-    kept = (int)scan((uint64_t)fine[0] + fine[1], unused, s.wave_b);
+    uint32_t unused;
+    kept = (int)scan((uint32_t)fine[0] + fine[1], unused, s.wave_b);
     if (kept <= 64) {  // in order of the index, at once
       __syncthreads();
       if (tid == 0) s.counter = 0;
