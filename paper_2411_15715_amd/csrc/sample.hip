@@ -8,10 +8,10 @@
 //
 // Up to 256 chunks and the rest are one launch, in which the block of a row that finishes last goes on; more have a launch of their own, whose blocks need
 // half the registers.
-// Measured in the kernels: one row of 32000 bf16, top_k 50 and top_p 0.95, 20.7 us, nearly all of it one dependent step after another; 256 x 131072
-// fp32, top_p 0.9, 40 + 79 us, 134 MB once at 3.4 TB/s and then twice at 8 from the caches, bound by vector instructions: 25 for a weight in 64 bits, which
-// a token's border needs (an error of 1e-7 of the sum would move one draw in a hundred here), and 10 for a place in a bin; 61 rows of 100003 with
-// limits of their own 13 + 76 us, a compute unit a row.
+// Measured in the kernels: one row of 32000 bf16, top_k 50 and top_p 0.95, 17 us, one dependent step after another (chunks 4, bound 4, pass over the
+// row 3, order and draw 5); 256 x 131072 fp32, top_p 0.9, 38 + 73 us: 134 MB once at 3.5 TB/s and then twice at some 8 from the caches, bound by vector
+// instructions, 25 for a weight in 64 bits, which a token's border needs (an error of 1e-7 of the sum would move one draw in a hundred here), and 10
+// for a place in a bin; 61 rows of 100003 with limits of their own 12 + 70 us, a compute unit a row.
 #include "si_internal.h"
 #include "si_error.h"
 #include "scheinfer_attention.h"
@@ -35,7 +35,6 @@ constexpr int MAX_ROUNDS = SI_SAMPLE_MAX_VOCAB / ROUND;
 constexpr int RUNS = THREADS / 4;          // of a round, 4 threads each
 constexpr int WIDE = 4;                    // rounds of a chunk at most
 constexpr int BINS = 2048, LIST = 2048;    // two a thread
-constexpr int QUEUE = 64 * EACH;           // of a wave
 
 struct Args {
   si_sample_t a;
@@ -50,19 +49,23 @@ struct Args {
   float* runs;     // [rows][rounds * RUNS]
 };
 
-struct Shared {
+struct SumsShared {  // of a block that has chunks only: two on a compute unit
+  double pow2[256];                   // 2^(i / 256)
+  double wave_d[WAVES];
+  uint32_t wave_k[WAVES];
+  uint32_t counter;
+};
+struct Shared : SumsShared {
   union {
     uint64_t hist[BINS];
     uint64_t list[LIST];
   };
   uint64_t part[MAX_ROUNDS * WAVES];  // sums of runs of 512 elements
   uint64_t wave_a[WAVES], wave_b[WAVES];
-  float queue[WAVES][QUEUE];
-  double pow2[256];                   // 2^(i / 256)
-  double wave_d[WAVES];
-  uint32_t wave_k[WAVES];
+  float queue[WAVES][64 * EACH];
+  uint64_t late[WAVES][128];
   uint64_t found[3];
-  uint32_t counter, seen, last;
+  uint32_t seen, last;
 };
 
 // what other blocks read within the launch goes past the caches of this die
@@ -86,6 +89,8 @@ __device__ __forceinline__ float a_little_below(double v) {
 }
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }  // (the same in all lanes)
 __device__ __forceinline__ uint64_t composite(uint32_t hi, uint32_t lo) { return (uint64_t)hi << 32 | lo; }
+
+__device__ __forceinline__ uint32_t lanes_before(unsigned long long who) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u)); }
 
 // LDS of a wave: its accesses are in order, only the compiler has to keep it
 __device__ __forceinline__ void wave_lds() {
@@ -141,14 +146,14 @@ template <class T> __device__ __forceinline__ T scan(T v, T& before, uint64_t (&
   before = x - v + of_lane((T)(y - own), wave);
   return of_lane(y, WAVES - 1);
 }
-__device__ __forceinline__ double block_sum(double v, Shared& s) {
+__device__ __forceinline__ double block_sum(double v, SumsShared& s) {
   v = wave_total(v);
   __syncthreads();
   if (threadIdx.x % 64 == 0) s.wave_d[threadIdx.x / 64] = v;
   __syncthreads();
   return of_lane(total_row(s.wave_d[threadIdx.x % WAVES]), 0);
 }
-__device__ __forceinline__ float block_max(float v, Shared& s) {  // of numbers
+__device__ __forceinline__ float block_max(float v, SumsShared& s) {  // of numbers
   const uint32_t key = wave_max(key_of(v));
   __syncthreads();
   if (threadIdx.x % 64 == 0) s.wave_k[threadIdx.x / 64] = key;
@@ -156,9 +161,9 @@ __device__ __forceinline__ float block_max(float v, Shared& s) {  // of numbers
   return uniform(value_of(wave_max(s.wave_k[threadIdx.x % WAVES])));
 }
 
-template <int TYPE> struct Row {
+template <int TYPE, class S> struct Row {
   const Args& g;
-  Shared& s;
+  S& s;
   const char* logits;
   int vocab, row, tid;
   float top;        // the row's largest (in the first pass the chunk's)
@@ -227,6 +232,28 @@ template <int TYPE> struct Row {
     }
   }
 
+  // those of a round's elements for which in(logit) holds, into the list as (key, ~index); s.counter counts beyond LIST too.  (One addition a wave: with one for
+  // each of its elements a pass that lists 1442 of 100003 took 14 us.)
+  template <class F> __device__ __forceinline__ void listed(const float (&l)[EACH], int at, F in) const {
+    unsigned long long who[EACH];
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      who[i] = __ballot(in(l[i]));
+      n += __popcll(who[i]);
+    }
+    if (n == 0) return;
+    uint32_t to = 0;
+    if (tid % 64 == 0) to = atomicAdd(&s.counter, n);
+    to = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const uint32_t mine = to + lanes_before(who[i]);
+      if (in(l[i]) && mine < LIST) s.list[mine] = composite(key_of(l[i]), ~(uint32_t)(at + i));
+      to += __popcll(who[i]);
+    }
+  }
+
   // The lowest key of [lo, hi] for which `is` holds, where it holds for hi and for all above one that it holds for: 64 keys at a time, by any one wave
   template <class F> __device__ __forceinline__ uint32_t lowest_key(uint32_t lo, uint32_t hi, F is) const {
 #pragma unroll 1
@@ -272,43 +299,78 @@ template <int TYPE> struct Row {
     return add_parts(r0, r1);
   }
   // Sums of weights over runs of 512 tokens of the rounds [r0, r1), into s.part; returns their sum and the number of tokens.  in(logit, index): whether it counts;
-  // other(logit, index): looked at besides, for all lanes.  What counts of a round goes through a queue of its wave, so that weights are formed by 64 lanes that
-  // have one each.  (By the lanes that found them, a third of 131072 or not: 50 vector instructions an element, this way 25.)
+  // other(logits, first index): looked at besides.  What counts goes through a queue of its wave, so that weights are formed by 64 lanes that have one
+  // each.  (By the lanes that found them, a third of 131072 or not: 50 vector instructions an element, this way 25.  Rounds
+  // of few by themselves: of a row in which 328 of 100003 count the pass 17.5 us, together 11.6; all by way of the runs' atomics: where 56000 do 44 us, this way 36.)
   struct Sum { uint64_t w, n; };
   template <class F, class G> __device__ __forceinline__ Sum add_weights(int r0, int r1, F in, G other) const {
+    const int lane = tid % 64, wave = tid / 64, parts = (r1 - r0) * WAVES;
     __syncthreads();
-    uint64_t all = 0;
-    float* queue = s.queue[tid / 64];
+    for (int i = tid; i < parts; i += THREADS) s.part[i] = 0;
+    __syncthreads();
+    // What 64 or more of a round bring is summed at once; of fewer, logits wait with their runs until they are 64.  A wave alone adds to the sums of its runs
+    float* queue = s.queue[wave];
+    uint64_t* late = s.late[wave];
+    uint32_t n_late = 0, all = 0;
+    auto add_late = [&](uint32_t many) {  // the first 64, or as many as there are
+      wave_lds();
+      if ((uint32_t)lane < many) {
+        const uint64_t e = late[lane];
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s.part[(e >> 32) * WAVES + wave]), (unsigned long long)whole(__uint_as_float((uint32_t)e)));
+      }
+      const uint64_t next = late[lane + 64];
+      wave_lds();
+      late[lane] = next;
+      n_late -= many;
+      wave_lds();
+    };
     each(r0, r1, [&](int at, const float (&l)[EACH], int r) {
+      other(l, at);
+      unsigned long long who[EACH];
       uint32_t n = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        other(l[i], at + i);
-        const bool mine = in(l[i], at + i);
-        const unsigned long long who = __ballot(mine);
-        if (who == 0) continue;
-        if (mine) queue[n + __popcll(who & ((1ull << (tid % 64)) - 1))] = l[i];
-        n += __popcll(who);
+        who[i] = __ballot(in(l[i], at + i));
+        n += __popcll(who[i]);
       }
-      wave_lds();
-      uint64_t sum = 0;
-      for (uint32_t k = tid % 64; k - tid % 64 < n; k += 128) {  // (two series at a time; -infinity weighs nothing)
-        const float a = k < n ? queue[k] : -INFINITY, b = k + 64 < n ? queue[k + 64] : -INFINITY;
-        sum += whole(a) + whole(b);
+      if (n == 0) return true;
+      all += n;
+      uint32_t to = 0;
+      if (n >= 64) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          if (in(l[i], at + i)) queue[to + lanes_before(who[i])] = l[i];
+          to += __popcll(who[i]);
+        }
+        wave_lds();
+        uint64_t sum = 0;
+        for (uint32_t k = lane; k - lane < n; k += 128) {  // (two series at a time; -infinity weighs nothing)
+          const float a = k < n ? queue[k] : -INFINITY, b = k + 64 < n ? queue[k + 64] : -INFINITY;
+          sum += whole(a) + whole(b);
+        }
+        wave_lds();
+        sum = wave_total(sum);
+        if (lane == 0) s.part[(r - r0) * WAVES + wave] = sum;
+        return true;
       }
-      wave_lds();
-      if (tid % 64 == 0) all += n;
-      if (n > 0) sum = wave_total(sum);
-      if (tid % 64 == 0) s.part[(r - r0) * WAVES + tid / 64] = sum;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        if (in(l[i], at + i)) late[n_late + to + lanes_before(who[i])] = composite((uint32_t)(r - r0), __float_as_uint(l[i]));
+        to += __popcll(who[i]);
+      }
+      n_late += n;
+      if (n_late >= 64) add_late(64);
       return true;
     });
-    uint64_t unused;
-    all = scan(all, unused, s.wave_b);
-    return Sum{add_parts(r0, r1), all};
+    if (n_late > 0) add_late(n_late);
+    __syncthreads();
+    uint32_t unused;
+    const uint32_t total = scan(lane == 0 ? all : 0u, unused, s.wave_b);
+    return Sum{add_parts(r0, r1), total};
   }
   __device__ __forceinline__ Sum add_left(int r0, int r1, const Left& left) const {
     const float last = value_of(left.key);
-    return add_weights(r0, r1, [&](float l, int i) { return is_left(last, left.index, l, i); }, [](float, int) {});
+    return add_weights(r0, r1, [&](float l, int i) { return is_left(last, left.index, l, i); }, [](const float (&)[EACH], int) {});
   }
   // The first token at which the sum is above `target` (below the sum of all), with s.part of the same
   __device__ __forceinline__ int locate(int r0, int r1, int what, const Left& left, uint64_t target) const {
@@ -389,23 +451,13 @@ template <int TYPE> struct Row {
     __syncthreads();
   }
 
-  // what a wave has to say, into the list as (key, ~index); s.counter counts beyond LIST too
-  __device__ __forceinline__ void listed(bool in, float l, int index) const {
-    const unsigned long long who = __ballot(in);
-    if (who == 0) return;
-    uint32_t to = 0;
-    if (tid % 64 == 0) to = atomicAdd(&s.counter, (uint32_t)__popcll(who));
-    to = __builtin_amdgcn_readfirstlane(to) + __popcll(who & ((1ull << (tid % 64)) - 1));
-    if (in && to < LIST) s.list[to] = composite(key_of(l), ~(uint32_t)index);
-  }
   // elements of lo or more into the list; returns their number, or some number above LIST
   __device__ __forceinline__ int collect(float lo) const {
     __syncthreads();
     if (tid == 0) s.counter = 0;
     __syncthreads();
     each(0, g.rounds, [&](int at, const float (&l)[EACH], int) {
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) listed(l[i] >= lo, l[i], at + i);
+      listed(l, at, [&](float v) { return v >= lo; });
       // (a wave may see a count of the round that others are in: it only goes on for nothing)
       return __hip_atomic_load(&s.counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) <= LIST;
     });
@@ -439,17 +491,18 @@ template <int TYPE> struct Row {
       // (a rough sum: 2^31 of the weight of `of`, in fp32)
       auto put_all = [&](auto values, auto numbers) {
         each(0, g.rounds, [&](int, const float (&l)[EACH], int) {
+          uint32_t bin[EACH], rough[EACH];
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) {  // (of what is out of range: anything)
+            const float below = of - l[i];
+            bin[i] = values ? min((uint32_t)(below * scale), BINS - 1u) : (hi - key_of(l[i])) >> drop;
+            rough[i] = numbers ? 1u : !values && l[i] == of ? 1u << 31 : (uint32_t)__builtin_amdgcn_exp2f(fmaf(below, -rate32, 31.f));
+          }
 #pragma unroll
           for (int i = 0; i < EACH; ++i) {
             const bool in = l[i] >= from && l[i] <= to;
-            const unsigned long long who = __ballot(in);
-            if (who == 0) continue;
-            n_range += __popcll(who);
-            if (!in) continue;
-            const float below = of - l[i];
-            const uint32_t bin = values ? min((uint32_t)(below * scale), BINS - 1u) : (hi - key_of(l[i])) >> drop;
-            const uint32_t rough = numbers ? 1u : !values && l[i] == of ? 1u << 31 : (uint32_t)__builtin_amdgcn_exp2f(fmaf(below, -rate32, 31.f));
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin]), (unsigned long long)rough);
+            n_range += __popcll(__ballot(in));
+            if (in) atomicAdd(reinterpret_cast<unsigned long long*>(&s.hist[bin[i]]), (unsigned long long)rough[i]);
           }
           return true;
         });
@@ -488,7 +541,7 @@ template <int TYPE> struct Row {
         }
       }
       const float bin_to = value_to(top_of), bin_from = value_of(low_of);
-      const Sum above = add_weights(0, g.rounds, [&](float l, int) { return l > bin_to; }, [&](float l, int i) { listed(l >= bin_from && l <= bin_to, l, i); });
+      const Sum above = add_weights(0, g.rounds, [&](float l, int) { return l > bin_to; }, [&](const float (&l)[EACH], int at) { listed(l, at, [&](float v) { return v >= bin_from && v <= bin_to; }); });
       const int inside = (int)s.counter;
       const uint64_t n_above = above.n, w_above = above.w, reached = by_n ? n_above : w_above;
       if (reached >= need && top_of < hi) {  // the border is above this bin
@@ -581,17 +634,17 @@ struct Wishes {
     summed = !greedy && k == 0 && (by_p || !by_m);  // the sum over the whole row is needed
   }
 };
-template <int TYPE> __device__ __forceinline__ Row<TYPE> row_of(const Args& g, Shared& s, int row, const Wishes& w) {
+template <int TYPE, class S> __device__ __forceinline__ Row<TYPE, S> row_of(const Args& g, S& s, int row, const Wishes& w) {
   if (threadIdx.x < 256) s.pow2[threadIdx.x] = exp2(threadIdx.x / 256.0);
-  return Row<TYPE>{g, s, static_cast<const char*>(g.a.logits) + (int64_t)row * g.a.stride * (TYPE == SI_BF16 ? 2 : 4), g.a.vocab, row, (int)threadIdx.x, 0.f,
+  return Row<TYPE, S>{g, s, static_cast<const char*>(g.a.logits) + (int64_t)row * g.a.stride * (TYPE == SI_BF16 ? 2 : 4), g.a.vocab, row, (int)threadIdx.x, 0.f,
                    w.greedy ? 0.0 : 369.3299304675746 / (double)w.t};
 }
 
 // A chunk of g.per rounds: its maximum, number of tokens, sum, and the maxima of its runs.  A wave goes on by itself, with a maximum of its own
 // to which it brings its sum; the waves are joined at the end.
-template <int TYPE> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, const Wishes& w, int chunk) {
+template <int TYPE, class S> __device__ __forceinline__ void sums_of_chunk(Row<TYPE, S>& R, const Wishes& w, int chunk) {
   const Args& g = R.g;
-  Shared& s = R.s;
+  S& s = R.s;
   const int tid = threadIdx.x, lane = tid % 64, r0 = chunk * g.per, r1 = min(r0 + g.per, g.rounds);
   uint32_t n = 0;
   double sum = 0.0;
@@ -637,11 +690,11 @@ template <int TYPE> __device__ __forceinline__ void sums_of_chunk(Row<TYPE>& R, 
 
 // Many rows: a launch for the chunks alone, two blocks a compute unit
 template <int TYPE> __global__ __launch_bounds__(THREADS, 8) void k_sample_sums(Args g) {
-  __shared__ Shared s;
+  __shared__ SumsShared s;
   const int row = blockIdx.x / g.chunks;
   const Wishes w(g.a, row);
-  Row<TYPE> R = row_of<TYPE>(g, s, row, w);
-  sums_of_chunk<TYPE>(R, w, blockIdx.x % g.chunks);
+  auto R = row_of<TYPE>(g, s, row, w);
+  sums_of_chunk(R, w, blockIdx.x % g.chunks);
 }
 
 // ALONE: the chunks too, and the block of a row that finishes last goes on; else a block a row
@@ -650,9 +703,9 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   const int row = ALONE ? blockIdx.x / g.chunks : blockIdx.x, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const si_sample_t& a = g.a;
   const Wishes w(a, row);
-  Row<TYPE> R = row_of<TYPE>(g, s, row, w);
+  auto R = row_of<TYPE>(g, s, row, w);
   if constexpr (ALONE) {
-    sums_of_chunk<TYPE>(R, w, blockIdx.x % g.chunks);
+    sums_of_chunk(R, w, blockIdx.x % g.chunks);
     // all of this block's values have reached memory before it is counted
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -681,7 +734,7 @@ template <int TYPE, bool ALONE> __global__ __launch_bounds__(THREADS) void k_sam
   const double one = ldexp(1.0, g.shift);
   // How the row is gone through in the end, and with which target
   int r0 = 0, r1 = g.rounds, what = R.WEIGHT;
-  typename Row<TYPE>::Left left{LOWEST_KEY, 0xffffffffu};
+  typename Row<TYPE, Shared>::Left left{LOWEST_KEY, 0xffffffffu};
   double sum = 0.0, rest = 0.0;
   int kept = (int)n_all;
   uint64_t w_all = 0;
