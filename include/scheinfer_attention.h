@@ -5,10 +5,10 @@
  * Between two feed-forward layers (scheinfer.h) a serving program calls, on one stream,
  *   si_norm          r' = res_scale r + y_scale gate * N1(y),  out = N2(r')
  *   (its own projection of out to q, k and v)
- *   si_cache_append  rotates q and k, writes k and v into the pages of the cache
- *   si_attend        the new tokens attend to the cache
+ *   si_cache_append  rotates q and k, writes k and v into the pages of the cache (si_cache_append_normed: after a norm of each head)
+ *   si_attend        the new tokens attend to the cache (si_attend_shared: what sequences share is read once for them)
  *   (its own output projection), si_norm again, then si_layer_forward
- * and, between steps, si_cache_extend / _trim / _fork / _compact.
+ * at the end of a step si_sample (scheinfer_sample.h) and, between steps, si_cache_extend / _trim / _fork / _compact.
  *
  * Conventions: those of scheinfer.h (codes, si_last_error, bf16 as bit patterns, stream as void*), and
  *  - every pointer inside the descriptors is a DEVICE address, aligned to its element; the descriptors themselves are HOST and are
