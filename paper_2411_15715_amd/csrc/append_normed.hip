@@ -3,7 +3,7 @@
 // L lanes have a head, 16 of its elements each (12 of 16 lanes with heads of 192, 6 of 8 with 96): the two vectors of 8 that turn into
 // each other, so that statistics, weights and rotation meet in registers and nothing is read twice.  Sums are over the 16 elements of a lane, then
 // over neighbouring lanes; the second moment of a norm about the mean is taken about the mean.  v goes its way as without the norm.
-// Bound by memory, as the append without a norm: 4099 tokens of 64 + 8 heads of 128 (160 MB) into e4m3 39.0 us, 4.1 TB/s (without norm 37.6); in
+// Bound by memory, as the append without a norm: 4099 tokens of 64 + 8 heads of 128 (160 MB) into e4m3 38.3 us, 4.2 TB/s (without norm 38.2); in
 // between, by the waves that fit: with 150 registers, the weights of q and k among them, 66 us, with 64 forced 46.  8 tokens: 4.7 us in the kernel.
 #include "si_error.h"
 #include "append_device.h"

@@ -5,6 +5,7 @@
 // so neighbours of the list whose tables begin with the same pages attend to these as rows of one sequence, which is read once for all of them and
 // fills the matrix instructions, and each to what it alone has.  Three launches: the plan makes pieces of both kinds, shared and own; their
 // blocks, one after the other, are cut into equal slices as those of whole sequences are in si_attend; and every row's sums are joined.
+// The plan takes 10 us and the joining 7 to 10 (64 sequences with 8000 shared tokens: 18 MB of sums), whatever the pieces take (attend_wide.h).
 #include "si_internal.h"
 #include "si_error.h"
 #include "attend_device.h"

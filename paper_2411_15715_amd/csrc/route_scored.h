@@ -5,6 +5,7 @@
 //   the k largest c of the open groups (ties: the lower expert),   w = scale s / sum of the k s   (or scale s)
 // Scores, sums and comparisons are in 64 bits: two experts whose c differ by less than 2^-24 of it would come out in the order of their
 // roundings, and the sum with a bias rounds scores that do differ together (of 8192 tokens on 256 experts dozens).
+// A wave a token, bound by its some 1000 vector instructions: 8192 tokens, top-8 of 256 in 8 groups, 18.5 us; 1 token, top-8 of 64, with the tables 4.5.
 #pragma once
 #include "si_internal.h"
 #include "route_device.h"
@@ -44,7 +45,7 @@ __device__ __forceinline__ void open_groups(int E, const si_score_t& rule, int l
   uint64_t worth[MAX_EXPERTS / 64];
   if (rule.group_best <= 2) {
     // P neighbouring lanes look at a group and keep its two largest keys.  (One lane a group, of 8 with 32 experts each, for 8192 tokens: the launch
-    // 38.9 us, this way and with the rounds below 16.)
+    // 38.9 us, this way and with the rounds below 18.5.)
     int P = 1;
     while (2 * P * n <= 64 && 2 * P <= of_group) P *= 2;
 #pragma unroll
