@@ -232,7 +232,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
 }
 
 constexpr int WIDE = 128;  // rows of a shared piece
-constexpr int MOST_ROWS = 1 << 16;
+constexpr int MOST_ROWS = 1 << 16, MOST_SUMS = 1 << 19;  // of a kv head, of all
 
 struct Layout {
   AttendCut alone;           // of si_attend
@@ -247,7 +247,7 @@ Layout lay_out(const si_cache_t& c, const si_attend_t& a) {
   l.alone = cut_attend(c, a);
   const int64_t of_entry = (int64_t)a.n_new * (a.n_heads / c.n_kv_heads);
   // (a block of the joining launch has 4 rows or more, and all rows have two sums; longer lists are si_attend's and need its scratch and that of shorter ones)
-  const int n = (int)std::min<int64_t>(a.n, MOST_ROWS / of_entry);
+  const int n = (int)std::min<int64_t>(a.n, std::min(MOST_ROWS, MOST_SUMS / c.n_kv_heads) / of_entry);
   const int64_t rows = n * of_entry;
   l.bytes = l.alone.scratch;
   if (n < 2) return l;

@@ -56,6 +56,8 @@ def test_calls_that_are_never_in_pieces_need_no_scratch_for_them():
     assert si.si_attend_shared_scratch_bytes(c, one) == si.si_attend_scratch_bytes(c, one)
     most = si.si_attend_shared_scratch_bytes(c, attend(n=4000, n_new=100, n_heads=64, max_len=5000))
     assert most < 2 << 30
+    many = cache(head_dim=128, n_kv_heads=1024, n_seqs=4096, max_pages=4096)
+    assert si.si_attend_shared_scratch_bytes(many, attend(n=4000, n_new=16, n_heads=1024, max_len=5000)) < 3 << 30
     for n in (2, 50, 81, 82, 1000, 3999):
         a = attend(n=n, n_new=100, n_heads=64, max_len=5000)
         assert si.si_attend_scratch_bytes(c, a) <= si.si_attend_shared_scratch_bytes(c, a) <= most
