@@ -7,6 +7,7 @@
 // between, by the waves that fit: with 150 registers, the weights of q and k among them, 66 us, with 64 forced 46.  8 tokens: 4.7 us in the kernel.
 #include "si_error.h"
 #include "append_device.h"
+#include "wave_device.h"
 
 #include <algorithm>
 #include <cmath>
@@ -49,12 +50,6 @@ __device__ __forceinline__ void weights_at(const void* w, int type, int at, floa
     }
   }
 }
-// The lanes of a head (of one wave) exchange by way of LDS, whose accesses are in order: only the compiler has to keep it
-__device__ __forceinline__ void wave_lds() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // GENERAL: each head has weights of its own, or the halves of the rotated part do not begin at a vector of 8, so that the other element of a
 // pair is in another lane.  Else the weights that all heads share lie in LDS, in fp32, and a lane has both elements of its pairs.
 template <int TYPE, int L, bool GENERAL> __device__ void normed_part(const NormedArgs& na, int block) {

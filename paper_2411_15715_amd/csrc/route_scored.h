@@ -5,10 +5,11 @@
 //   the k largest c of the open groups (ties: the lower expert),   w = scale s / sum of the k s   (or scale s)
 // Scores, sums and comparisons are in 64 bits: two experts whose c differ by less than 2^-24 of it would come out in the order of their
 // roundings, and the sum with a bias rounds scores that do differ together (of 8192 tokens on 256 experts dozens).
-// A wave a token, bound by its some 1000 vector instructions: 8192 tokens, top-8 of 256 in 8 groups, 18.5 us; 1 token, top-8 of 64, with the tables 4.5.
+// A wave a token, bound by its some 1000 vector instructions: 8192 tokens, top-8 of 256 in 8 groups, 17.8 us; 1 token, top-8 of 64, with the tables 4.5.
 #pragma once
 #include "si_internal.h"
 #include "route_device.h"
+#include "wave_device.h"
 
 namespace si {
 
@@ -17,12 +18,6 @@ struct ScoreLds {  // of a wave
   uint64_t c[MAX_EXPERTS];    // keys of s + b; then, of the groups, their worth
   uint32_t open[MAX_EXPERTS];
 };
-
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
-  return v;
-}
 
 // order-preserving map to an unsigned integer and back; NaN: 0, below -infinity
 __device__ __forceinline__ uint64_t score_key(double v) {
@@ -33,19 +28,13 @@ __device__ __forceinline__ double score_of(uint64_t key) {
   return __longlong_as_double((long long)(key == 0 ? ~0ull : key >> 63 ? key & ~(1ull << 63) : ~key));
 }
 
-// LDS of a wave: its accesses are in order, only the compiler has to keep it
-__device__ __forceinline__ void wave_lds() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // Which groups are open: lds.open[g].  lds.c holds the experts' keys.
 __device__ __forceinline__ void open_groups(int E, const si_score_t& rule, int lane, ScoreLds& lds) {
   const int n = rule.n_groups, of_group = E / n;
   uint64_t worth[MAX_EXPERTS / 64];
   if (rule.group_best <= 2) {
     // P neighbouring lanes look at a group and keep its two largest keys.  (One lane a group, of 8 with 32 experts each, for 8192 tokens: the launch
-    // 38.9 us, this way and with the rounds below 18.5.)
+    // 38.9 us, this way and with the rounds below 17.8.)
     int P = 1;
     while (2 * P * n <= 64 && 2 * P <= of_group) P *= 2;
 #pragma unroll
@@ -136,7 +125,7 @@ template <int N, class F> __device__ __forceinline__ void scored_rounds(const fl
       s[i] = x[i] == -INFINITY ? 0.0 : x[i] == top ? 1.0 : exp((double)x[i] - (double)top);
       sum += s[i];
     }
-    sum = wave_sum(sum);
+    sum = wave_total(sum);
     const double inv = sum == 0.0 ? 0.0 : 1.0 / sum;
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] *= inv;
@@ -155,10 +144,10 @@ template <int N, class F> __device__ __forceinline__ void scored_rounds(const fl
   wave_lds();
   if (rule.n_groups > 1) {
     open_groups(E, rule, lane, lds);
-    const int of_group = E / rule.n_groups;
+    const int of_group = E / rule.n_groups, inv = (65535 + of_group) / of_group;  // (e inv >> 16 is e / of_group for all e < 256)
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (ex[i] < MAX_EXPERTS && !lds.open[ex[i] / of_group]) { key[i] = 0; ex[i] = MAX_EXPERTS; }
+      if (ex[i] < MAX_EXPERTS && !lds.open[ex[i] * inv >> 16]) { key[i] = 0; ex[i] = MAX_EXPERTS; }
   }
   // The keys of a lane in order, (larger key, then lower expert) first, so that a round looks at one of them
   auto before = [](uint64_t k0, int e0, uint64_t k1, int e1) { return k0 > k1 || (k0 == k1 && e0 < e1); };
@@ -186,7 +175,7 @@ template <int N, class F> __device__ __forceinline__ void scored_rounds(const fl
     const int w = __builtin_ctzll(who), e = __builtin_amdgcn_readlane(ex[0], w);
 #pragma unroll
     for (int g = 0; g < N; ++g)
-      if (lane + 64 * g == r) sel[g] = e;
+      if ((g == 0 || k > 64) && lane + 64 * g == r) sel[g] = e;
     if (lane == w) {
 #pragma unroll
       for (int i = 0; i + 1 < N; ++i) { key[i] = key[i + 1]; ex[i] = ex[i + 1]; }
@@ -202,7 +191,7 @@ template <int N, class F> __device__ __forceinline__ void scored_rounds(const fl
   }
   const double scale = rule.scale == 0.f ? 1.0 : (double)rule.scale;
   if (rule.renorm) {
-    sum = wave_sum(sum);
+    sum = wave_total(sum);
 #pragma unroll
     for (int g = 0; g < N; ++g) v[g] = sum == 0.0 ? 0.0 : v[g] / sum;
   }
