@@ -220,6 +220,25 @@ def test_draws_follow_the_distribution():
     assert np.all(np.abs(np.bincount(token, minlength=50) - n * w / w.sum()) <= 1)
 
 
+@pytest.mark.parametrize("R, V", [(51, 40000), (52, 40000), (130, 40000), (300, 40000), (450, 33000)])
+def test_many_rows(R, V):
+    """chunks of one to four rounds, the last of a row shorter, in a launch of their own (51 rows: in the same); some rows are compared"""
+    x = normal(R, V, peaks=9)
+    limits = [dict(), dict(top_k=60), dict(top_p=0.9), dict(min_p=0.01), dict(temperature=0.0), dict(top_k=3000, top_p=0.8), dict(temperature=1.7, top_p=0.97), dict(temperature=0.3)]
+    full = {n: np.array([limits[r % 8].get(n, v) for r in range(R)], np.int32 if n == "top_k" else np.float32) for n, v in NONE.items()}
+    u = np.random.default_rng(R).random(R, dtype=np.float32)
+    some = sorted({r for r in range(0, R, max(1, R // 24))} | {R - 1})
+    args = {r: tuple(float(full[n][r]) if n != "top_k" else int(full[n][r]) for n in NONE) for r in some}
+    l = {r: x[r].cpu().numpy() for r in some}
+    for r in some:
+        u[r] = clear_of_borders(l[r], *args[r], u[r])
+    token, prob, kept = sample(x, full, u)
+    for r in some:
+        want = one_row(l[r], *args[r], float(u[r]))
+        assert (int(token[r]), int(kept[r])) == (want[0], want[2]), (r, args[r], float(u[r]))
+        assert abs(float(prob[r]) - want[1]) <= (2.0 ** -24 + 2.0 ** -25) * want[1] + 2.0 ** -42, r
+
+
 def test_one_scratch_for_calls_of_all_sizes():
     big = normal(40, 20000)
     d = si.si_sample_t(rows=64, vocab=70000, type=si.SI_F32)
