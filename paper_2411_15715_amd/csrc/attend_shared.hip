@@ -5,10 +5,11 @@
 // so neighbours of the list whose tables begin with the same pages attend to these as rows of one sequence, which is read once for all of them and
 // fills the matrix instructions, and each to what it alone has.  Three launches: the plan makes pieces of both kinds, shared and own; their
 // blocks, one after the other, are cut into equal slices as those of whole sequences are in si_attend; and every row's sums are joined.
-// The plan takes 10 us and the joining 7 to 10 (64 sequences with 8000 shared tokens: 18 MB of sums), whatever the pieces take (attend_wide.h).
+// The plan takes 8 to 10 us and the joining 7 to 10 (64 sequences with 8000 shared tokens: 18 MB of sums), whatever the pieces take (attend_wide.h).
 #include "si_internal.h"
 #include "si_error.h"
 #include "attend_device.h"
+#include "wave_device.h"
 
 #include <algorithm>
 #include <cstdlib>
@@ -55,7 +56,7 @@ __device__ __forceinline__ Run joined(const Run& a, const Run& b) {  // b begins
 
 // A block for each entry: the pages that it has in common with the one before.  The block that finishes last forms the groups; it alone is what the call
 // waits for, so all that it needs again is in shared memory and each list is scanned once (13 to 16 us with scans over lists in memory and a
-// thread that wrote the slices of a piece in turn; 10 to 11 us as it is for 64 and 45 sequences, most of it one round trip to memory or one barrier after another).  LOCAL: where the notes are
+// thread that wrote the slices of a piece in turn; 8.3 and 10.4 as it is for 64 and 45 sequences, most of it one round trip to memory or one barrier after another).  LOCAL: where the notes are
 // is known when this is compiled.  A pointer to either memory would not do: such an address is told by its base before the instruction's
 // offset is added, and the compiler may take one from a base that lies below the array.
 template <bool LOCAL>
@@ -122,14 +123,21 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
       if (!any) r.pages = min(r.pages, common[i]);
     }
     const bool ends = in && (i + 1 == n || begins(i + 1));
-    for (int d = 1; d < 64; d *= 2) {
-      const Run o{__shfl_up(r.first, d), __shfl_up(r.pages, d), __shfl_up(r.shortest, d), __shfl_up(r.longest, d)};
-      const bool o_any = __shfl_up((int)any, d);
-      if (lane >= d && !any) {
+    auto step = [&](auto ctrl, auto rows, bool there) {  // there: a lane that this one takes a run from
+      constexpr int C = decltype(ctrl)::value, M = decltype(rows)::value;
+      const Run o{(int)moved<C, M>((uint32_t)r.first), (int)moved<C, M>((uint32_t)r.pages), (int)moved<C, M>((uint32_t)r.shortest), (int)moved<C, M>((uint32_t)r.longest)};
+      const bool o_any = moved<C, M>((uint32_t)any) != 0;
+      if (there && !any) {
         r = joined(o, r);
         any = o_any;
       }
-    }
+    };
+    step(std::integral_constant<int, SHIFT + 1>{}, std::integral_constant<int, 0xf>{}, lane % 16 >= 1);
+    step(std::integral_constant<int, SHIFT + 2>{}, std::integral_constant<int, 0xf>{}, lane % 16 >= 2);
+    step(std::integral_constant<int, SHIFT + 4>{}, std::integral_constant<int, 0xf>{}, lane % 16 >= 4);
+    step(std::integral_constant<int, SHIFT + 8>{}, std::integral_constant<int, 0xf>{}, lane % 16 >= 8);
+    step(std::integral_constant<int, FROM_ROW>{}, std::integral_constant<int, 0xa>{}, lane / 16 % 2 == 1);
+    step(std::integral_constant<int, FROM_HALF>{}, std::integral_constant<int, 0xc>{}, lane >= 32);
     __syncthreads();
     if (lane == 63) { s_run[wave] = r; s_begins[wave] = any; }
     __syncthreads();
@@ -141,11 +149,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
     // (beyond the last entry a run is empty and changes nothing)
     const int members = i - r.first + 1, tokens = ends && members > 1 ? r.pages * g.c.page_tokens : 0, rows = members * of_entry;
     const int pieces = tokens > 0 ? (rows + g.wide_rows - 1) / g.wide_rows : 0;
-    int at = pieces;
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(at, d);
-      if (lane >= d) at += o;
-    }
+    int at = (int)scan_wave((uint32_t)pieces);
     if (lane == 63) s_offset[wave] = at;
     __syncthreads();
     at += n_shared - pieces;
@@ -180,11 +184,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
   for (int k0 = 0; k0 < max(n_own, n_shared); k0 += THREADS) {
     const int k = k0 + tid;
     int64_t x[2] = {k < n_shared ? shared_to[k] : 0, k < n_own ? own_to[k] : 0};
-    for (int d = 1; d < 64; d *= 2)
-      for (int q = 0; q < 2; ++q) {
-        const int64_t o = __shfl_up(x[q], d);
-        if (lane >= d) x[q] += o;
-      }
+    for (int q = 0; q < 2; ++q) x[q] = (int64_t)scan_wave((uint64_t)x[q]);
     __syncthreads();
     if (lane == 63) { s_sum[0][wave] = x[0]; s_sum[1][wave] = x[1]; }
     __syncthreads();
@@ -202,20 +202,20 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
   // Equal slices of each list's blocks: slice w is [end(w - 1), end(w)) with end(w) = (w + 1) total / G.  (Quotients by way of double: exact, as the dividends
   // stay below 2^53.)
   auto quotient = [](int64_t x, int64_t y) { return (int64_t)((double)x / (double)y); };
-#pragma unroll 1
-  for (int q = 0; q < 2; ++q) {
+  {
+    const int q = wave * 2 / WAVES, id = tid % (THREADS / 2);  // (half of the threads a list)
     const int64_t *to = q ? own_to : shared_to, sum = q ? total[1] : total[0];
     const int pieces = q ? n_own : n_shared, slices = q ? g.own.slices : g.shared.slices, G = (int)min<int64_t>(slices, sum);
     int2* parted = q ? g.own.parted : g.shared.parted;
     SliceStart* starts = q ? g.own.starts : g.shared.starts;
 #pragma unroll 1
-    for (int k = tid; k < pieces; k += THREADS) {
+    for (int k = id; k < pieces; k += THREADS / 2) {
       int of[2];  // the slices of its first and last block: those whose ends are the first beyond them
       for (int h = 0; h < 2; ++h) of[h] = (int)quotient((h ? to[k] : (k > 0 ? to[k - 1] : 0) + 1) * G - 1, sum);
       parted[k] = make_int2(of[0], of[1] - of[0] + 1);
     }
 #pragma unroll 1
-    for (int w = tid; w < slices; w += THREADS) {
+    for (int w = id; w < slices; w += THREADS / 2) {
       SliceStart start{0, 0, 0};
       if (w < G) {
         const int64_t begin = quotient(w * sum, G), end = quotient((w + 1) * sum, G);
