@@ -110,7 +110,7 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
   // prompts with the same few words before them are two groups).
   auto begins = [&](int i) { return i == 0 || common[i] == 0 || 2ll * common[i] < max(i > 1 ? common[i - 1] : 0, i + 1 < n ? common[i + 1] : 0); };
 
-  Run carry{0, 0x7fffffff, 0x7fffffff, 0};  // the group that is open before this round
+  Run carry{0, 0x7fffffff, 0x7fffffff, 0};  // the group that is open before these entries
   int n_shared = 0;
   for (int e0 = 0; e0 < n; e0 += THREADS) {
     const int i = e0 + tid;
