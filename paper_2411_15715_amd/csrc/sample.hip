@@ -432,9 +432,13 @@ template <int TYPE, class S> struct Row {
   // does, of the last.  A pass puts numbers or rough sums of the range into bins; the next takes what is above the bin in which they reach `need` exactly,
   // and lists what is in it.  Where that shows another bin, or the list is full, once more with what is left of the range.  Bins are equal parts of the logits'
   // range at first, where a lower end is known, and of the keys' then: keys are dense next to 0, where a range that holds it would leave
-  // few bins for the rest, but three times are enough for any values.
+  // few bins for the rest.  Rough sums are some 1e-6 of the range off, so the bin can be one beside the border's: what is known exactly tells.
   __device__ __forceinline__ Border border(uint32_t lo, uint32_t hi, bool by_n, uint64_t need) const {
-    uint64_t done = 0, n_hi = 0;  // number or sum above hi, as far as known; number above hi
+    uint64_t done = 0;  // number or sum above hi
+    // The border is at or above `least_key`, and so many tokens are; lo is above it while the range is a bin that may not have the border
+    uint32_t least_key = lo;
+    uint64_t n_least = 0;
+    bool counted = false;
     const float rate32 = (float)fmin(rate / 256, 1e30), range = value_of(hi) - value_of(lo);
     bool by_value = lo > LOWEST_KEY && range > 1e-30f && range < 1e30f;
     const float scale = (BINS - 1) / range;
@@ -472,6 +476,8 @@ template <int TYPE, class S> struct Row {
       if (tid % 64 == 0) atomicAdd(&s.seen, n_range);
       __syncthreads();
       n_range = s.seen;
+      if (!counted) n_least = n_range;  // (the first range is all from its lower end on)
+      counted = true;
       const uint64_t h0 = s.hist[2 * tid], h1 = s.hist[2 * tid + 1], goal = by_n ? need - done : (uint64_t)fmin(fmax((double)(need - done) / weight(of, g.shift) * 0x1p31, 1.0), 1e18);
       uint64_t x;
       scan(h0 + h1, x, s.wave_a);
@@ -496,7 +502,6 @@ template <int TYPE, class S> struct Row {
           lo = low_of;
           hi = top_of;
           done += s.found[1];
-          n_hi += s.found[1];
           continue;
         }
       }
@@ -505,24 +510,24 @@ template <int TYPE, class S> struct Row {
       const int inside = (int)s.counter;
       const uint64_t n_above = above.n, w_above = above.w, reached = by_n ? n_above : w_above;
       if (reached >= need && top_of < hi) {  // the border is above this bin
-        lo = top_of + 1;
+        lo = least_key = top_of + 1;
+        n_least = n_above;
         continue;
       }
-      const bool more = n_hi + n_range > n_above + inside;  // below low_of
+      const bool more = n_least > n_above + inside;  // below low_of
       if (inside > LIST && low_of < top_of) {
         lo = low_of;
         hi = top_of;
         done = reached;
-        n_hi = n_above;
         continue;
       }
       if (inside > LIST) {  // more tokens of one logit than the list holds: as many as are needed, from the lowest index
         const uint64_t each_w = whole(value_of(top_of)), most = inside;
         const uint64_t k = by_n ? min(need - reached, most) : each_w == 0 ? most : min((need - reached + each_w - 1) / each_w, most);
         if (more && (by_n ? reached + most : reached + most * each_w) < need) {
+          lo = least_key;
           hi = low_of - 1;
           done = by_n ? reached + most : reached + most * each_w;
-          n_hi = n_above + most;
           continue;
         }
         const Left same{top_of, 0};
@@ -540,9 +545,9 @@ template <int TYPE, class S> struct Row {
       uint64_t before;
       const uint64_t listed_w = scan(w[0] + w[1], before, s.wave_a), all = by_n ? n_above + inside : w_above + listed_w;
       if (all < need && more) {  // the border is below this bin
+        lo = least_key;
         hi = low_of - 1;
         done = all;
-        n_hi = n_above + inside;
         continue;
       }
       const uint64_t last = min(need, all);
