@@ -170,8 +170,9 @@ struct Span {
   int entry;                    // of a piece
   __device__ __forceinline__ Span(const AttendArgs& g, const Piece& p) {
     seq = p.seq;
-    window = g.a.window;
-    len = why = 0;
+    len = p.sight + g.a.n_new - 1;
+    window = g.a.window < len ? g.a.window : 0;
+    why = 0;
     first = p.sight;
     lo = p.lo; hi = p.hi; lo_all = p.lo_all; hi_all = p.hi_all;
     fb = p.fb; nb = p.nb;

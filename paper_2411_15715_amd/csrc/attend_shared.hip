@@ -161,7 +161,8 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
     if (ends) {
       tokens_of[r.first] = tokens;
       piece_of[r.first] = pieces > 0 ? at : -1;
-      const int lo = g.window ? min(tokens, max(0, r.shortest - g.n_new + 1 - g.window)) : 0, lo_all = g.window ? min(tokens, max(0, r.longest - g.window)) : 0;
+      const bool windows = g.window > 0 && tokens > 0;  // (all of a group have n_new tokens then: no difference passes 32 bits)
+      const int lo = windows ? min(tokens, max(0, r.shortest - g.n_new + 1 - g.window)) : 0, lo_all = windows ? min(tokens, max(0, r.longest - g.window)) : 0;
       const int nb = tokens > lo ? tokens / B - lo / B : 0;
       for (int k = 0; k < pieces; ++k) {
         g.shared.pieces[at + k] = Piece{seqs[r.first], r.first * of_entry + k * g.wide_rows, min(g.wide_rows, rows - k * g.wide_rows), lo, tokens, lo_all, tokens, lo / B, nb, -1, 0};
@@ -174,8 +175,9 @@ __global__ __launch_bounds__(THREADS) void k_share(PlanArgs g) {
   for (int k = tid; k < n_own; k += THREADS) {
     const int i = k / g.chunks, row0 = (k - i * g.chunks) * g.block_rows, rows = min(g.block_rows, of_entry - row0), first = firsts[i], from = tokens_of[first];
     const int sight = lens[i] - g.n_new + 1, t0 = row0 / g.per, t1 = (row0 + rows - 1) / g.per;
-    const int hi = max(0, sight + t1), lo = g.window ? max(from, sight + t0 - g.window) : from, nb = hi > lo ? (hi + B - 1) / B - lo / B : 0;
-    g.own.pieces[k] = Piece{seqs[i], i * of_entry + row0, rows, lo, hi, g.window ? max(from, sight + t1 - g.window) : from, max(0, sight + t0), lo / B, nb, i, sight};
+    const int window = g.window < lens[i] ? g.window : 0;  // (sight may be negative: less the longest windows it would pass 32 bits)
+    const int hi = max(0, sight + t1), lo = window ? max(from, sight + t0 - window) : from, nb = hi > lo ? (hi + B - 1) / B - lo / B : 0;
+    g.own.pieces[k] = Piece{seqs[i], i * of_entry + row0, rows, lo, hi, window ? max(from, sight + t1 - window) : from, max(0, sight + t0), lo / B, nb, i, sight};
     own_to[k] = max(1, nb);
     if (row0 == 0) g.group[i] = make_int2(piece_of[first], first);
   }
