@@ -80,9 +80,10 @@ template <int TYPE, int D> struct Wide {
     const int tiles = pc.rows > 64 ? 4 : pc.rows > 32 ? 2 : 1, streams = WAVES / tiles, stream = wave / tiles, row0 = wave % tiles * ROWS;
     const bool here = row0 < pc.rows;
 
-    // this lane's row of q, as right operands; a negative scale goes with its signs
+    // this lane's row of q, as right operands; a negative scale goes with its signs, and the smallest number there is stands for 0 (a product with what a
+    // window hides, -infinity, has to stay it; scores of up to 10^38 are as good as 0 this way)
     const int row = row0 + col;
-    const float sc_all = g.scale2 * (TYPE == SI_KV_E4M3 && c.scale_k ? c.scale_k[kv] : 1.f), sc = fabsf(sc_all);
+    const float sc_all = g.scale2 * (TYPE == SI_KV_E4M3 && c.scale_k ? c.scale_k[kv] : 1.f), sc = sc_all == 0.f ? 1.4e-45f : fabsf(sc_all);
     const int tok = row < pc.rows ? (pc.first + row) / per : -1;
     u32x4 q[D / 16];
     {
