@@ -311,7 +311,7 @@ extern "C" int si_attend_shared(const si_cache_t* c, int32_t layer, const si_att
   if (int rc = check(c, a, who)) return rc;
   if (nothing) return SI_OK;
   const Layout l = lay_out(*c, *a);
-  if (!a->scratch || a->scratch_bytes < l.bytes || (reinterpret_cast<uintptr_t>(a->scratch) & 15) != 0)
+  if (l.bytes > 0 && (!a->scratch || a->scratch_bytes < l.bytes || (reinterpret_cast<uintptr_t>(a->scratch) & 15) != 0))  // (none needed: an empty tensor's address may be NULL)
     return set_error(SI_EINVAL, "%s: %lld bytes of scratch needed, 16-byte aligned", who, (long long)l.bytes);
   char* p = static_cast<char*>(a->scratch);
   AttendArgs g = attend_args(*c, *a, layer, l.alone);
