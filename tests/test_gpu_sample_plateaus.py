@@ -1,9 +1,9 @@
 """si_sample on rows with a few heavy plateaus of equal logits, where top_p ends at a plateau's end or a little beyond it: more tokens of one value than are put in
 order at once, and sums whose parts differ by 2^20 and more.
 
-The expected number of tokens is formed with sums of 64-bit mantissas; every p of the tests is 1e-11 of the sum or more away from the border between two
-numbers of tokens (checked here, on the CPU): the kernel's sums are some 1e-12 off (131072 weights cut to 2^-45 of the largest are 4e-9 of it, of sums
-above 3000 times the largest; sums of doubles), those here 2^-64 times 131072."""
+The expected number of tokens is formed with sums of 64-bit mantissas of the weights as the header has them, multiples of 2^-(62 - ceil(log2 vocab)), up to
+top_p times the sum of the weights as they are.  Every p of the tests is 1e-11 of the sum or more away from the border between two numbers of tokens
+(checked here, on the CPU): sums of doubles are some 1e-14 off, a weight next to a multiple may be cut to the one below, those here 2^-64 times 131072."""
 import numpy as np
 import pytest
 import torch
@@ -16,9 +16,11 @@ pytestmark = pytest.mark.gpu
 def expected(l, t, p):
     """number of tokens left, indices left, their weights; None where p is too near to a border"""
     w = np.exp((l.astype(np.float64) - float(l.max())) / t).astype(np.longdouble)
+    goal = np.longdouble(p) * np.sum(w)
+    unit = np.longdouble(2.0) ** (int(np.ceil(np.log2(len(l)))) - 62)
+    w = np.floor(w / unit) * unit
     order = np.argsort(-l, kind="stable")
     sums = np.cumsum(w[order])
-    goal = np.longdouble(p) * sums[-1]
     n = 1 + int(np.searchsorted(sums, goal))
     if sums[n - 1] - goal < 1e-11 * sums[-1] or goal - (sums[n - 2] if n > 1 else 0) < 1e-11 * sums[-1]:
         return None
@@ -31,7 +33,7 @@ def check_rows(l, t, ps, dtype=torch.float32, seed=0):
     rng = np.random.default_rng(seed)
     t = float(np.float32(t))
     rows = [(p, e) for p, e in ((float(np.float32(p)), expected(l, t, float(np.float32(p)))) for p in ps) if e is not None]
-    assert len(rows) >= min(3, len(ps))
+    assert len(rows) >= min(2, len(ps))
     us, tokens, probs = [], [], []
     for _, (n, left, w) in rows:
         sums = np.cumsum(w)
