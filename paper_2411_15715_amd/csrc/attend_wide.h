@@ -6,10 +6,12 @@
 // g, i < 4: the tokens of the chunks h and 2 + h of V).  All rows see all positions but for a window, so that there is no mask in the loop.  Of at most 32 or 64
 // rows the waves take the cache blocks in turn.
 // Beside each such block runs one with sequences' own tokens (attend_device.h), which is bound by memory where this one is by instructions.
-// Measured: 64 sequences with 8000 shared and up to 500 own tokens, 4 rows each, heads of 128: 37 us, of which the matrix instructions are busy a
-// third (si_attend 143: it reads 1.1 GB, in part from the caches, where this reads 112 MB); 45 windows of e4m3 over 6 prompts, 18 rows each, 89 us, most of it the
-// codes, which every wave of a block converts for itself.  A wave's products of a cache block take 768 cycles and its vector instructions some 1000, one after the
-// other; two tiles of V at a time, which could overlap them, need more registers than there are (50 us a call become 56).
+// Measured: 64 sequences with 8000 shared and up to 500 own tokens, 4 rows each, heads of 128: 37 us (si_attend 143: it reads 1.1 GB, in part from the
+// caches, where this reads 112 MB); 45 windows of e4m3 over 6 prompts, 18 rows each, 89 us.  Compute units are busy 27 and 62 us of these, matrix
+// instructions a fifth of that.  A wave's products of a cache block take 768 cycles and its vector instructions some 1000, one after the other: in 16 turns 12
+// us of the 37; what takes the rest is not known.  Two tiles of V at a time, which could overlap them, need more registers than there are (50 us a call
+// become 56).  Of e4m3 every wave of a block converts the codes for itself, and slices, which are equal in cache blocks, are not in time: of a
+// piece of up to 32 rows the four waves take the blocks in turn.
 #pragma once
 #include "attend_device.h"
 

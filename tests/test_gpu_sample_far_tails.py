@@ -62,7 +62,7 @@ def test_tokens_of_a_far_tail(name):
 
 @pytest.mark.parametrize("name", sorted(ROWS))
 def test_a_far_tail_takes_a_few_times_an_ordinary_row(name):
-    """at most four turns of the search for one; with bins that are passed one by one these rows took up to a hundred"""
+    """a few turns of the search instead of one; with bins that are passed one by one these rows took up to four hundred"""
     rng = np.random.default_rng(1)
     usual = time_of((2 * rng.standard_normal(V)).astype(np.float32), 1.0, 0.9)
     t = time_of(*ROWS[name])
